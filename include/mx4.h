@@ -268,6 +268,98 @@ int mx_gemm_mbs_elem_grouped(mx_elem_t a_elem, const uint8_t* a_codes, const uin
                              int32_t num_groups, const int64_t* row_offsets, int64_t M_total, int64_t N, int64_t K,
                              mx_dtype_t c_dtype, void* C, int64_t ldc, void* stream);
 
+/* ---- a paged key/value cache in MXFP4, and the attention that reads it ----
+ * The same formats applied to the other large operand of a serving step: keys and values, quantized per token and head
+ * along the head's D elements exactly as mx_quantize / mx_quantize_mbs quantize a row of K = D (Sec. 2.2, 4.2, 4.3.1; the
+ * window of 128 elements is a head of 128).  x_hat = value(code) * 2^(E-127) / F as everywhere.
+ *
+ * Cache: num_pages pages of page_size tokens (a power of two, 16 to 4096), Hkv heads of D elements, D one of 64, 96, 128,
+ * 192, 256; other sizes return MX_EUNSUPPORTED.  A token's place is its slot = page * page_size + place.  Arrays (uint8):
+ *   k_codes  [num_pages, Hkv, D/32, page_size, 16]    the 16 bytes of a 32-element block, canonical nibble order
+ *   v_codes  [num_pages, Hkv, page_size/4, D/8, 4, 4] 4 neighbouring tokens of 8 codes (4 bytes) each
+ *   k_scales, v_scales  [num_pages, Hkv, D/32, page_size]
+ *   k_mbs, v_mbs        [num_pages, Hkv, ceil(D/128), page_size], or both NULL: no MBS words
+ * Alignment: codes 16 bytes, scales 4 bytes, rows of q, k, v and outputs 16 bytes with leading dimensions (elements from
+ * one token's heads to the next one's; a token's heads lie next to each other) a multiple of 8.
+ *
+ * Indexes that are on the GPU are not trusted with memory: slots outside the cache are not written or read, pages outside
+ * it hold no keys, rows outside the query tensor are not touched. */
+typedef enum {
+    MX_ROPE_HALF = 0, /* rotates elements i and i + R/2   */
+    MX_ROPE_PAIRS = 1 /* rotates elements 2i and 2i + 1   */
+} mx_rope_t;
+
+/* Where the tokens of a step go.  Request s has ctx_lens[s] tokens in the cache, in the pages block_table[s, 0 ..
+ * ceil(ctx/page_size)), and brings new_lens[s] more (negative lengths count as 0).  Pages it then lacks are taken from
+ * free_pages[free_start[0] ..), request after request; they are written into its row of block_table [num_seqs, max_pages]
+ * (other entries stay).  Written besides:
+ *   row_offsets int64 [num_seqs+1]  rows of request s among the step's tokens: row_offsets[s] .. row_offsets[s+1]-1
+ *   kv_lens int32 [num_seqs]        ctx + new
+ *   slots int64 [T], positions int32 [T]  of every token; -1 at and beyond row_offsets[num_seqs]
+ *   free_next int32 [1]             free_start[0] and the pages that were wanted; beyond free_count if they were too few
+ * A token whose page is missing (free_pages or the table's row is at its end) gets slot -1.  All arrays are DEVICE memory;
+ * nothing is allocated on the host, so the call can be captured; the next step takes kv_lens and free_next as its ctx_lens and
+ * free_start.  The sum of new_lens is at most T (tokens beyond T get no place).  num_seqs <= 4096, else MX_EUNSUPPORTED;
+ * max_pages * page_size <= 2^30.  kv_lens may not be ctx_lens or new_lens, free_next not free_start (MX_EINVAL). */
+int mx_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int64_t num_seqs, int64_t page_size, int32_t* block_table,
+               int64_t max_pages, const int32_t* free_pages, int64_t free_count, const int32_t* free_start, int64_t T,
+               int64_t* row_offsets, int32_t* kv_lens, int64_t* slots, int32_t* positions, int32_t* free_next, void* stream);
+
+/* RMS norm and rotation of every head of queries [T, Hq, D] and keys [T, Hkv, D] (bf16) in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * weight        (weight bf16 [D]; a NULL weight: y = x)
+ *   (y_i, y_j) -> (y_i cos - y_j sin, y_j cos + y_i sin)   on the first R elements, R a multiple of 16 (else MX_EUNSUPPORTED)
+ * cos_sin: fp32 [max_position, R], a position's R/2 cosines and then its R/2 sines; NULL with R = 0: no rotation.  Evaluated in
+ * fp64 and rounded to fp32 and then to bf16.  A token of negative position (padding) keeps its outputs as they are; the rotated
+ * elements of one at or beyond max_position are NaN.  Outputs may be the inputs themselves.  Hq or Hkv may be 0. */
+int mx_qk_norm_rope(const void* q_bf16, int64_t ldq, const void* k_bf16, int64_t ldk, const int32_t* positions,
+                    const float* cos_sin_or_null, int64_t max_position, const void* q_weight_or_null, const void* k_weight_or_null,
+                    double eps, mx_rope_t style, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t R,
+                    void* q_out, int64_t ldq_out, void* k_out, int64_t ldk_out, void* stream);
+
+/* Quantizes keys and values [T, Hkv, D] into the places slots[t] of the cache; rows of other slots stay as they are.  Slots of a
+ * call are distinct: of two tokens with the same one the row may hold parts of either. */
+int mx_kv_write(const void* k_bf16, int64_t ldk, const void* v_bf16, int64_t ldv, const int64_t* slots, mx_rule_t rule,
+                uint8_t* k_codes, uint8_t* k_scales, uint8_t* k_mbs_or_null, uint8_t* v_codes, uint8_t* v_scales, uint8_t* v_mbs_or_null,
+                int64_t num_pages, int64_t page_size, int64_t T, int64_t Hkv, int64_t D, void* stream);
+
+/* mx_qk_norm_rope and mx_kv_write of the rotated keys and of the values in one launch; the keys in bf16 are not written.  q_out
+ * and the cache hold the same bits as after the two calls.  A token of negative position is left out altogether. */
+int mx_qk_norm_rope_kv_write(const void* q_bf16, int64_t ldq, const void* k_bf16, int64_t ldk, const void* v_bf16, int64_t ldv,
+                             const int32_t* positions, const float* cos_sin_or_null, int64_t max_position,
+                             const void* q_weight_or_null, const void* k_weight_or_null, double eps, mx_rope_t style,
+                             const int64_t* slots, mx_rule_t rule, uint8_t* k_codes, uint8_t* k_scales, uint8_t* k_mbs_or_null,
+                             uint8_t* v_codes, uint8_t* v_scales, uint8_t* v_mbs_or_null, int64_t num_pages, int64_t page_size,
+                             int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t R, void* q_out, int64_t ldq_out, void* stream);
+
+/* Rows of the cache by slot, rounded as by mx_dequantize: k_out, v_out [T, Hkv, D] (either may be NULL) of out_dtype.  Rows
+ * whose slot is outside the cache stay as they are. */
+int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* k_mbs_or_null,
+               const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs_or_null, int64_t num_pages, int64_t page_size,
+               int64_t T, int64_t Hkv, int64_t D, mx_dtype_t out_dtype, void* k_out, int64_t ldk, void* v_out, int64_t ldv,
+               void* stream);
+
+/* Attention of bf16 queries over the cache.  Request s owns the query rows row_offsets[s] .. row_offsets[s+1]-1 (n of them) and
+ * the keys 0 .. kv_lens[s]-1, key j in place j % page_size of page block_table[s, j / page_size]; its last query stands on its
+ * last key.  Query head h reads key head h / (Hq/Hkv).  Row i sees
+ *   causal:      keys 0 .. p, p = kv_lens[s] - n + i;  with window > 0 only the last `window` of them
+ *   not causal:  all keys (window must be 0)
+ * of those whose page exists.  out = softmax(scale q . k_hat) v_hat, bf16 [T, Hq, D]; lse (natural logarithm of the sum of
+ * exponentials, fp32 [T, Hq]) if not NULL.  A row that sees no key: zeros, -inf.  Rows at or beyond row_offsets[num_seqs] are not
+ * written.  Requests' rows do not overlap.  NaN in a key or value reaches the rows that see it and no others.
+ * Scores, softmax and sums in fp32, weights rounded to bf16 for the product with the values.
+ * |x_hat F| of the cache's rows has to be below 2^127 (what mx_kv_write stores of |x| < 2^125 is).
+ * workspace: DEVICE memory, 16-byte aligned, of at least mx_attention_kv_workspace(...) bytes, which the call overwrites; calls
+ * that can run at the same time need one each. */
+int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,
+                    int64_t max_pages, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* k_mbs_or_null,
+                    const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs_or_null, int64_t num_pages,
+                    int64_t page_size, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, float scale, int causal,
+                    int64_t window, void* out_bf16, int64_t ldo, float* lse_or_null, void* workspace, int64_t workspace_bytes,
+                    void* stream);
+
+/* Bytes that mx_attention_kv wants for these sizes, whatever the lengths; a negative status if it does not take them. */
+int64_t mx_attention_kv_workspace(int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
+
 /* Human-readable text for a status code (static storage, host pointer). */
 const char* mx_status_string(int status);
 

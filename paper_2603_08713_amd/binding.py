@@ -94,6 +94,23 @@ def load_library() -> ctypes.CDLL:
     L.mx_gemm_mbs_elem_grouped.argtypes = [ci, vp, vp, vp, ci, vp, vp, vp, ctypes.c_int32, vp, i64, i64, i64, ci, vp, i64, vp]
     L.mx_internal_gemm_elem.restype = ci
     L.mx_internal_gemm_elem.argtypes = [ci, vp, vp, vp, ci, vp, vp, vp, i64, i64, i64, ci, vp, i64, ci, vp]
+    ip, d, f = vp, ctypes.c_double, ctypes.c_float
+    L.mx_kv_plan.restype = ci
+    L.mx_kv_plan.argtypes = [ip, ip, i64, i64, ip, i64, ip, i64, ip, i64, vp, ip, vp, ip, ip, vp]
+    L.mx_qk_norm_rope.restype = ci
+    L.mx_qk_norm_rope.argtypes = [vp, i64, vp, i64, ip, vp, i64, vp, vp, d, ci, i64, i64, i64, i64, i64, vp, i64, vp, i64, vp]
+    L.mx_kv_write.restype = ci
+    L.mx_kv_write.argtypes = [vp, i64, vp, i64, vp, ci, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, vp]
+    L.mx_qk_norm_rope_kv_write.restype = ci
+    L.mx_qk_norm_rope_kv_write.argtypes = [vp, i64, vp, i64, vp, i64, ip, vp, i64, vp, vp, d, ci, vp, ci, vp, vp, vp, vp, vp, vp,
+                                           i64, i64, i64, i64, i64, i64, i64, vp, i64, vp]
+    L.mx_kv_read.restype = ci
+    L.mx_kv_read.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, ci, vp, i64, vp, i64, vp]
+    L.mx_attention_kv.restype = ci
+    L.mx_attention_kv.argtypes = [vp, i64, vp, ip, ip, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, i64, f, ci, i64, vp, i64, vp,
+                                  vp, i64, vp]
+    L.mx_attention_kv_workspace.restype = i64
+    L.mx_attention_kv_workspace.argtypes = [i64, i64, i64, i64, i64]
     _lib = L
     return L
 
@@ -617,4 +634,213 @@ def mx_gemm_mbs_grouped(a_codes, a_scales, a_mbs, b_codes, b_scales, b_mbs, row_
                                                             b_codes.data_ptr(), _ptr(b_scales), _ptr(b_mbs), G,
                                                             row_offsets.data_ptr(), M, N, K, code, out.data_ptr(), ldc,
                                                             _stream()), "mx_gemm_mbs_grouped")
+    return out
+
+
+# ---- the paged MXFP4 key/value cache --------------------------------------------------------------------
+_STYLES = {"half": 0, "pairs": 1}
+
+
+def _here(t, dtype, name, dims=None):
+    """A CUDA tensor of that type (and rank) on the current device: the launch goes to the current device's stream."""
+    torch = _torch_module or _torch()
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or (dims is not None and t.dim() != dims):
+        raise TypeError("%s must be a %s CUDA tensor%s" % (name, dtype, "" if dims is None else " of %d dimensions" % dims))
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, the current device is %d" % (name, t.device, torch.cuda.current_device()))
+    return t
+
+
+def _flat(t, dtype, shape, name):
+    _here(t, dtype, name)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise TypeError("%s must be contiguous of shape %s" % (name, tuple(shape)))
+    return t
+
+
+def _rows_of_heads(t, dtype, name, shape=None):
+    """[T, heads, D] with a token's heads next to each other -> elements from one token to the next."""
+    _here(t, dtype, name, 3)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise TypeError("%s must have the shape %s" % (name, tuple(shape)))
+    T, H, D = t.shape
+    ld, between, inner = t.stride()
+    if T and H and ((inner != 1 and D > 1) or (between != D and H > 1)):
+        raise ValueError("the heads of a token of %s must lie next to each other" % name)
+    return ld if T > 1 else max(ld, H * D)
+
+
+def _cache_arrays(k_cache, v_cache):
+    """((codes, scales, mbs or None), the same for V) -> pointers in the order of the C calls, pages, heads, page size, D."""
+    torch = _torch_module or _torch()
+    (kc, ks, km), (vc, vs, vm) = k_cache, v_cache
+    _here(kc, torch.uint8, "k codes", 5)
+    pages, heads, blocks, page, _ = kc.shape
+    D = 32 * blocks
+    _flat(kc, torch.uint8, (pages, heads, blocks, page, 16), "k codes")
+    _flat(vc, torch.uint8, (pages, heads, page // 4, D // 8, 4, 4), "v codes")
+    _flat(ks, torch.uint8, (pages, heads, blocks, page), "k scales")
+    _flat(vs, torch.uint8, (pages, heads, blocks, page), "v scales")
+    if (km is None) != (vm is None):
+        raise ValueError("MBS words for both keys and values, or for neither")
+    if km is not None:
+        _flat(km, torch.uint8, (pages, heads, (D + 127) // 128, page), "k mbs")
+        _flat(vm, torch.uint8, (pages, heads, (D + 127) // 128, page), "v mbs")
+    return (_ptr(kc), _ptr(ks), _ptr(km), _ptr(vc), _ptr(vs), _ptr(vm)), pages, heads, page, D
+
+
+def mx_kv_cache(num_pages, heads, head_dim, page_size=64, use_mbs=True, device="cuda"):
+    """The zeroed arrays of a cache: (k_cache, v_cache), each (codes, scales, mbs or None), in the layout of include/mx4.h."""
+    torch = _torch_module or _torch()
+
+    def array(*shape):
+        return torch.zeros(shape, dtype=torch.uint8, device=device)
+
+    words, blocks = (head_dim + 127) // 128, head_dim // 32
+    return tuple((array(*codes), array(num_pages, heads, blocks, page_size), array(num_pages, heads, words, page_size) if use_mbs else None)
+                 for codes in ((num_pages, heads, blocks, page_size, 16), (num_pages, heads, page_size // 4, head_dim // 8, 4, 4)))
+
+
+def mx_kv_plan(ctx_lens, new_lens, page_size, block_table, free_pages, free_start, total_tokens, row_offsets=None, kv_lens=None, slots=None,
+               positions=None, free_next=None):
+    """Pages, slots, positions and offsets of a step whose requests have ctx_lens tokens and bring new_lens; block_table is extended in place.
+    Returns (row_offsets, kv_lens, slots, positions, free_next)."""
+    torch = _torch_module or _torch()
+    i32, i64 = torch.int32, torch.int64
+    S = _here(ctx_lens, i32, "ctx_lens", 1).shape[0]
+    _flat(ctx_lens, i32, (S,), "ctx_lens")
+    _flat(new_lens, i32, (S,), "new_lens")
+    _here(block_table, i32, "block_table", 2)
+    _flat(block_table, i32, (S, block_table.shape[1]), "block_table")
+    _here(free_pages, i32, "free_pages", 1)
+    _flat(free_pages, i32, free_pages.shape, "free_pages")
+    _flat(free_start, i32, (1,), "free_start")
+
+    def output(t, dtype, n, name):
+        return torch.empty(n, dtype=dtype, device=ctx_lens.device) if t is None else _flat(t, dtype, (n,), name)
+
+    T = int(total_tokens)
+    row_offsets, kv_lens = output(row_offsets, i64, S + 1, "row_offsets"), output(kv_lens, i32, S, "kv_lens")
+    slots, positions = output(slots, i64, T, "slots"), output(positions, i32, T, "positions")
+    free_next = output(free_next, i32, 1, "free_next")
+    _check((_lib or load_library()).mx_kv_plan(_ptr(ctx_lens), _ptr(new_lens), S, int(page_size), _ptr(block_table), block_table.shape[1],
+                                               _ptr(free_pages), free_pages.shape[0], _ptr(free_start), T, _ptr(row_offsets), _ptr(kv_lens),
+                                               _ptr(slots), _ptr(positions), _ptr(free_next), _stream()), "mx_kv_plan")
+    return row_offsets, kv_lens, slots, positions, free_next
+
+
+def _turn_arguments(q, k, positions, cos_sin, q_weight, k_weight, style):
+    """What mx_qk_norm_rope and its form with the cache pass alike."""
+    torch = _torch_module or _torch()
+    bf16 = torch.bfloat16
+    ldq, ldk = _rows_of_heads(q, bf16, "q"), _rows_of_heads(k, bf16, "k")
+    T, Hq, D = q.shape
+    if k.shape[0] != T or k.shape[2] != D:
+        raise ValueError("q and k disagree on the tokens or on the head size")
+    table, R = 0, 0
+    if cos_sin is not None:
+        table, R = _here(cos_sin, torch.float32, "cos_sin", 2).shape
+        _flat(cos_sin, torch.float32, (table, R), "cos_sin")
+        _flat(positions, torch.int32, (T,), "positions")
+    for weight, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if weight is not None:
+            _flat(weight, bf16, (D,), name)
+    return T, Hq, k.shape[1], D, R, table, ldq, ldk, _STYLES[style] if isinstance(style, str) else int(style)
+
+
+def mx_qk_norm_rope(q, k, positions, cos_sin, q_weight=None, k_weight=None, eps=1e-6, style="half", q_out=None, k_out=None):
+    """RMS norm (where there is a weight) and rotation (where there is a table) of the heads of q [T, Hq, D] and k [T, Hkv, D], bf16.
+    cos_sin fp32 [positions, R]: R/2 cosines, then R/2 sines.  Outputs may be the inputs.  Returns (q_out, k_out)."""
+    torch = _torch_module or _torch()
+    T, Hq, Hkv, D, R, table, ldq, ldk, code = _turn_arguments(q, k, positions, cos_sin, q_weight, k_weight, style)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+    ldqo, ldko = _rows_of_heads(q_out, q.dtype, "q_out", q.shape), _rows_of_heads(k_out, k.dtype, "k_out", k.shape)
+    _check((_lib or load_library()).mx_qk_norm_rope(_ptr(q), ldq, _ptr(k), ldk, _ptr(positions), _ptr(cos_sin), table, _ptr(q_weight),
+                                                    _ptr(k_weight), eps, code, T, Hq, Hkv, D, R, _ptr(q_out), ldqo, _ptr(k_out), ldko, _stream()),
+           "mx_qk_norm_rope")
+    return q_out, k_out
+
+
+def mx_kv_write(k, v, slots, k_cache, v_cache, rule="oas"):
+    """Quantizes k, v [T, Hkv, D] (bf16) into the places `slots` (int64 [T], distinct) of the cache."""
+    torch = _torch_module or _torch()
+    pointers, pages, heads, page, D = _cache_arrays(k_cache, v_cache)
+    ldk = _rows_of_heads(k, torch.bfloat16, "k")
+    T = k.shape[0]
+    if tuple(k.shape) != (T, heads, D):
+        raise ValueError("k and the cache disagree on heads or head size")
+    ldv = _rows_of_heads(v, torch.bfloat16, "v", k.shape)
+    _flat(slots, torch.int64, (T,), "slots")
+    _check((_lib or load_library()).mx_kv_write(_ptr(k), ldk, _ptr(v), ldv, _ptr(slots), _rule(rule), *pointers, pages, page, T, heads, D, _stream()),
+           "mx_kv_write")
+
+
+def mx_qk_norm_rope_kv_write(q, k, v, positions, slots, cos_sin, k_cache, v_cache, q_weight=None, k_weight=None, eps=1e-6, style="half", rule="oas",
+                             q_out=None):
+    """mx_qk_norm_rope, then mx_kv_write of the rotated keys and the values, in one launch and with the same bits.  Returns q_out."""
+    torch = _torch_module or _torch()
+    pointers, pages, heads, page, head_dim = _cache_arrays(k_cache, v_cache)
+    T, Hq, Hkv, D, R, table, ldq, ldk, code = _turn_arguments(q, k, positions, cos_sin, q_weight, k_weight, style)
+    if (Hkv, D) != (heads, head_dim):
+        raise ValueError("k and the cache disagree on heads or head size")
+    ldv = _rows_of_heads(v, torch.bfloat16, "v", k.shape)
+    _flat(slots, torch.int64, (T,), "slots")
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    ldqo = _rows_of_heads(q_out, q.dtype, "q_out", q.shape)
+    _check((_lib or load_library()).mx_qk_norm_rope_kv_write(_ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(positions), _ptr(cos_sin), table,
+                                                             _ptr(q_weight), _ptr(k_weight), eps, code, _ptr(slots), _rule(rule), *pointers, pages,
+                                                             page, T, Hq, Hkv, D, R, _ptr(q_out), ldqo, _stream()), "mx_qk_norm_rope_kv_write")
+    return q_out
+
+
+def mx_kv_read(slots, k_cache, v_cache, out_dtype="bf16", k_out=None, v_out=None):
+    """Rows of the cache by slot, rounded as by mx_dequantize.  Returns (k_out, v_out) [T, Hkv, D]."""
+    torch = _torch_module or _torch()
+    pointers, pages, heads, page, D = _cache_arrays(k_cache, v_cache)
+    T = _here(slots, torch.int64, "slots", 1).shape[0]
+    _flat(slots, torch.int64, (T,), "slots")
+    code, dtype = _out_dtypes[out_dtype]
+    k_out = torch.empty((T, heads, D), dtype=dtype, device=slots.device) if k_out is None else k_out
+    v_out = torch.empty((T, heads, D), dtype=dtype, device=slots.device) if v_out is None else v_out
+    ldk, ldv = _rows_of_heads(k_out, dtype, "k_out", (T, heads, D)), _rows_of_heads(v_out, dtype, "v_out", (T, heads, D))
+    _check((_lib or load_library()).mx_kv_read(_ptr(slots), *pointers, pages, page, T, heads, D, code, _ptr(k_out), ldk, _ptr(v_out), ldv, _stream()),
+           "mx_kv_read")
+    return k_out, v_out
+
+
+def mx_attention_kv_workspace(num_seqs, total_tokens, q_heads, kv_heads, head_dim) -> int:
+    """Bytes of workspace that mx_attention_kv wants for these sizes, whatever the lengths."""
+    need = (_lib or load_library()).mx_attention_kv_workspace(num_seqs, total_tokens, q_heads, kv_heads, head_dim)
+    _check(min(need, 0), "mx_attention_kv_workspace")
+    return need
+
+
+def mx_attention_kv(q, row_offsets, kv_lens, block_table, k_cache, v_cache, scale=None, causal=True, window=0, out=None, lse=None, workspace=None):
+    """Attention of q [T, Hq, D] (bf16; request s has the rows row_offsets[s] .. row_offsets[s+1]-1) over the cache: request s has kv_lens[s]
+    keys in the pages block_table[s].  scale: 1 / sqrt(D) if None.  lse: fp32 [T, Hq], filled if given.  workspace: uint8, if the caller keeps
+    one (calls that can run at the same time need one each); else it comes from the allocator.  Returns out, bf16 [T, Hq, D]."""
+    torch = _torch_module or _torch()
+    pointers, pages, heads, page, D = _cache_arrays(k_cache, v_cache)
+    ldq = _rows_of_heads(q, torch.bfloat16, "q")
+    T, Hq, _ = q.shape
+    if q.shape[2] != D or Hq % heads:
+        raise ValueError("q and the cache disagree on the head size, or the key heads do not divide the query heads")
+    S = _here(kv_lens, torch.int32, "kv_lens", 1).shape[0]
+    _flat(kv_lens, torch.int32, (S,), "kv_lens")
+    _flat(row_offsets, torch.int64, (S + 1,), "row_offsets")
+    _here(block_table, torch.int32, "block_table", 2)
+    _flat(block_table, torch.int32, (S, block_table.shape[1]), "block_table")
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    ldo = _rows_of_heads(out, q.dtype, "out", q.shape)
+    if lse is not None:
+        _flat(lse, torch.float32, (T, Hq), "lse")
+    if workspace is None:
+        workspace = torch.empty(mx_attention_kv_workspace(S, T, Hq, heads, D), dtype=torch.uint8, device=q.device)
+    else:
+        _here(workspace, torch.uint8, "workspace", 1)
+    _check((_lib or load_library()).mx_attention_kv(_ptr(q), ldq, _ptr(row_offsets), _ptr(kv_lens), _ptr(block_table), block_table.shape[1], *pointers,
+                                                    pages, page, S, T, Hq, heads, D, D ** -0.5 if scale is None else scale, int(bool(causal)),
+                                                    int(window), _ptr(out), ldo, _ptr(lse), _ptr(workspace), workspace.numel(), _stream()),
+           "mx_attention_kv")
     return out

@@ -1,0 +1,100 @@
+// Attention over the paged MXFP4 cache: what its kernels share (private; the public ABI is include/mx4.h).
+//
+// Query row i of a request sees keys [lo, hi) (KvRequest); with s_j = scale q . k_j,
+//     m = max s_j,  l = sum exp(s_j - m),  o = sum exp(s_j - m) v_j / l,  lse = m + ln l,
+// in one pass over the keys: m is a running maximum, and l and the accumulated o are rescaled when it grows.  A row that sees
+// nothing is written as zeros, its lse as -inf.
+//
+// Both products go to the bf16 matrix instruction 16 x 16 x 32 in transposed form, S^T = K Q^T and O^T = V^T P^T.  Its result has
+// one query row per lane column (lane mod 16) and four keys (or four of D) per lane, so that
+//   - statistics of a row are numbers of a lane, and rescaling O^T needs no exchange;
+//   - the four lane groups hold P^T for 4 keys each of every 16, and the order in which a product runs over its sum is free: with
+//     V taken in the same order P goes from one product to the next without leaving its registers.
+// Codes are expanded by the hardware convert with the block scale applied, which is exact in bf16.  A lane's 16 bytes of K are one
+// block of one key (D = 128: lane group g has block g), so that one scale serves four instructions.  V comes as 8 neighbouring
+// codes of each of 4 tokens; pairs of converted tokens are interleaved by v_perm into the operands of 8 products, one for each of the
+// 8 columns, which then lie next to each other in a lane's results.  The MBS factors multiply a key's score and its weight (1 / F
+// by the hardware reciprocal, within an ulp), once per window of 128 of D.
+// Rounding: q, K, V are exact operands; scores, statistics and sums are fp32; P is rounded to bf16 (2^-9 relative to each weight,
+// independent from key to key), the sum l takes the weights before that rounding.
+//
+// Masked places.  Tiles that some row does not see whole take the masked form: scores are replaced, not added to; V and its scales
+// of keys that no row of the tile sees are replaced by zeros (a page's unused places hold anything, and 0 times NaN is NaN).  A NaN
+// block (E = 255) of a key that only some rows see is replaced likewise and put into exactly those rows' results.
+#pragma once
+
+#include "mx_kv.h"
+
+namespace mx {
+
+struct AttentionArgs {
+    const uint16_t* q;
+    const int64_t* row_offsets;
+    const int32_t *kv_lens, *block_table;
+    KvArrays cache;
+    uint16_t* out;
+    float* lse;      // or NULL
+    float* partial;  // workspace of split rows
+    int64_t ldq, ldo;
+    int32_t num_pages, max_pages, room;
+    int32_t S, T, Hq, group;  // group: query heads of a key head
+    int32_t window, causal;
+    int32_t target;           // pieces that the batch is cut into, about
+    int64_t slots;            // pieces that the workspace has room for
+    float scale2;             // scale * log2(e)
+};
+
+// kernels of mx_attention_rows.hip
+int launch_attention_rows(const AttentionArgs& a, hipStream_t stream);
+int64_t attention_rows_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr float kLowest = -3.0e38f;  // where a running maximum starts: finite, so that differences of two are never NaN
+
+// Codes of byte kByte of a dword times 2^(E - 127), as a pair of bf16.
+template <int kByte>
+__device__ __forceinline__ uint32_t expand(uint32_t codes, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, kByte));
+}
+__device__ __forceinline__ u32x4 expand8(uint32_t codes, float scale) {
+    return u32x4{expand<0>(codes, scale), expand<1>(codes, scale), expand<2>(codes, scale), expand<3>(codes, scale)};
+}
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// Largest (sum) over the four lanes with the same lane mod 16.
+__device__ __forceinline__ float column_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+__device__ __forceinline__ float scale_of(uint32_t E) { return __uint_as_float(E << 23); }
+__device__ __forceinline__ float sigma_of(uint32_t m8) { return __builtin_amdgcn_rcpf(__uint_as_float(0x3F800000u | (m8 << 15))); }
+
+// How a head of D elements is taken: 128 at a time, then 64, then 32.  Of 128, lane group g has block g of a key, and lane n of 16
+// has 8 neighbouring columns of V; of 64, half a block and 4 columns; of 32, 8 elements and 2 columns.
+template <int D>
+struct HeadShape {
+    static constexpr int full = D / 128, half = D % 128 / 64, quarter = D % 64 / 32;
+    static constexpr int parts = full + half + quarter;
+    static constexpr int steps = D / 32;    // products along D for 16 keys
+    static constexpr int columns = D / 16;  // products for 16 of D each
+    static constexpr int words = (D + 127) / 128;
+    // part p: its first element, and how many elements of a block a lane has (32, 16, 8)
+    static constexpr int start(int p) { return p < full ? 128 * p : p == full && half ? 128 * full : 128 * full + 64 * half; }
+    static constexpr int width(int p) { return p < full ? 128 : p == full && half ? 64 : 32; }
+};
+
+}  // namespace
+}  // namespace mx

@@ -1,0 +1,65 @@
+// Argument checks and dispatch of the attention over the paged MXFP4 cache.
+#include "mx_attention.h"
+
+namespace mx {
+namespace {
+
+bool good_shape(int64_t S, int64_t T, int64_t Hq, int64_t Hkv) {
+    return S >= 0 && T >= 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && S <= kKvMost && T <= kKvMost && Hq <= kKvMostHeads;
+}
+
+}  // namespace
+}  // namespace mx
+
+extern "C" int64_t mx_attention_kv_workspace(int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    using namespace mx;
+    if (!good_shape(num_seqs, T, Hq, Hkv)) return MX_EINVAL;
+    if (!kv_head_dim(D)) return MX_EUNSUPPORTED;
+    return num_seqs && T ? attention_rows_workspace(num_seqs, T, Hq, Hkv, D) : 0;
+}
+
+extern "C" int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,
+                               int64_t max_pages, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* k_mbs_or_null,
+                               const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs_or_null, int64_t num_pages,
+                               int64_t page_size, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, float scale, int causal,
+                               int64_t window, void* out_bf16, int64_t ldo, float* lse_or_null, void* workspace, int64_t workspace_bytes,
+                               void* stream) {
+    using namespace mx;
+    AttentionArgs a = {};
+    a.cache = {const_cast<uint8_t*>(k_codes), const_cast<uint8_t*>(k_scales), const_cast<uint8_t*>(k_mbs_or_null),
+               const_cast<uint8_t*>(v_codes), const_cast<uint8_t*>(v_scales), const_cast<uint8_t*>(v_mbs_or_null), {}};
+    if (!good_shape(num_seqs, T, Hq, Hkv) || max_pages < 0 || window < 0 || (window && !causal)) return MX_EINVAL;
+    if (int st = a.cache.check(num_pages, page_size, Hkv, D)) return st;
+    if (num_pages > INT32_MAX || max_pages > kKvMostKeys / page_size) return MX_EINVAL;
+    if (num_seqs == 0 || T == 0) return MX_OK;
+    if (ldq < Hq * D || ldo < Hq * D) return MX_EINVAL;
+    if (!q_bf16 || !row_offsets || !kv_lens || (max_pages && !block_table) || !out_bf16) return MX_ENULL;
+    if (!aligned(q_bf16, 16) || ldq % 8 || !aligned(out_bf16, 16) || ldo % 8 || !aligned(row_offsets, 8) || !aligned(kv_lens, 4) ||
+        !aligned(block_table, 4) || !aligned(lse_or_null, 4) || !aligned(workspace, 16))
+        return MX_EALIGN;
+    const int64_t need = attention_rows_workspace(num_seqs, T, Hq, Hkv, D);
+    if (workspace_bytes < need) return MX_EINVAL;
+    if (need && !workspace) return MX_ENULL;
+    if (int st = check_device()) return st;
+    a.q = static_cast<const uint16_t*>(q_bf16);
+    a.row_offsets = row_offsets;
+    a.kv_lens = kv_lens;
+    a.block_table = block_table;
+    a.cache.shape(page_size, Hkv, D);
+    a.out = static_cast<uint16_t*>(out_bf16);
+    a.lse = lse_or_null;
+    a.partial = static_cast<float*>(workspace);
+    a.ldq = ldq;
+    a.ldo = ldo;
+    a.num_pages = (int32_t)num_pages;
+    a.max_pages = (int32_t)max_pages;
+    a.room = num_pages ? (int32_t)(max_pages * page_size) : 0;
+    a.S = (int32_t)num_seqs;
+    a.T = (int32_t)T;
+    a.Hq = (int32_t)Hq;
+    a.group = (int32_t)(Hq / Hkv);
+    a.window = (int32_t)(window < kKvMostKeys ? window : kKvMostKeys);
+    a.causal = causal != 0;
+    a.scale2 = scale * 1.4426950408889634f;
+    return launch_attention_rows(a, static_cast<hipStream_t>(stream));
+}

@@ -32,6 +32,11 @@ __device__ __forceinline__ uint32_t dpp_row_ror8(uint32_t v) {
     return __builtin_amdgcn_update_dpp(0u, v, 0x128, 0xF, 0xF, true);
 }
 
+// lane i <-> 7 - i inside each half row: on values that are uniform over quads this exchanges neighbouring ones
+__device__ __forceinline__ uint32_t dpp_half_mirror(uint32_t v) {
+    return __builtin_amdgcn_update_dpp(0u, v, 0x141, 0xF, 0xF, true);
+}
+
 // fp32 -> bf16 bits, round to nearest even; NaN stays NaN.
 __device__ __forceinline__ uint32_t f32_to_bf16_bits(float f) {
     uint32_t u = __float_as_uint(f);

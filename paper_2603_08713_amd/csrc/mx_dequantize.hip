@@ -7,13 +7,8 @@
 // them through the LDS crossbar (ds_bpermute): a load instruction occupies the texture-address unit for its 64
 // lanes however few bytes each lane asks for, and fetching a byte of each kind per lane and run made that unit,
 // not the memory, the limit.
-// The hardware convert expands two codes at a time and applies the block scale (exact).  The division by F costs
-// one IEEE division per run of 8 (F is shared by them): with r = RN(1 / F), q = RN(t r) is corrected once by the
-// exact remainder, q' = RN(q + (t - q F) r), which is the correctly rounded quotient for every E2M1 magnitude
-// (mantissa 1 or 1.5) and every MBS word - checked with exact rationals on the host (tests/test_abi_cpu.py); a
-// power-of-two scale commutes with all of it.  That holds while every intermediate is a normal number: lanes whose
-// scale byte is outside [64, 230] (and NaN blocks) take the element-by-element route.
-#include "mx_common.h"
+// The arithmetic is in mx_dequantize_math.h.
+#include "mx_dequantize_math.h"
 
 namespace mx {
 namespace {
@@ -23,22 +18,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kRuns = 4, kLaneElems = 8 * kRuns, kChunk = kWave * kLaneElems;
-
-// fp32 pattern of an E2M1 magnitude index: {0, .5, 1, 1.5, 2, 3, 4, 6}.
-__device__ __forceinline__ float e2m1_value(uint32_t code) {
-    const uint32_t m = code & 7u;
-    uint32_t bits = m >= 2u ? (m + 252u) << 22 : (m ? 0x3F000000u : 0u);
-    return __uint_as_float(bits | ((code & 8u) << 28));
-}
-
-// One element through fp64, valid for every scale byte: the product is exact, the quotient is rounded at 53 bits
-// and once more to fp32 (to a subnormal where the result is one), which never differs from a single rounding here
-// (the exact quotient of a 2-bit by a 9-bit integer has no run of 28 equal bits after its leading 25).
-__device__ __forceinline__ float dequantize_element(uint32_t code, uint32_t E, float F, bool divide) {
-    double y = (double)e2m1_value(code) * __longlong_as_double((long long)(E + 896u) << 52);  // 2^(E-127)
-    if (divide) y = y / (double)F;
-    return E == 255u ? __uint_as_float(0x7FC00000u) : (float)y;
-}
 
 struct DequantArgs {
     const uint8_t *codes, *scales, *mbs;
@@ -74,32 +53,8 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(DequantArgs q) {
         for (int u = 0; u < kRuns; ++u) {
             const uint32_t col = col0 + u * 512;
             if (col >= q.K) continue;  // no cross-lane operations below
-            const float F = __uint_as_float(0x3F800000u | (m8[u] << 15));  // 1 + m8/256
             float v[8];
-            if (E[u] >= 64u && E[u] <= 230u) {
-#pragma clang fp contract(off)
-                typedef float v2f __attribute__((ext_vector_type(2)));
-                const float r = 1.0f / F;                         // IEEE division, once per run (m8 = 0: exactly 1)
-                const float scale = __uint_as_float(E[u] << 23);  // 2^(E-127)
-                auto quotient = [&](float t) __attribute__((always_inline)) {  // t / F, correctly rounded (see the header)
-                    const float q0 = t * r;
-                    const float rem = __builtin_fmaf(-q0, F, t);  // exact
-                    return __builtin_copysignf(__builtin_fmaf(rem, r, q0), t);  // (the sign of a zero)
-                };
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v2f t;  // codes 2 i and 2 i + 1 (byte i of the dword) times the scale: exact
-                    if (i == 0) t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(cw[u], scale, 0);
-                    if (i == 1) t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(cw[u], scale, 1);
-                    if (i == 2) t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(cw[u], scale, 2);
-                    if (i == 3) t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(cw[u], scale, 3);
-                    v[2 * i] = quotient(t.x);
-                    v[2 * i + 1] = quotient(t.y);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = dequantize_element((cw[u] >> (4 * j)) & 15u, E[u], F, q.mbs != nullptr);
-            }
+            dequantize8(cw[u], E[u], m8[u], q.mbs != nullptr, v);
             if constexpr (kBf16) {
                 uint32_t w[4];
 #pragma unroll

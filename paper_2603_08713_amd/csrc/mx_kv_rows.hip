@@ -1,0 +1,436 @@
+// Rows of queries, keys and values on their way from the projection to the attention: RMS norm and rotation of each head, and
+// the paged MXFP4 cache written (quantized as mx_quantize / mx_quantize_mbs quantize a row) and read (as mx_dequantize).
+//
+// A row is one head of one token.  A lane owns 8 consecutive elements (16 bytes), 8, 16 or 32 lanes a row, as many as let a
+// 128-element window fill a row of 16 lanes for the quantizer's DPP maxima; the rows of a wavefront are the same head of
+// neighbouring tokens.  So a token's angles are fetched once for all heads that the wavefront takes, and neighbouring tokens,
+// which mostly lie in neighbouring places of a page, fill the 16-byte units of the V codes and the runs of scale bytes together.
+//
+// Norm and rotation are one expression, y_i = r (x_i (w_i c) -+ x_j (w_j s)), j the partner in the rotation and r = 1 / sqrt(mean
+// x^2 + eps): the partner's raw bits come through the LDS crossbar (4 dwords for 8 elements).  It is evaluated in fp64 and
+// rounded to fp32 and then bf16: w c and w s are exact, the sum carries one rounding, so that the result does not depend on how
+// anyone orders the operations - a neighbouring bf16 value would change MBS words and codes of its whole window.
+// Bound: HBM, 2 bytes in and 2 (0.55 for a cached row) out per element.
+#include "mx_dequantize_math.h"
+#include "mx_internal.h"
+#include "mx_kv.h"
+#include "mx_quantize_math.h"
+
+namespace mx {
+namespace {
+
+constexpr int kThreads = 256;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct RowsArgs {
+    const uint16_t *q, *k, *v, *q_weight, *k_weight;
+    const int32_t* positions;
+    const float* cos_sin;
+    const int64_t* slots;
+    uint16_t *q_out, *k_out;
+    KvArrays cache;
+    int64_t ldq, ldk, ldv, ldq_out, ldk_out, max_position, places;
+    double eps;
+    int32_t T, Hq, R, rule, per_wave, q_chunks, kv_chunks;
+    uint32_t carry, token_groups, waves;
+};
+
+__device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+template <int kLanes>
+__device__ __forceinline__ double row_sum(double x) {
+#pragma unroll
+    for (int m = 1; m < kLanes; m <<= 1) x += __shfl_xor(x, m);
+    return x;
+}
+
+// kLanes: of a row.  kTurn: norm, rotation or both are asked for.  kPairs: neighbours are rotated, else halves.  kCache: keys and
+// values go to the cache.
+template <int kLanes, bool kTurn, bool kPairs, bool kCache, bool kMbs>
+__global__ __launch_bounds__(kThreads) void kv_rows_kernel(RowsArgs a) {
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t id = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / kWave) + (threadIdx.x >> 6));
+    if (id >= a.waves) return;
+    const uint32_t chunks = a.q_chunks + a.kv_chunks * (kCache ? 2 : 1);
+    const uint32_t group = id / chunks, chunk = id - group * chunks;
+    const int D = a.cache.at.D, j = lane % kLanes;
+    const uint32_t token = group * (kWave / kLanes) + lane / kLanes;
+    // which rows: queries, keys or values (wave-uniform)
+    const int role = chunk < (uint32_t)a.q_chunks ? 0 : chunk < (uint32_t)(a.q_chunks + a.kv_chunks) ? 1 : 2;
+    const int first = (role == 0 ? chunk : role == 1 ? chunk - a.q_chunks : chunk - a.q_chunks - a.kv_chunks) * a.per_wave;
+    const int heads = min(a.per_wave, (role == 0 ? a.Hq : a.cache.at.heads) - first);
+    const uint16_t* x = role == 0 ? a.q : role == 1 ? a.k : a.v;
+    const int64_t ldx = role == 0 ? a.ldq : role == 1 ? a.ldk : a.ldv;
+    uint16_t* out = role == 0 ? a.q_out : role == 1 ? a.k_out : nullptr;
+    const int64_t ldo = role == 0 ? a.ldq_out : a.ldk_out;
+
+    bool live = token < (uint32_t)a.T && j * 8 < D;
+    int32_t position = 0;
+    if (kTurn && a.cos_sin && live) {
+        position = a.positions[token];
+        live = position >= 0;  // a padding token: its rows stay as they are
+    }
+    int64_t place = -1;
+    if (kCache && role != 0 && live) place = a.slots[token];
+    const bool cached = kCache && role != 0 && place >= 0 && place < a.places;
+    const int32_t shift = a.cache.at.page_shift;
+    const int64_t page = place >> shift;
+    const int32_t in_page = (int32_t)(place & ((1 << shift) - 1));
+
+    const uint16_t* row = x + (int64_t)token * ldx + (int64_t)first * D + j * 8;
+    u32x4 next = {0, 0, 0, 0};
+    if (live) next = *reinterpret_cast<const u32x4*>(row);
+
+    // coefficients of the lane's elements and of their partners
+    double own[8], other[8];
+    int partner = lane;
+    bool normed = false;
+    if constexpr (kTurn) {
+        const uint16_t* weight = role == 0 ? a.q_weight : a.k_weight;
+        normed = weight != nullptr && role != 2;
+        const int half = a.R >> 1, e = j * 8;
+        const bool turned = a.cos_sin && e < a.R && live;
+        const bool upper = !kPairs && e >= half;
+        if (turned && !kPairs) partner = upper ? lane - half / 8 : lane + half / 8;
+        const int pe = e + (partner - (int)lane) * 8;
+        const bool known = position < a.max_position;
+        const float* angle = a.cos_sin + (int64_t)(known && turned ? position : 0) * a.R + (kPairs ? e >> 1 : upper ? e - half : e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            double c = 1.0, s = 0.0;
+            if (turned) {
+                if (known) {
+                    c = angle[kPairs ? i >> 1 : i];
+                    s = angle[half + (kPairs ? i >> 1 : i)];
+                } else {
+                    c = __builtin_nan("");
+                }
+                if (kPairs ? (i & 1) == 0 : !upper) s = -s;
+            }
+            double w = 1.0, wp = 1.0;
+            if (normed && live) {
+                w = bf16_low(weight[e + i]);
+                wp = bf16_low(weight[kPairs ? e + (i ^ 1) : pe + i]);
+            }
+            own[i] = c * w;
+            other[i] = s * wp;
+        }
+    }
+
+    for (int h = 0; h < heads; ++h) {
+        u32x4 raw = next;
+        if (h + 1 < heads && live) next = *reinterpret_cast<const u32x4*>(row + (int64_t)(h + 1) * D);
+        if constexpr (kTurn) {
+            if (role != 2) {
+                double r = 1.0;
+                if (normed) {
+                    double sum = 0.0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const double lo = bf16_low(raw[i]), hi = bf16_high(raw[i]);
+                        sum = __builtin_fma(lo, lo, sum);
+                        sum = __builtin_fma(hi, hi, sum);
+                    }
+                    r = 1.0 / __builtin_sqrt(row_sum<kLanes>(sum) / D + a.eps);
+                }
+                u32x4 mate = raw;
+                if (!kPairs && a.cos_sin) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mate[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(partner * 4, (int)raw[i]);
+                }
+                u32x4 turned;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const double lo = bf16_low(raw[i]), hi = bf16_high(raw[i]);
+                    double y0 = lo * own[2 * i], y1 = hi * own[2 * i + 1];
+                    // (no partner: 0 times an infinity would not be 0)
+                    if (kPairs || partner != (int)lane) {
+                        const double mlo = bf16_low(mate[i]), mhi = bf16_high(mate[i]);
+                        if (!kPairs || (a.cos_sin && j * 8 < a.R)) {
+                            y0 = __builtin_fma(kPairs ? mhi : mlo, other[2 * i], y0);
+                            y1 = __builtin_fma(kPairs ? mlo : mhi, other[2 * i + 1], y1);
+                        }
+                    }
+                    turned[i] = pack_bf16((float)(y0 * r), (float)(y1 * r));
+                }
+                raw = turned;
+            }
+        }
+        if (out && live) *reinterpret_cast<u32x4*>(out + (int64_t)token * ldo + (int64_t)(first + h) * D + j * 8) = raw;
+        if constexpr (kCache) {
+            if (role != 0) {
+                if (!live) raw = u32x4{0, 0, 0, 0};  // (inactive lanes of a window)
+                const ChunkResult res = quantize_chunk<true, kMbs, kLanes == 8 ? 8 : 16>(raw, a.rule, a.carry);
+                if (cached) {
+                    const int head = first + h;
+                    const KvLayout& at = a.cache.at;
+                    if (role == 1) {
+                        *reinterpret_cast<uint32_t*>(a.cache.k_codes + at.k_block(page, head, j >> 2, in_page) + (j & 3) * 4) = res.codes;
+                    } else {
+                        *reinterpret_cast<uint32_t*>(a.cache.v_codes + at.v_unit(page, head, j, in_page)) = res.codes;
+                    }
+                    if ((j & 3) == 0) (role == 1 ? a.cache.k_scales : a.cache.v_scales)[at.scale(page, head, j >> 2, in_page)] = (uint8_t)res.E;
+                    if (kMbs && (j & 15) == 0) (role == 1 ? a.cache.k_mbs : a.cache.v_mbs)[at.word(page, head, j >> 4, in_page)] = (uint8_t)res.m8;
+                }
+            }
+        }
+    }
+}
+
+// Rows taken out of the cache: a lane 8 codes of a key or a value.
+struct ReadArgs {
+    const int64_t* slots;
+    KvArrays cache;
+    void *k_out, *v_out;
+    int64_t ldk, ldv, places;
+    int32_t T, per_wave;
+    uint32_t waves, chunks;
+};
+
+template <int kLanes, bool kBf16>
+__global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t id = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / kWave) + (threadIdx.x >> 6));
+    if (id >= a.waves) return;
+    const uint32_t group = id / (2 * a.chunks), chunk = id - group * 2 * a.chunks;
+    const bool key = chunk < a.chunks;
+    const KvLayout& at = a.cache.at;
+    const int first = (key ? chunk : chunk - a.chunks) * a.per_wave, heads = min(a.per_wave, at.heads - first);
+    const int j = lane % kLanes;
+    const uint32_t token = group * (kWave / kLanes) + lane / kLanes;
+    if (token >= (uint32_t)a.T || j * 8 >= at.D) return;  // (no cross-lane operations below)
+    const int64_t place = a.slots[token];
+    if (place < 0 || place >= a.places) return;
+    const int64_t page = place >> at.page_shift;
+    const int32_t in_page = (int32_t)(place & (at.page_size() - 1));
+    const uint8_t* words = key ? a.cache.k_mbs : a.cache.v_mbs;
+    void* out = key ? a.k_out : a.v_out;
+    if (!out) return;
+    const int64_t ldo = key ? a.ldk : a.ldv;
+    for (int h = first; h < first + heads; ++h) {
+        const uint32_t codes = *reinterpret_cast<const uint32_t*>(key ? a.cache.k_codes + at.k_block(page, h, j >> 2, in_page) + (j & 3) * 4
+                                                                      : a.cache.v_codes + at.v_unit(page, h, j, in_page));
+        const uint32_t E = (key ? a.cache.k_scales : a.cache.v_scales)[at.scale(page, h, j >> 2, in_page)];
+        const uint32_t m8 = words ? words[at.word(page, h, j >> 4, in_page)] : 0u;
+        float v[8];
+        dequantize8(codes, E, m8, words != nullptr, v);
+        const int64_t o = (int64_t)token * ldo + (int64_t)h * at.D + j * 8;
+        if constexpr (kBf16) {
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + o) =
+                u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        } else {
+            f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(out) + o);
+            p[0] = f32x4{v[0], v[1], v[2], v[3]};
+            p[1] = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    }
+}
+
+inline int lanes_of(int D) { return D <= 64 ? 8 : D <= 128 ? 16 : 32; }
+
+// Heads that a wavefront takes one after the other: one where the launch is small (its latency is what counts), four where it
+// fills the device several times.
+inline int heads_per_wave(int64_t rows_of_waves) { return rows_of_waves > 16384 ? 4 : 1; }
+
+template <int kLanes, bool kTurn, bool kPairs>
+void launch_rows(const RowsArgs& a, bool cache, bool mbs, dim3 grid, hipStream_t s) {
+    if (!cache) hipLaunchKernelGGL((kv_rows_kernel<kLanes, kTurn, kPairs, false, false>), grid, dim3(kThreads), 0, s, a);
+    else if (mbs) hipLaunchKernelGGL((kv_rows_kernel<kLanes, kTurn, kPairs, true, true>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((kv_rows_kernel<kLanes, kTurn, kPairs, true, false>), grid, dim3(kThreads), 0, s, a);
+}
+template <int kLanes>
+void launch_rows(const RowsArgs& a, bool turn, bool pairs, bool cache, bool mbs, dim3 grid, hipStream_t s) {
+    if (!turn) launch_rows<kLanes, false, false>(a, cache, mbs, grid, s);
+    else if (pairs) launch_rows<kLanes, true, true>(a, cache, mbs, grid, s);
+    else launch_rows<kLanes, true, false>(a, cache, mbs, grid, s);
+}
+
+// Everything but what tells the calls apart has been checked.
+int run_rows(RowsArgs a, bool turn, bool pairs, bool cache, hipStream_t stream) {
+    const int lanes = lanes_of(a.cache.at.D), tokens = kWave / lanes;
+    a.token_groups = (uint32_t)((a.T + (int64_t)tokens - 1) / tokens);
+    a.carry = rule_carry(a.rule);
+    a.per_wave = heads_per_wave((int64_t)a.token_groups * (a.Hq + 2 * (int64_t)a.cache.at.heads));
+    a.q_chunks = (a.Hq + a.per_wave - 1) / a.per_wave;
+    a.kv_chunks = (a.cache.at.heads + a.per_wave - 1) / a.per_wave;
+    const int64_t waves = (int64_t)a.token_groups * (a.q_chunks + (int64_t)a.kv_chunks * (cache ? 2 : 1));
+    if (waves >= (int64_t)1 << 26) return MX_EINVAL;  // a launch of fewer than 2^32 work-items
+    a.waves = (uint32_t)waves;
+    if (waves == 0) return MX_OK;
+    const dim3 grid((unsigned)((waves + kThreads / kWave - 1) / (kThreads / kWave)));
+    const bool mbs = a.cache.k_mbs != nullptr;
+    if (lanes == 8) launch_rows<8>(a, turn, pairs, cache, mbs, grid, stream);
+    else if (lanes == 16) launch_rows<16>(a, turn, pairs, cache, mbs, grid, stream);
+    else launch_rows<32>(a, turn, pairs, cache, mbs, grid, stream);
+    return launch_status();
+}
+
+bool good_rows(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0; }
+
+// What mx_qk_norm_rope and its form with the cache check alike.
+int check_turn(const RowsArgs& a, mx_rope_t style, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t R) {
+    if (T < 0 || Hq < 0 || Hkv < 0 || T > kKvMost || Hq > kKvMostHeads || Hkv > kKvMostHeads || a.max_position < 0 || R < 0 || R > D) return MX_EINVAL;
+    if (style != MX_ROPE_HALF && style != MX_ROPE_PAIRS) return MX_EINVAL;
+    if (!(a.eps >= 0.0)) return MX_EINVAL;
+    if (!kv_head_dim(D) || R % 16 != 0) return MX_EUNSUPPORTED;
+    if (T == 0) return MX_OK;
+    if (Hq && (a.ldq < Hq * D || a.ldq_out < Hq * D)) return MX_EINVAL;
+    if (Hkv && a.ldk < Hkv * D) return MX_EINVAL;
+    if ((Hq && (!a.q || !a.q_out)) || (Hkv && !a.k)) return MX_ENULL;
+    if ((a.cos_sin != nullptr) != (R != 0)) return MX_EINVAL;
+    if (a.cos_sin && !a.positions) return MX_ENULL;
+    if ((Hq && (!good_rows(a.q, a.ldq) || !good_rows(a.q_out, a.ldq_out))) || (Hkv && !good_rows(a.k, a.ldk))) return MX_EALIGN;
+    if (!aligned(a.cos_sin, 4) || !aligned(a.q_weight, 2) || !aligned(a.k_weight, 2) || !aligned(a.positions, 4)) return MX_EALIGN;
+    return MX_OK;
+}
+
+}  // namespace
+
+int KvArrays::check(int64_t num_pages, int64_t page_size, int64_t Hkv, int64_t D) const {
+    if (num_pages < 0 || Hkv <= 0 || Hkv > kKvMostHeads || page_size <= 0) return MX_EINVAL;
+    if (!kv_head_dim(D) || page_size < 16 || page_size > 4096 || (page_size & (page_size - 1)) != 0) return MX_EUNSUPPORTED;
+    if (num_pages > ((int64_t)1 << 40) / (Hkv * page_size)) return MX_EINVAL;
+    if (!!k_mbs != !!v_mbs) return MX_EINVAL;
+    if (num_pages == 0) return MX_OK;
+    if (!k_codes || !k_scales || !v_codes || !v_scales) return MX_ENULL;
+    if (!aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scales, 4) || !aligned(v_scales, 4)) return MX_EALIGN;
+    return MX_OK;
+}
+
+void KvArrays::shape(int64_t page_size, int64_t Hkv, int64_t D) {
+    at.page_shift = 0;
+    while (((int64_t)1 << at.page_shift) < page_size) ++at.page_shift;
+    at.heads = (int32_t)Hkv;
+    at.D = (int32_t)D;
+}
+
+}  // namespace mx
+
+extern "C" int mx_qk_norm_rope(const void* q_bf16, int64_t ldq, const void* k_bf16, int64_t ldk, const int32_t* positions,
+                               const float* cos_sin_or_null, int64_t max_position, const void* q_weight_or_null, const void* k_weight_or_null,
+                               double eps, mx_rope_t style, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t R,
+                               void* q_out, int64_t ldq_out, void* k_out, int64_t ldk_out, void* stream) {
+    using namespace mx;
+    RowsArgs a = {};
+    a.q = static_cast<const uint16_t*>(q_bf16);
+    a.k = static_cast<const uint16_t*>(k_bf16);
+    a.q_weight = static_cast<const uint16_t*>(q_weight_or_null);
+    a.k_weight = static_cast<const uint16_t*>(k_weight_or_null);
+    a.positions = positions;
+    a.cos_sin = cos_sin_or_null;
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.k_out = static_cast<uint16_t*>(k_out);
+    a.ldq = ldq; a.ldk = ldk; a.ldq_out = ldq_out; a.ldk_out = ldk_out;
+    a.max_position = max_position;
+    a.eps = eps;
+    if (int st = check_turn(a, style, T, Hq, Hkv, D, R)) return st;
+    if (T == 0 || Hq + Hkv == 0) return MX_OK;
+    if (Hkv && ldk_out < Hkv * D) return MX_EINVAL;
+    if (Hkv && !k_out) return MX_ENULL;
+    if (Hkv && !good_rows(k_out, ldk_out)) return MX_EALIGN;
+    if (int st = check_device()) return st;
+    a.T = (int32_t)T; a.Hq = (int32_t)Hq; a.R = (int32_t)R;
+    a.cache.shape(16, Hkv, D);
+    return run_rows(a, true, style == MX_ROPE_PAIRS, false, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int mx_kv_write(const void* k_bf16, int64_t ldk, const void* v_bf16, int64_t ldv, const int64_t* slots, mx_rule_t rule,
+                           uint8_t* k_codes, uint8_t* k_scales, uint8_t* k_mbs_or_null, uint8_t* v_codes, uint8_t* v_scales, uint8_t* v_mbs_or_null,
+                           int64_t num_pages, int64_t page_size, int64_t T, int64_t Hkv, int64_t D, void* stream) {
+    using namespace mx;
+    RowsArgs a = {};
+    a.cache = {k_codes, k_scales, k_mbs_or_null, v_codes, v_scales, v_mbs_or_null, {}};
+    if (int st = a.cache.check(num_pages, page_size, Hkv, D)) return st;
+    if (T < 0 || T > kKvMost || rule < MX_RULE_OCP || rule > MX_RULE_OAS) return MX_EINVAL;
+    if (T == 0) return MX_OK;
+    if (ldk < Hkv * D || ldv < Hkv * D) return MX_EINVAL;
+    if (!k_bf16 || !v_bf16 || !slots) return MX_ENULL;
+    if (!good_rows(k_bf16, ldk) || !good_rows(v_bf16, ldv) || !aligned(slots, 8)) return MX_EALIGN;
+    if (num_pages == 0) return MX_OK;  // no slot exists
+    if (int st = check_device()) return st;
+    a.k = static_cast<const uint16_t*>(k_bf16);
+    a.v = static_cast<const uint16_t*>(v_bf16);
+    a.ldk = ldk; a.ldv = ldv;
+    a.slots = slots;
+    a.rule = rule;
+    a.T = (int32_t)T;
+    a.cache.shape(page_size, Hkv, D);
+    a.places = num_pages * page_size;
+    return run_rows(a, false, false, true, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int mx_qk_norm_rope_kv_write(const void* q_bf16, int64_t ldq, const void* k_bf16, int64_t ldk, const void* v_bf16, int64_t ldv,
+                                        const int32_t* positions, const float* cos_sin_or_null, int64_t max_position,
+                                        const void* q_weight_or_null, const void* k_weight_or_null, double eps, mx_rope_t style,
+                                        const int64_t* slots, mx_rule_t rule, uint8_t* k_codes, uint8_t* k_scales, uint8_t* k_mbs_or_null,
+                                        uint8_t* v_codes, uint8_t* v_scales, uint8_t* v_mbs_or_null, int64_t num_pages, int64_t page_size,
+                                        int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t R, void* q_out, int64_t ldq_out, void* stream) {
+    using namespace mx;
+    RowsArgs a = {};
+    a.q = static_cast<const uint16_t*>(q_bf16);
+    a.k = static_cast<const uint16_t*>(k_bf16);
+    a.v = static_cast<const uint16_t*>(v_bf16);
+    a.q_weight = static_cast<const uint16_t*>(q_weight_or_null);
+    a.k_weight = static_cast<const uint16_t*>(k_weight_or_null);
+    a.positions = positions;
+    a.cos_sin = cos_sin_or_null;
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldq_out = ldq_out;
+    a.max_position = max_position;
+    a.eps = eps;
+    a.cache = {k_codes, k_scales, k_mbs_or_null, v_codes, v_scales, v_mbs_or_null, {}};
+    if (int st = a.cache.check(num_pages, page_size, Hkv, D)) return st;
+    if (rule < MX_RULE_OCP || rule > MX_RULE_OAS) return MX_EINVAL;
+    if (int st = check_turn(a, style, T, Hq, Hkv, D, R)) return st;
+    if (T == 0) return MX_OK;
+    if (ldv < Hkv * D) return MX_EINVAL;
+    if (!v_bf16 || !slots) return MX_ENULL;
+    if (!good_rows(v_bf16, ldv) || !aligned(slots, 8)) return MX_EALIGN;
+    if (int st = check_device()) return st;
+    a.slots = slots;
+    a.rule = rule;
+    a.T = (int32_t)T; a.Hq = (int32_t)Hq; a.R = (int32_t)R;
+    a.cache.shape(page_size, Hkv, D);
+    a.places = num_pages * page_size;
+    return run_rows(a, true, style == MX_ROPE_PAIRS, true, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* k_mbs_or_null,
+                          const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs_or_null, int64_t num_pages, int64_t page_size,
+                          int64_t T, int64_t Hkv, int64_t D, mx_dtype_t out_dtype, void* k_out, int64_t ldk, void* v_out, int64_t ldv,
+                          void* stream) {
+    using namespace mx;
+    ReadArgs a = {};
+    a.cache = {const_cast<uint8_t*>(k_codes), const_cast<uint8_t*>(k_scales), const_cast<uint8_t*>(k_mbs_or_null),
+               const_cast<uint8_t*>(v_codes), const_cast<uint8_t*>(v_scales), const_cast<uint8_t*>(v_mbs_or_null), {}};
+    if (int st = a.cache.check(num_pages, page_size, Hkv, D)) return st;
+    if (T < 0 || T > kKvMost || (out_dtype != MX_OUT_F32 && out_dtype != MX_OUT_BF16)) return MX_EINVAL;
+    if (T == 0) return MX_OK;
+    if ((k_out && ldk < Hkv * D) || (v_out && ldv < Hkv * D)) return MX_EINVAL;
+    if (!slots || (!k_out && !v_out)) return MX_ENULL;
+    const int64_t per16 = out_dtype == MX_OUT_F32 ? 4 : 8;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16) || (k_out && ldk % per16) || (v_out && ldv % per16) || !aligned(slots, 8)) return MX_EALIGN;
+    if (num_pages == 0) return MX_OK;
+    if (int st = check_device()) return st;
+    a.slots = slots;
+    a.k_out = k_out; a.v_out = v_out;
+    a.ldk = ldk; a.ldv = ldv;
+    a.T = (int32_t)T;
+    a.cache.shape(page_size, Hkv, D);
+    a.places = num_pages * page_size;
+    const int lanes = lanes_of((int)D), tokens = kWave / lanes;
+    const int64_t groups = (T + tokens - 1) / tokens;
+    a.per_wave = heads_per_wave(groups * 2 * Hkv);
+    a.chunks = (uint32_t)((Hkv + a.per_wave - 1) / a.per_wave);
+    const int64_t waves = groups * 2 * a.chunks;
+    if (waves >= (int64_t)1 << 26) return MX_EINVAL;
+    a.waves = (uint32_t)waves;
+    const dim3 grid((unsigned)((waves + kThreads / kWave - 1) / (kThreads / kWave)));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool bf16 = out_dtype == MX_OUT_BF16;
+    if (lanes == 8) { if (bf16) hipLaunchKernelGGL((kv_read_kernel<8, true>), grid, dim3(kThreads), 0, s, a); else hipLaunchKernelGGL((kv_read_kernel<8, false>), grid, dim3(kThreads), 0, s, a); }
+    else if (lanes == 16) { if (bf16) hipLaunchKernelGGL((kv_read_kernel<16, true>), grid, dim3(kThreads), 0, s, a); else hipLaunchKernelGGL((kv_read_kernel<16, false>), grid, dim3(kThreads), 0, s, a); }
+    else { if (bf16) hipLaunchKernelGGL((kv_read_kernel<32, true>), grid, dim3(kThreads), 0, s, a); else hipLaunchKernelGGL((kv_read_kernel<32, false>), grid, dim3(kThreads), 0, s, a); }
+    return launch_status();
+}

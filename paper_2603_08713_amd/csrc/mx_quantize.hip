@@ -56,117 +56,6 @@ struct QuantArgs {
     uint32_t split, total_chunks2;
 };
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-// Round |t| (t already multiplied by the block scale) to the E2M1 grid, nearest-even, saturating.
-// Adding 1.5 * 2^(22 + e), e = max(exponent(t), 0), leaves t in units of the grid step of its
-// binade in the low mantissa bits of the sum.
-__device__ __forceinline__ uint32_t e2m1_code_alu(float t) {
-    const uint32_t tb = __float_as_uint(t);
-    const float y = fminf(__uint_as_float(tb & 0x7FFFFFFFu), 6.0f);
-    const uint32_t ey = max(__float_as_uint(y) >> 23, 127u);
-    const float w = y + __uint_as_float(((ey + 22u) << 23) | 0x400000u);
-    const uint32_t mag = (__float_as_uint(w) & 0xFu) + 2u * (ey - 127u);
-    return mag | ((tb >> 28) & 8u);
-}
-
-struct ChunkResult {
-    uint32_t codes;  // 8 E2M1 codes of this lane
-    uint32_t E;      // E8M0 byte of this lane's block
-    uint32_t m8;     // MBS word of this lane's macro block
-};
-
-// All-integer path, exact for every bf16 input including subnormals, huge values and Inf/NaN.
-// m8_given >= 0 replaces the static word (the searched word of MBS-Dynamic).
-__device__ __noinline__ ChunkResult quantize_chunk_exact(u32x4 v, int rule, int use_mbs, int m8_given = -1) {
-    uint32_t h[8] = {v.x & 0xFFFFu, v.x >> 16, v.y & 0xFFFFu, v.y >> 16,
-                     v.z & 0xFFFFu, v.z >> 16, v.w & 0xFFFFu, v.w >> 16};
-    uint32_t amax = 0, nf = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t a = h[i] & 0x7FFFu;
-        if (a >= 0x7F80u) nf = 1; else amax = max(amax, a);
-    }
-    nf |= dpp_quad_xor1(nf);
-    nf |= dpp_quad_xor2(nf);
-    amax = max(amax, dpp_quad_xor1(amax));
-    amax = max(amax, dpp_quad_xor2(amax));
-    uint32_t mmax = amax;
-    mmax = max(mmax, dpp_row_ror4(mmax));
-    mmax = max(mmax, dpp_row_ror8(mmax));
-
-    uint32_t m8 = use_mbs ? mbs_word_of_absmax(mmax) : 0u;
-    if (m8_given >= 0) m8 = (uint32_t)m8_given;
-    const uint32_t u = 256u + m8;  // F = u / 256
-
-    const int E = nf ? 255 : amax == 0 ? 127 : exact_scale_byte(amax, u, rule);
-    const int s = 127 - E;
-    uint32_t codes = 0;
-    if (!nf) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) codes |= exact_code(h[i], u, s) << (4 * i);
-    }
-    return {codes, (uint32_t)E, m8};
-}
-
-template <bool kHwCvt, bool kMbs>
-__device__ __forceinline__ ChunkResult quantize_chunk(u32x4 v, const QuantArgs& q) {
-    // lane, block and macro-block absmax on the magnitude bits
-    uint32_t m = pk_max_u16(pk_max_u16(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu),
-                            pk_max_u16(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-    uint32_t amax = max(m & 0xFFFFu, m >> 16);
-    amax = max(amax, dpp_quad_xor1(amax));
-    amax = max(amax, dpp_quad_xor2(amax));
-
-    // exponent field outside [24, 249] (or Inf/NaN): leave fp32 arithmetic, wave-uniformly
-    const bool odd = (amax >= (250u << 7)) || (amax != 0 && amax < (24u << 7));
-    if (__builtin_amdgcn_ballot_w64(odd) != 0) return quantize_chunk_exact(v, q.rule, kMbs);
-
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t codes = 0;
-    if constexpr (!kMbs && kHwCvt) {
-        // no MBS: the block exponent comes straight off the bf16 absmax, and the hardware converts
-        // bf16 pairs with the block scale applied (x / 2^(E-127), nearest-even, saturating)
-        uint32_t E = (((amax << 16) + q.carry) >> 23) - 2u;
-        E = amax ? E : 127u;
-        const float scale = __uint_as_float(E << 23);
-        typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(v2bf, w[0]), scale, 0);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(v2bf, w[1]), scale, 1);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(v2bf, w[2]), scale, 2);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(v2bf, w[3]), scale, 3);
-        return {codes, E, 0u};
-    } else {
-        uint32_t m8 = 0;
-        if constexpr (kMbs) {
-            uint32_t mmax = max(amax, dpp_row_ror4(amax));
-            mmax = max(mmax, dpp_row_ror8(mmax));
-            m8 = mmax ? mbs_word_of_mantissa_fast(mmax & 0x7Fu) : 0u;
-        }
-        // absmax * F is exact in fp32; exponent field + carry gives the stored byte
-        const float scaled_max = __uint_as_float(amax << 16) * __uint_as_float(0x3F800000u | (m8 << 15));
-        uint32_t E = ((__float_as_uint(scaled_max) + q.carry) >> 23) - 2u;
-        E = amax ? E : 127u;
-        // multiplier F * 2^(127-E): exponent field 254-E under F's mantissa
-        const float mult = __uint_as_float(((254u - E) << 23) | (m8 << 15));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float t0 = __uint_as_float(w[i] << 16) * mult;
-            const float t1 = __uint_as_float(w[i] & 0xFFFF0000u) * mult;
-            if constexpr (kHwCvt) {
-                // hardware fp32 -> E2M1 pair convert (scale 1: the block scale is already applied)
-                if (i == 0) codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, t0, t1, 1.0f, 0);
-                if (i == 1) codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, t0, t1, 1.0f, 1);
-                if (i == 2) codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, t0, t1, 1.0f, 2);
-                if (i == 3) codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, t0, t1, 1.0f, 3);
-            } else {
-                codes |= (e2m1_code_alu(t0) | (e2m1_code_alu(t1) << 4)) << (8 * i);
-            }
-        }
-        return {codes, E, m8};
-    }
-}
-
 template <bool kHwCvt, bool kMbs>
 __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantArgs q) {
     const uint32_t lane = threadIdx.x & 63;
@@ -205,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantArgs q) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             if (c0 + u >= total) break;  // wave-uniform
-            const ChunkResult res = quantize_chunk<kHwCvt, kMbs>(v[u], q);
+            const ChunkResult res = quantize_chunk<kHwCvt, kMbs>(v[u], q.rule, q.carry);
             // scales of the macro block gathered into one dword across the row of 16 lanes
             uint32_t ew = res.E << (8 * ((lane >> 2) & 3));
             if ((lane & 3) != 0) ew = 0;

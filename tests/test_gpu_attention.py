@@ -1,0 +1,274 @@
+"""Attention over the paged MXFP4 cache against a plain 64-bit implementation (tests/kv_reference.py derives the tolerances)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+import kv_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2603_08713_amd as mx_
+
+    mx_.load_library()
+    return mx_
+
+
+class Batch:
+    """Requests of n[s] queries on keys[s] keys over a cache whose unused bytes hold anything."""
+
+    def __init__(self, mx, seed, n, keys, Hq, Hkv, D, page, mbs, spread=1.0, width=0, wide=0):
+        self.mx = mx
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        need = [-(-max(0, L) // page) for L in keys]
+        pages = sum(need) + 2
+        order = rng.permutation(pages).astype(np.int32)
+        table = rng.integers(-5, 2 * pages, (len(n), max([1, width] + need) + 1)).astype(np.int32)  # unused entries hold anything
+        at = 0
+        for s, c in enumerate(need):
+            table[s, :c] = order[at:at + c]
+            at += c
+        self.table = torch.from_numpy(table).cuda()
+        self.caches = tuple(tuple(None if a is None else torch.randint(0, 256, a.shape, generator=g, device="cuda", dtype=torch.uint8) for a in c)
+                            for c in mx.mx_kv_cache(pages, Hkv, D, page, mbs))
+        slots = np.concatenate([table[s, np.arange(L) // page].astype(np.int64) * page + np.arange(L) % page for s, L in enumerate(keys)] + [np.zeros(0, np.int64)])
+        self.slots = slots
+        rows = torch.randn((len(slots), 2 * Hkv, D), generator=g, device="cuda")
+        rows[:, :Hkv, D // 5] *= 8
+        rows = rows.to(torch.bfloat16)
+        if len(slots):
+            mx.mx_kv_write(rows[:, :Hkv], rows[:, Hkv:], torch.from_numpy(slots).cuda(), *self.caches)
+        self.offsets = torch.tensor([0] + list(np.cumsum(n)), dtype=torch.int64, device="cuda")
+        self.lens = torch.tensor(list(keys), dtype=torch.int32, device="cuda")
+        T = int(sum(n)) + wide  # rows behind the last request
+        self.q = (torch.randn((T, Hq + 1, D), generator=g, device="cuda") * spread).to(torch.bfloat16)[:, :Hq]  # strided
+        self.page = page
+
+    def run(self, **how):
+        T, Hq, D = self.q.shape
+        out = torch.full((T, Hq, D), 5.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((T, Hq), 6.0, device="cuda")
+        self.mx.mx_attention_kv(self.q, self.offsets, self.lens, self.table, *self.caches, out=out, lse=lse, **how)
+        return out, lse
+
+    def check(self, scale=None, causal=True, window=0):
+        out, lse = self.run(scale=scale, causal=causal, window=window)
+        scale = self.q.shape[2] ** -0.5 if scale is None else scale
+        want, want_lse, tol, tol_lse, written = ref.attention(self.q, self.offsets, self.lens, self.table, *self.caches, scale, causal, window)
+        assert bool((out[~written] == 5.0).all()) and bool((lse[~written] == 6.0).all()), "rows behind the last request"
+        got, got_lse = out.cpu().double().numpy()[written], lse.cpu().double().numpy()[written]
+        want, want_lse, tol, tol_lse = want[written], want_lse[written], tol[written], tol_lse[written]
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isnan(got_lse), np.isnan(want_lse)), "NaN"
+        assert np.array_equal(np.isneginf(got_lse), np.isneginf(want_lse)), "rows without keys"
+        assert (got[np.isneginf(want_lse)] == 0).all()
+        fine = ~np.isnan(want)
+        off = np.abs(got - want)[fine] - tol[fine]
+        assert not off.size or off.max() <= 0, "off by %g more than %g" % (off.max(), tol[fine][off.argmax()])
+        fine = np.isfinite(want_lse)
+        off = np.abs(got_lse[fine] - want_lse[fine]) - tol_lse[fine]
+        assert not off.size or off.max() <= 0, "lse off by %g more than %g" % (off.max(), tol_lse[fine][off.argmax()])
+        return out, lse
+
+
+# one token each: lengths around the sizes of pages, subtiles, tiles and pieces
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("mbs", [True, False])
+@pytest.mark.parametrize("Hq, Hkv, page", [(8, 2, 16), (3, 3, 64), (20, 1, 32), (24, 8, 128)])
+def test_single_tokens(mx, D, mbs, Hq, Hkv, page):
+    keys = [1, 2, 15, 16, 17, 63, 64, 65, 127, 129, 255, 256, 257, 300]
+    Batch(mx, D + Hq, [1] * len(keys), keys, Hq, Hkv, D, page, mbs).check()
+
+
+@pytest.mark.parametrize("D, page, mbs", [(128, 64, True), (64, 16, False), (96, 32, True), (256, 128, True)])
+@pytest.mark.parametrize("L", [1000, 4097, 9000])
+def test_long_contexts_are_cut(mx, D, page, mbs, L):
+    Batch(mx, L, [1, 1], [L, 3], 8, 2, D, page, mbs).check()
+    Batch(mx, L + 1, [3, 2], [L, L // 3], 4, 1, D, page, mbs).check()
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("mbs", [True, False])
+@pytest.mark.parametrize("window", [0, 1, 40, 64])
+def test_several_tokens_and_prompts(mx, D, mbs, window):
+    # whole prompts, chunks behind a context, a request without rows, one without keys, more queries than keys
+    Batch(mx, D + window, [70, 5, 0, 33, 9, 130], [70, 200, 50, 33, 4, 131], 6, 2, D, 16, mbs, wide=3).check(window=window)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_all_keys(mx, D):
+    Batch(mx, D, [40, 1, 7], [33, 190, 0], 4, 2, D, 32, True).check(causal=False)
+
+
+@pytest.mark.parametrize("n, keys", [([1], [0]), ([1, 1, 1], [0, 0, 0]), ([4], [1]), ([100], [20]), ([0, 0], [5, 6]), ([1, 0, 1], [64, 64, 0])])
+def test_rows_without_keys(mx, n, keys):
+    b = Batch(mx, 1, n, keys, 8, 2, 128, 16, True, wide=2)
+    b.check()
+    b.check(window=3)
+    b.check(causal=False)
+
+
+def test_large_scores_and_scales(mx):
+    """Scores far apart: one key takes all of a row, and the running maximum moves often."""
+    for spread, scale in ((30.0, None), (1.0, 5.0), (1e-3, None), (2.0, -0.3), (1.0, 0.0)):
+        Batch(mx, 3, [1, 20], [500, 300], 8, 2, 128, 64, True, spread=spread).check(scale=scale)
+
+
+def test_missing_pages(mx):
+    """Pages outside the cache hold no keys, and lengths beyond the table end with it."""
+    b = Batch(mx, 4, [1, 30, 2, 1], [200, 150, 90, 40], 4, 2, 128, 16, True)
+    pages = b.caches[0][1].shape[0]
+    b.table[0, 3], b.table[0, 7] = -1, pages
+    b.table[1, 0], b.table[1, 9] = 1 << 30, -(1 << 31)
+    b.table[3, :] = -7
+    b.check()
+    b.check(window=33)
+    b.lens[2] = 100000
+    b.table[2, :] = b.table[2, 0]
+    b.check()
+    b.lens[:] = torch.tensor([-5, 2147483647, 0, -2147483648], dtype=torch.int32)
+    b.run()  # (nothing to compare: positions of the second request are far beyond its keys)
+    torch.cuda.synchronize()
+
+
+def test_offsets_that_make_no_sense_stay_inside(mx):
+    """Row offsets that run backwards, overlap or leave the tensor: no access outside, whatever the results."""
+    b = Batch(mx, 5, [3, 4, 5, 6], [300, 20, 500, 70], 4, 2, 128, 16, True)
+    for offsets in ([0, 18, 0, 18, 0], [5, 3, 2, 1, 0], [-9, -1, 1000, 1 << 40, -(1 << 62)], [0, 18, 18, 18, 18], [17, 1 << 62, 0, 4, 5]):
+        b.offsets.copy_(torch.tensor(offsets, dtype=torch.int64))
+        b.run()
+        torch.cuda.synchronize()
+
+
+def _slot(b, s, j):
+    return int(b.table[s, j // b.page]), j % b.page
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("mbs", [True, False])
+def test_nan_goes_where_it_is_seen(mx, D, mbs):
+    """NaN blocks of keys and of values: in the rows that see them and in no other, whatever tile they share."""
+    n, keys = [40, 1, 3], [40, 100, 70]
+    b = Batch(mx, 6, n, keys, 4, 2, D, 16, mbs)
+    clean, _ = b.run()
+    p, at = _slot(b, 0, 30)
+    b.caches[1][1][p, 1, D // 32 - 1, at] = 255   # value of key 30, head 1, last block
+    p, at = _slot(b, 1, 77)
+    b.caches[0][1][p, 0, 0, at] = 255             # key 77, head 0
+    p, at = _slot(b, 2, 69)
+    b.caches[1][1][p, 0, 0, at] = 255             # value that only the last query sees
+    out, _ = b.check()
+    nan = torch.isnan(out.float())
+    assert not bool(nan[:30].any()) and bool(nan[30:40, 2:, D - 32:].all()) and not bool(nan[30:40, :2].any()) and not bool(nan[30:40, 2:, :D - 32].any())
+    assert bool(nan[40, :2].all()) and not bool(nan[40, 2:].any())
+    assert not bool(nan[41:43].any()) and bool(nan[43, :2, :32].all()) and not bool(nan[43, 2:].any())
+    assert torch.equal(out[:30], clean[:30]) and torch.equal(out[41:43], clean[41:43])
+    b.check(causal=False)
+    b.check(window=7)
+
+
+def test_nan_and_infinity_in_queries(mx):
+    b = Batch(mx, 7, [1, 30], [100, 64], 4, 2, 128, 16, True)
+    b.q[0, 1, 5] = float("nan")
+    b.q[9, 2, 7] = float("inf")
+    out, lse = b.run()
+    nan = torch.isnan(out.float()).all(-1)
+    assert bool(nan[0, 1]) and bool(nan[9, 2]) and int(nan.sum()) == 2 and int(torch.isnan(lse).sum()) == 2
+    assert int(torch.isnan(out.float()).sum()) == 2 * 128
+
+
+def test_a_page_used_twice_and_a_shared_prefix(mx):
+    """Requests that share pages, and a page that stands in a table twice."""
+    b = Batch(mx, 8, [1, 2, 5], [150, 150, 150], 4, 2, 128, 16, True)
+    b.table[1, :6] = b.table[0, :6]
+    b.table[2, 3] = b.table[2, 1]
+    b.check()
+
+
+def test_results_do_not_depend_on_the_batch(mx):
+    """A request alone and among others: within the tolerance of either, and twice the same call the same bits."""
+    b = Batch(mx, 9, [1] * 9, [5000, 1, 77, 3000, 0, 64, 900, 2, 333], 8, 2, 128, 64, True)
+    one, lse = b.check()
+    again, lse_again = b.run()
+    assert torch.equal(one, again) and torch.equal(lse, lse_again)
+
+
+@pytest.mark.parametrize("n, keys", [([1, 1], [3000, 20]), ([50, 3], [70, 900])])
+def test_workspaces_streams_and_graphs(mx, n, keys):
+    """A caller's workspace with anything in it; another stream; captured and replayed over changed lengths and queries."""
+    b = Batch(mx, 10, n, keys, 8, 2, 128, 16, True)
+    T, Hq, D = b.q.shape
+    want = b.check()
+    size = mx.mx_attention_kv_workspace(len(n), T, Hq, 2, D)
+    work = torch.full((size + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+    got = b.run(workspace=work[:size])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool((work[size:] == 0xFF).all())
+    with pytest.raises(mx.MxError):
+        b.run(workspace=work[:size - 16])
+    out, lse = torch.zeros_like(want[0]), torch.zeros_like(want[1])
+
+    def call():
+        mx.mx_attention_kv(b.q, b.offsets, b.lens, b.table, *b.caches, out=out, lse=lse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out, want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for cut in (0, 1, 17):
+        b.lens.copy_(torch.tensor([max(0, L - cut) for L in keys], dtype=torch.int32))
+        b.q.mul_(0.9)
+        graph.replay()
+        got = out.clone(), lse.clone()
+        out.zero_()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+
+
+def test_a_serving_loop(mx, oracle):
+    """Prompts, then single tokens: plan, norm and rotation with the cache write, attention, step after step from the GPU's own arrays, against the
+    same steps in 64 bits on the rows that were stored."""
+    S, Hq, Hkv, D, page, width = 3, 6, 2, 128, 16, 6
+    k_cache, v_cache = mx.mx_kv_cache(12, Hkv, D, page)
+    table = torch.full((S, width), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(12, device="cuda").int()
+    lens, start = torch.zeros(S, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    angle = torch.arange(128, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64) / D)
+    cos_sin = torch.cat((angle.cos(), angle.sin()), -1).float().cuda()
+    w = torch.linspace(0.6, 1.4, D, device="cuda").to(torch.bfloat16)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    ctx = np.zeros(S, np.int64)
+    for step, new in enumerate(([20, 7, 33], [1, 1, 1], [1, 0, 1], [2, 9, 1], [1, 1, 1])):
+        T = sum(new) + 2  # a padded batch
+        qkv = torch.randn((T, Hq + 2 * Hkv, D), generator=g, device="cuda").to(torch.bfloat16)
+        q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+        n = torch.tensor(new, dtype=torch.int32, device="cuda")
+        offsets, lens, slots, positions, start = mx.mx_kv_plan(lens, n, page, table, free, start, T)
+        rotated = mx.mx_qk_norm_rope_kv_write(q, k, v, positions, slots, cos_sin, k_cache, v_cache, w, w)
+        out = torch.full((T, Hq, D), 5.0, dtype=torch.bfloat16, device="cuda")
+        mx.mx_attention_kv(rotated, offsets, lens, table, k_cache, v_cache, out=out)
+        ctx += np.array(new)
+        assert np.array_equal(lens.cpu().numpy(), ctx) and start.item() == sum(-(-int(c) // page) for c in ctx)
+        live = sum(new)
+        assert bool((slots[live:] == -1).all()) and bool((out[live:] == 5.0).all())
+        want_q = ref.to_bf16(ref.norm_rope(q[:live], positions[:live], cos_sin, w, 1e-6, "half"))
+        want_k = ref.to_bf16(ref.norm_rope(k[:live], positions[:live], cos_sin, w, 1e-6, "half"))
+        assert np.array_equal(ref.bits(rotated[:live]), ref.bits(want_q))
+        places = slots[:live].cpu().numpy()
+        for cache, is_key, x in ((k_cache, True, want_k), (v_cache, False, v[:live])):
+            for a, b in zip(ref.cached_rows(cache, is_key, places), ref.quantized_rows(oracle, x, "oas", True)):
+                assert np.array_equal(a, b)
+        want, _, tol, _, written = ref.attention(rotated, offsets, lens, table, k_cache, v_cache, D ** -0.5, True, 0)
+        assert written[:live].all() and not written[live:].any()
+        assert (np.abs(out.cpu().double().numpy() - want) <= tol)[written].all()
