@@ -199,7 +199,8 @@ def _torch():
 
 # (in the order in which csrc_host/marshal.cpp keeps the addresses)
 _NATIVE_CALLS = ("mx_quantize", "mx_quantize_mbs", "mx_quantize_mbs_pair", "mx_quantize_mbs_dynamic", "mx_quantize_elem", "mx_dequantize", "mx_gemm",
-                 "mx_gemm_mbs", "mx_gemm_mbs_grouped", "mx_gemm_mbs_quantize_a", "mx_gemm_mbs_elem", "mx_gemm_mbs_elem_grouped")
+                 "mx_gemm_mbs", "mx_gemm_mbs_grouped", "mx_gemm_mbs_quantize_a", "mx_gemm_mbs_elem", "mx_gemm_mbs_elem_grouped", "mx_kv_plan",
+                 "mx_qk_norm_rope", "mx_kv_write", "mx_qk_norm_rope_kv_write", "mx_kv_read", "mx_attention_kv", "mx_attention_kv_workspace")
 
 
 def marshal_tag(torch) -> str:
@@ -705,6 +706,9 @@ def mx_kv_plan(ctx_lens, new_lens, page_size, block_table, free_pages, free_star
                positions=None, free_next=None):
     """Pages, slots, positions and offsets of a step whose requests have ctx_lens tokens and bring new_lens; block_table is extended in place.
     Returns (row_offsets, kv_lens, slots, positions, free_next)."""
+    if _native is not None and free_next is not None and _done(_native.kv_plan(ctx_lens, new_lens, page_size, block_table, free_pages, free_start,
+                                                                               total_tokens, row_offsets, kv_lens, slots, positions, free_next), "mx_kv_plan"):
+        return row_offsets, kv_lens, slots, positions, free_next
     torch = _torch_module or _torch()
     i32, i64 = torch.int32, torch.int64
     S = _here(ctx_lens, i32, "ctx_lens", 1).shape[0]
@@ -751,6 +755,9 @@ def _turn_arguments(q, k, positions, cos_sin, q_weight, k_weight, style):
 def mx_qk_norm_rope(q, k, positions, cos_sin, q_weight=None, k_weight=None, eps=1e-6, style="half", q_out=None, k_out=None):
     """RMS norm (where there is a weight) and rotation (where there is a table) of the heads of q [T, Hq, D] and k [T, Hkv, D], bf16.
     cos_sin fp32 [positions, R]: R/2 cosines, then R/2 sines.  Outputs may be the inputs.  Returns (q_out, k_out)."""
+    if _native is not None and k_out is not None and _done(
+            _native.qk_norm_rope(q, k, positions, cos_sin, q_weight, k_weight, eps, style, q_out, k_out), "mx_qk_norm_rope"):
+        return q_out, k_out
     torch = _torch_module or _torch()
     T, Hq, Hkv, D, R, table, ldq, ldk, code = _turn_arguments(q, k, positions, cos_sin, q_weight, k_weight, style)
     q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
@@ -764,6 +771,8 @@ def mx_qk_norm_rope(q, k, positions, cos_sin, q_weight=None, k_weight=None, eps=
 
 def mx_kv_write(k, v, slots, k_cache, v_cache, rule="oas"):
     """Quantizes k, v [T, Hkv, D] (bf16) into the places `slots` (int64 [T], distinct) of the cache."""
+    if _native is not None and _done(_native.kv_write(k, v, slots, *k_cache, *v_cache, rule), "mx_kv_write"):
+        return
     torch = _torch_module or _torch()
     pointers, pages, heads, page, D = _cache_arrays(k_cache, v_cache)
     ldk = _rows_of_heads(k, torch.bfloat16, "k")
@@ -779,6 +788,10 @@ def mx_kv_write(k, v, slots, k_cache, v_cache, rule="oas"):
 def mx_qk_norm_rope_kv_write(q, k, v, positions, slots, cos_sin, k_cache, v_cache, q_weight=None, k_weight=None, eps=1e-6, style="half", rule="oas",
                              q_out=None):
     """mx_qk_norm_rope, then mx_kv_write of the rotated keys and the values, in one launch and with the same bits.  Returns q_out."""
+    if _native is not None and q_out is not None and _done(
+            _native.qk_norm_rope_kv_write(q, k, v, positions, slots, cos_sin, *k_cache, *v_cache, q_weight, k_weight, eps, style, rule, q_out),
+            "mx_qk_norm_rope_kv_write"):
+        return q_out
     torch = _torch_module or _torch()
     pointers, pages, heads, page, head_dim = _cache_arrays(k_cache, v_cache)
     T, Hq, Hkv, D, R, table, ldq, ldk, code = _turn_arguments(q, k, positions, cos_sin, q_weight, k_weight, style)
@@ -796,6 +809,8 @@ def mx_qk_norm_rope_kv_write(q, k, v, positions, slots, cos_sin, k_cache, v_cach
 
 def mx_kv_read(slots, k_cache, v_cache, out_dtype="bf16", k_out=None, v_out=None):
     """Rows of the cache by slot, rounded as by mx_dequantize.  Returns (k_out, v_out) [T, Hkv, D]."""
+    if _native is not None and v_out is not None and _done(_native.kv_read(slots, *k_cache, *v_cache, out_dtype, k_out, v_out), "mx_kv_read"):
+        return k_out, v_out
     torch = _torch_module or _torch()
     pointers, pages, heads, page, D = _cache_arrays(k_cache, v_cache)
     T = _here(slots, torch.int64, "slots", 1).shape[0]
@@ -820,6 +835,10 @@ def mx_attention_kv(q, row_offsets, kv_lens, block_table, k_cache, v_cache, scal
     """Attention of q [T, Hq, D] (bf16; request s has the rows row_offsets[s] .. row_offsets[s+1]-1) over the cache: request s has kv_lens[s]
     keys in the pages block_table[s].  scale: 1 / sqrt(D) if None.  lse: fp32 [T, Hq], filled if given.  workspace: uint8, if the caller keeps
     one (calls that can run at the same time need one each); else it comes from the allocator.  Returns out, bf16 [T, Hq, D]."""
+    if _native is not None and out is not None and _done(
+            _native.attention_kv(q, row_offsets, kv_lens, block_table, *k_cache, *v_cache, q.shape[-1] ** -0.5 if scale is None else scale, causal, window, out,
+                                 lse, workspace), "mx_attention_kv"):
+        return out
     torch = _torch_module or _torch()
     pointers, pages, heads, page, D = _cache_arrays(k_cache, v_cache)
     ldq = _rows_of_heads(q, torch.bfloat16, "q")

@@ -11,6 +11,7 @@
 
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -32,6 +33,13 @@ struct Calls {  // the C entry points, by the addresses that the binding passes 
     decltype(&mx_gemm_mbs_quantize_a) gemm_mbs_quantize_a;
     decltype(&mx_gemm_mbs_elem) gemm_mbs_elem;
     decltype(&mx_gemm_mbs_elem_grouped) gemm_mbs_elem_grouped;
+    decltype(&mx_kv_plan) kv_plan;
+    decltype(&mx_qk_norm_rope) qk_norm_rope;
+    decltype(&mx_kv_write) kv_write;
+    decltype(&mx_qk_norm_rope_kv_write) qk_norm_rope_kv_write;
+    decltype(&mx_kv_read) kv_read;
+    decltype(&mx_attention_kv) attention_kv;
+    decltype(&mx_attention_kv_workspace) attention_kv_workspace;
 } calls;
 
 struct Declined {};  // the arguments are not what is served here
@@ -130,7 +138,7 @@ bool flag(PyObject* o) { return o == Py_True; }
 void* stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
 // Whether the arguments have the types that are served: t = tensor, o = tensor or None, s = text, d = text or torch dtype, i = int,
-// b = bool.  Looked at before anything that throws: an exception costs 2 us, a third of the call that the binding's Python code then makes.
+// b = bool, f = float.  Looked at before anything that throws: an exception costs 2 us, a third of the call that the binding's Python code then makes.
 bool served(PyObject* const* a, Py_ssize_t n, const char* kinds) {
     for (Py_ssize_t i = 0; i < n; ++i) {
         bool ok = false;
@@ -141,6 +149,7 @@ bool served(PyObject* const* a, Py_ssize_t n, const char* kinds) {
             case 'd': ok = PyUnicode_CheckExact(a[i]) || THPDtype_Check(a[i]); break;
             case 'i': ok = PyLong_CheckExact(a[i]); break;
             case 'b': ok = PyBool_Check(a[i]); break;
+            case 'f': ok = PyFloat_CheckExact(a[i]); break;
         }
         if (!ok) return false;
     }
@@ -332,6 +341,198 @@ MX_CALL(gemm_mbs_elem_grouped) {  // a_elem .. b_mbs, row_offsets, N, type, out
     });
 }
 
+// ---- the paged cache: every tensor is on the current device, or the call is declined ----
+struct Here {
+    c10::hip::HIPStream on = c10::hip::getCurrentHIPStream();
+    void* stream() const { return on.stream(); }
+    const at::Tensor& any(PyObject* o, at::ScalarType type) const {
+        const at::Tensor& t = tensor(o);
+        need(t.scalar_type() == type && t.device().index() == on.device_index());
+        return t;
+    }
+    template <typename T>
+    T* flat(PyObject* o, at::ScalarType type, at::IntArrayRef shape) const {
+        const at::Tensor& t = any(o, type);
+        need(t.sizes() == shape && t.is_contiguous());
+        return address<T>(t);
+    }
+    template <typename T>
+    T* flat_or_null(PyObject* o, at::ScalarType type, at::IntArrayRef shape) const {
+        return o == Py_None ? nullptr : flat<T>(o, type, shape);
+    }
+    struct Heads {  // [T, heads, D], a token's heads next to each other
+        void* data;
+        int64_t T, H, D, ld;
+    };
+    Heads heads(PyObject* o, at::ScalarType type = at::kBFloat16) const {
+        const at::Tensor& t = any(o, type);
+        need(t.dim() == 3);
+        const Heads h = {address<void>(t), t.size(0), t.size(1), t.size(2), t.stride(0)};
+        if (h.T && h.H) need((t.stride(2) == 1 || h.D <= 1) && (t.stride(1) == h.D || h.H <= 1));
+        return {h.data, h.T, h.H, h.D, h.T > 1 ? h.ld : std::max(h.ld, h.H * h.D)};
+    }
+    Heads heads(PyObject* o, at::ScalarType type, int64_t T, int64_t H, int64_t D) const {
+        const Heads h = heads(o, type);
+        need(h.T == T && h.H == H && h.D == D);
+        return h;
+    }
+    struct Cache {
+        uint8_t *kc, *ks, *km, *vc, *vs, *vm;
+        int64_t pages, heads, page, D;
+    };
+    Cache cache(PyObject* const* a) const {  // k codes, scales, mbs, v codes, scales, mbs
+        const at::Tensor& k = any(a[0], at::kByte);
+        need(k.dim() == 5);
+        const int64_t P = k.size(0), H = k.size(1), B = k.size(2), page = k.size(3), D = 32 * B;
+        Cache c = {};
+        c.kc = flat<uint8_t>(a[0], at::kByte, {P, H, B, page, 16});
+        c.ks = flat<uint8_t>(a[1], at::kByte, {P, H, B, page});
+        c.km = flat_or_null<uint8_t>(a[2], at::kByte, {P, H, (D + 127) / 128, page});
+        c.vc = flat<uint8_t>(a[3], at::kByte, {P, H, page / 4, D / 8, 4, 4});
+        c.vs = flat<uint8_t>(a[4], at::kByte, {P, H, B, page});
+        c.vm = flat_or_null<uint8_t>(a[5], at::kByte, {P, H, (D + 127) / 128, page});
+        need((a[2] == Py_None) == (a[5] == Py_None));
+        c.pages = P; c.heads = H; c.page = page; c.D = D;
+        return c;
+    }
+    struct Turn {
+        Heads q, k;
+        const int32_t* positions;
+        const float* table;
+        const void *qw, *kw;
+        int64_t rows, R;
+    };
+    Turn turn(PyObject* q, PyObject* k, PyObject* positions, PyObject* table, PyObject* qw, PyObject* kw) const {
+        Turn t = {heads(q), heads(k), nullptr, nullptr, nullptr, nullptr, 0, 0};
+        need(t.k.T == t.q.T && t.k.D == t.q.D);
+        if (table != Py_None) {
+            const at::Tensor& x = any(table, at::kFloat);
+            need(x.dim() == 2 && x.is_contiguous() && positions != Py_None);
+            t.table = address<const float>(x);
+            t.rows = x.size(0);
+            t.R = x.size(1);
+            t.positions = flat<const int32_t>(positions, at::kInt, {t.q.T});
+        }
+        t.qw = flat_or_null<const void>(qw, at::kBFloat16, {t.q.D});
+        t.kw = flat_or_null<const void>(kw, at::kBFloat16, {t.q.D});
+        return t;
+    }
+};
+mx_rope_t style(PyObject* o) {
+    static const char* const kNames[] = {"half", "pairs"};  // MX_ROPE_HALF, MX_ROPE_PAIRS
+    return (mx_rope_t)name_of(o, kNames);
+}
+
+MX_CALL(kv_plan) {  // ctx_lens, new_lens, page, block_table, free_pages, free_start, tokens, row_offsets, kv_lens, slots, positions, free_next
+    return run(a, n, "ttitttittttt", [&] {
+        const Here at_;
+        const at::Tensor &ctx = at_.any(a[0], at::kInt), &table = at_.any(a[3], at::kInt), &free = at_.any(a[4], at::kInt);
+        need(ctx.dim() == 1 && table.dim() == 2 && free.dim() == 1);
+        const int64_t S = ctx.size(0), width = table.size(1), count = free.size(0), page = integer(a[2]), T = integer(a[6]);
+        need(T >= 0);
+        const int32_t *c = at_.flat<int32_t>(a[0], at::kInt, {S}), *nw = at_.flat<int32_t>(a[1], at::kInt, {S}), *f = at_.flat<int32_t>(a[4], at::kInt, {count}),
+                      *fs = at_.flat<int32_t>(a[5], at::kInt, {1});
+        int32_t *b = at_.flat<int32_t>(a[3], at::kInt, {S, width}), *lens = at_.flat<int32_t>(a[8], at::kInt, {S}), *pos = at_.flat<int32_t>(a[10], at::kInt, {T}),
+                *next = at_.flat<int32_t>(a[11], at::kInt, {1});
+        int64_t *off = at_.flat<int64_t>(a[7], at::kLong, {S + 1}), *slots = at_.flat<int64_t>(a[9], at::kLong, {T});
+        void* st = at_.stream();
+        return [=] { return calls.kv_plan(c, nw, S, page, b, width, f, count, fs, T, off, lens, slots, pos, next, st); };
+    });
+}
+MX_CALL(qk_norm_rope) {  // q, k, positions, cos_sin, q_weight, k_weight, eps, style, q_out, k_out
+    return run(a, n, "ttoooofstt", [&] {
+        const Here at_;
+        const Here::Turn t = at_.turn(a[0], a[1], a[2], a[3], a[4], a[5]);
+        const double eps = PyFloat_AS_DOUBLE(a[6]);
+        const mx_rope_t how = style(a[7]);
+        const Here::Heads qo = at_.heads(a[8], at::kBFloat16, t.q.T, t.q.H, t.q.D), ko = at_.heads(a[9], at::kBFloat16, t.k.T, t.k.H, t.k.D);
+        void* st = at_.stream();
+        return [=] {
+            return calls.qk_norm_rope(t.q.data, t.q.ld, t.k.data, t.k.ld, t.positions, t.table, t.rows, t.qw, t.kw, eps, how, t.q.T, t.q.H, t.k.H, t.q.D, t.R,
+                                      qo.data, qo.ld, ko.data, ko.ld, st);
+        };
+    });
+}
+MX_CALL(kv_write) {  // k, v, slots, the cache's six, rule
+    return run(a, n, "tttttottos", [&] {
+        const Here at_;
+        const Here::Cache c = at_.cache(a + 3);
+        const Here::Heads k = at_.heads(a[0]);
+        need(k.H == c.heads && k.D == c.D);
+        const Here::Heads v = at_.heads(a[1], at::kBFloat16, k.T, k.H, k.D);
+        const int64_t* slots = at_.flat<int64_t>(a[2], at::kLong, {k.T});
+        const mx_rule_t r = rule(a[9]);
+        void* st = at_.stream();
+        return [=] { return calls.kv_write(k.data, k.ld, v.data, v.ld, slots, r, c.kc, c.ks, c.km, c.vc, c.vs, c.vm, c.pages, c.page, k.T, c.heads, c.D, st); };
+    });
+}
+MX_CALL(qk_norm_rope_kv_write) {  // q, k, v, positions, slots, cos_sin, the cache's six, q_weight, k_weight, eps, style, rule, q_out
+    return run(a, n, "tttotottottooofsst", [&] {
+        const Here at_;
+        const Here::Cache c = at_.cache(a + 6);
+        const Here::Turn t = at_.turn(a[0], a[1], a[3], a[5], a[12], a[13]);
+        need(t.k.H == c.heads && t.k.D == c.D);
+        const Here::Heads v = at_.heads(a[2], at::kBFloat16, t.k.T, t.k.H, t.k.D);
+        const int64_t* slots = at_.flat<int64_t>(a[4], at::kLong, {t.k.T});
+        const double eps = PyFloat_AS_DOUBLE(a[14]);
+        const mx_rope_t how = style(a[15]);
+        const mx_rule_t r = rule(a[16]);
+        const Here::Heads qo = at_.heads(a[17], at::kBFloat16, t.q.T, t.q.H, t.q.D);
+        void* st = at_.stream();
+        return [=] {
+            return calls.qk_norm_rope_kv_write(t.q.data, t.q.ld, t.k.data, t.k.ld, v.data, v.ld, t.positions, t.table, t.rows, t.qw, t.kw, eps, how, slots, r, c.kc, c.ks,
+                                               c.km, c.vc, c.vs, c.vm, c.pages, c.page, t.q.T, t.q.H, t.k.H, t.q.D, t.R, qo.data, qo.ld, st);
+        };
+    });
+}
+MX_CALL(kv_read) {  // slots, the cache's six, type, k_out, v_out
+    return run(a, n, "tttottodtt", [&] {
+        const Here at_;
+        const Here::Cache c = at_.cache(a + 1);
+        const mx_dtype_t type = out_type(a[7]);
+        const at::Tensor& s = at_.any(a[0], at::kLong);
+        need(s.dim() == 1);
+        const int64_t T = s.size(0);
+        const int64_t* slots = at_.flat<int64_t>(a[0], at::kLong, {T});
+        const at::ScalarType as = type == MX_OUT_F32 ? at::kFloat : at::kBFloat16;
+        const Here::Heads k = at_.heads(a[8], as, T, c.heads, c.D), v = at_.heads(a[9], as, T, c.heads, c.D);
+        void* st = at_.stream();
+        return [=] { return calls.kv_read(slots, c.kc, c.ks, c.km, c.vc, c.vs, c.vm, c.pages, c.page, T, c.heads, c.D, type, k.data, k.ld, v.data, v.ld, st); };
+    });
+}
+MX_CALL(attention_kv) {  // q, row_offsets, kv_lens, block_table, the cache's six, scale, causal, window, out, lse, workspace
+    return run(a, n, "ttttttottofbitoo", [&] {
+        const Here at_;
+        const Here::Cache c = at_.cache(a + 4);
+        const Here::Heads q = at_.heads(a[0]);
+        need(q.D == c.D && c.heads && q.H % c.heads == 0);
+        const at::Tensor &l = at_.any(a[2], at::kInt), &b = at_.any(a[3], at::kInt);
+        need(l.dim() == 1 && b.dim() == 2);
+        const int64_t S = l.size(0), width = b.size(1), window = integer(a[12]);
+        const int32_t *lens = at_.flat<int32_t>(a[2], at::kInt, {S}), *table = at_.flat<int32_t>(a[3], at::kInt, {S, width});
+        const int64_t* off = at_.flat<int64_t>(a[1], at::kLong, {S + 1});
+        const float scale = (float)PyFloat_AS_DOUBLE(a[10]);
+        const int causal = flag(a[11]);
+        const Here::Heads o = at_.heads(a[13], at::kBFloat16, q.T, q.H, q.D);
+        float* lse = at_.flat_or_null<float>(a[14], at::kFloat, {q.T, q.H});
+        // (without a workspace of the caller's one from the allocator, which gives it to later work on this stream only)
+        at::Tensor own;
+        if (a[15] == Py_None) {
+            const int64_t size = calls.attention_kv_workspace(S, q.T, q.H, c.heads, c.D);
+            need(size >= 0);
+            own = at::empty({size}, l.options().dtype(at::kByte));
+        } else {
+            own = at_.any(a[15], at::kByte);
+            need(own.dim() == 1 && own.is_contiguous());
+        }
+        void* st = at_.stream();
+        return [=] {
+            return calls.attention_kv(q.data, q.ld, off, lens, table, width, c.kc, c.ks, c.km, c.vc, c.vs, c.vm, c.pages, c.page, S, q.T, q.H, c.heads, c.D, scale, causal,
+                                      window, o.data, o.ld, lse, own.data_ptr(), own.numel(), st);
+        };
+    });
+}
+
 // entry points' addresses, in the order of `Calls`
 PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
     constexpr Py_ssize_t kCount = sizeof(Calls) / sizeof(void*);
@@ -358,7 +559,8 @@ PyObject* built_for(PyObject*, PyObject* const*, Py_ssize_t) { return PyUnicode_
 #define MX_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MX_METHOD(built_for), MX_METHOD(use), MX_METHOD(quantize), MX_METHOD(quantize_mbs), MX_METHOD(quantize_mbs_pair), MX_METHOD(quantize_mbs_dynamic),
                          MX_METHOD(quantize_elem), MX_METHOD(dequantize), MX_METHOD(gemm), MX_METHOD(gemm_mbs), MX_METHOD(gemm_mbs_grouped),
-                         MX_METHOD(gemm_mbs_quantize_a), MX_METHOD(gemm_mbs_elem), MX_METHOD(gemm_mbs_elem_grouped), {nullptr, nullptr, 0, nullptr}};
+                         MX_METHOD(gemm_mbs_quantize_a), MX_METHOD(gemm_mbs_elem), MX_METHOD(gemm_mbs_elem_grouped), MX_METHOD(kv_plan), MX_METHOD(qk_norm_rope), MX_METHOD(kv_write),
+                         MX_METHOD(qk_norm_rope_kv_write), MX_METHOD(kv_read), MX_METHOD(attention_kv), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

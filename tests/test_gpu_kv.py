@@ -294,3 +294,71 @@ def test_refused_on_the_gpu(mx):
                 lambda: mx.mx_qk_norm_rope(x, x, slots.int(), torch.zeros((4, 24), device="cuda"))):
         with pytest.raises((TypeError, ValueError, mx.MxError)):
             bad()
+
+
+# ---- the two ways through the binding ---------------------------------------------------------------------------
+def _calls(mx):
+    """name -> (call with all outputs given, what it writes)"""
+    T, Hq, Hkv, D, page = 21, 4, 2, 128, 16
+    qkv = _rows(3, T, Hq + 2 * Hkv, D)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    one, two = mx.mx_kv_cache(3, Hkv, D, page), mx.mx_kv_cache(3, Hkv, D, page, use_mbs=False)
+    table, positions, slots = _cos_sin(64, D), torch.arange(T, device="cuda").int(), torch.arange(T, device="cuda")
+    w = torch.ones(D, device="cuda", dtype=torch.bfloat16)
+    new = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype, device="cuda")  # noqa: E731
+    qo, ko, qf, kr, vr, out, lse = new(T, Hq, D), new(T, Hkv, D), new(T, Hq, D), new(T, Hkv, D), new(T, Hkv, D), new(T, Hq, D), new(T, Hq, dtype=torch.float32)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    blocks, plan = i32(0, 1, 2).reshape(1, 3), (new(2, dtype=torch.int64), i32(0), new(30, dtype=torch.int64), new(30, dtype=torch.int32), i32(0))
+    arrays = lambda *caches: tuple(a for c in caches for a in c if a is not None)  # noqa: E731
+    return {
+        "kv_plan": (lambda: mx.mx_kv_plan(i32(20), i32(9), page, blocks, i32(5, 6), i32(0), 30, *plan), plan + (blocks,)),
+        "qk_norm_rope": (lambda: mx.mx_qk_norm_rope(q, k, positions, table, w, None, q_out=qo, k_out=ko), (qo, ko)),
+        "kv_write": (lambda: mx.mx_kv_write(k, v, slots, *two), arrays(*two)),
+        "qk_norm_rope_kv_write": (lambda: mx.mx_qk_norm_rope_kv_write(q, k, v, positions, slots, table, *one, w, w, q_out=qf), arrays(*one) + (qf,)),
+        "kv_read": (lambda: mx.mx_kv_read(slots, *one, k_out=kr, v_out=vr), (kr, vr)),
+        "attention_kv": (lambda: mx.mx_attention_kv(qf, torch.tensor([0, T], device="cuda"), i32(T), i32(0, 1, 2).reshape(1, 3), *one, out=out, lse=lse), (out, lse)),
+    }
+
+
+def test_native_and_ctypes_marshalling_agree(mx, monkeypatch):
+    native = mx.binding._native
+    assert native is not None, "the build step makes _marshal.so"
+    served = []
+
+    class Recorder:
+        def __getattr__(self, name):
+            def call(*a):
+                status = getattr(native, name)(*a)
+                served.append((name, status))
+                return status
+            return call
+
+    got = []
+    for used in (Recorder(), None):
+        monkeypatch.setattr(mx.binding, "_native", used)
+        results = {}
+        for name, (call, outputs) in _calls(mx).items():
+            call()
+            results[name] = [o.clone() for o in outputs]
+        got.append(results)
+    assert served == [(name, 0) for name in got[0]]
+    for name in got[0]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0][name], got[1][name])), name
+        assert any(bool((a != 0).any()) for a in got[0][name]), name
+
+
+def test_native_marshalling_declines_what_the_binding_refuses(mx):
+    native = mx.binding._native
+    kc, vc = mx.mx_kv_cache(2, 2, 128, 16)
+    x = torch.zeros((3, 2, 128), dtype=torch.bfloat16, device="cuda")
+    slots, lens, off = torch.arange(3, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+    table = torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    attend = lambda **k: native.attention_kv(*dict(dict(q=x, off=off, lens=lens, table=table, a=kc[0], b=kc[1], c=kc[2], d=vc[0], e=vc[1], f=vc[2], scale=1.0,  # noqa: E731
+                                                        causal=True, window=0, out=x.clone(), lse=None, work=None), **k).values())
+    assert attend() == 0 and attend(window=-1) == -1 and attend(work=torch.empty(0, dtype=torch.uint8, device="cuda")) == -1
+    assert attend(q=x.float()) is None and attend(off=off[:1]) is None and attend(out=x[:2]) is None and attend(c=None) is None and attend(scale=1) is None
+    assert attend(table=table.long()) is None and attend(lse=torch.zeros(3, 2)) is None and attend(a=kc[0].cpu()) is None
+    assert native.kv_write(x, x, slots, *kc, *vc, "oas") == 0 and native.kv_write(x, x, slots, *kc, *vc, "best") is None
+    assert native.kv_write(x, x[:, :1], slots, *kc, *vc, "oas") is None and native.kv_write(x, x, slots, *vc, *kc, "oas") is None
+    assert native.kv_read(slots, *kc, *vc, "bf16", x.clone(), x.clone().float()) is None
+    assert native.qk_norm_rope(x, x, None, torch.zeros((4, 128), device="cuda"), None, None, 1e-6, "half", x.clone(), x.clone()) is None
