@@ -39,8 +39,7 @@ struct AttentionArgs {
     int32_t num_pages, max_pages, room;
     int32_t S, T, Hq, group;  // group: query heads of a key head
     int32_t window, causal;
-    int32_t target;           // pieces that the batch is cut into, about
-    int64_t slots;            // pieces that the workspace has room for
+    int32_t workers_log2;     // wavefronts that the batch is cut for
     float scale2;             // scale * log2(e)
 };
 
@@ -51,6 +50,7 @@ int64_t attention_rows_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, 
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));

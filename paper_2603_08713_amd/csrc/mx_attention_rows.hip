@@ -1,11 +1,10 @@
 // Attention over the paged MXFP4 cache for few query rows per key head: single tokens (decode), a few tokens of a request.
 //
-// A row tile is 16 kTiles rows: (token, query head of the key head), padded.  A workgroup of four wavefronts takes one piece of one
-// row tile's keys, each wavefront every fourth tile of 64 keys, loading the next one's codes while it works on one; their results
-// are joined in LDS.  Pieces are cut on the GPU from the lengths of the moment: every wavefront sums up the batch (requests x row
-// tiles x tiles of keys), so that a share is the same for all and a long request among short ones is spread over more workgroups; the
-// grid has room for the most that can come out.  Rows cut into several pieces leave (m, l, O) in the workspace, joined by
-// a second kernel.
+// A row tile is 16 kTiles rows: (token, query head of the key head), padded.  The tiles of 64 keys of all row tiles, heads and requests
+// stand in one line (KvLine), which is cut into equal shares on the GPU, from the lengths of the moment: one for each of the wavefronts
+// that the device holds at once, whatever the batch - a long request among short ones is spread over more of them, and none waits for a
+// second round.  A wavefront goes along its share by itself, loading the next tile's codes while it works on one; items that it
+// does not take whole leave (m, l, O) in the workspace, joined by a second kernel.
 #include "mx_attention.h"
 
 #include <type_traits>
@@ -14,80 +13,74 @@ namespace mx {
 namespace {
 
 constexpr int kThreads = 256, kWavesInGroup = kThreads / kWave;
-constexpr int32_t kLeastShare = kWavesInGroup;  // a tile for every wavefront
+constexpr int32_t kLeastShare = 1;
 
-__device__ __forceinline__ KvRequest request_of(const AttentionArgs& a, int s) {
-    return KvRequest::make(a.row_offsets[s], a.row_offsets[s + 1], a.kv_lens[s], a.T, a.room);
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int32_t read_lane(int32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ int64_t read_lane(int64_t x, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)read_lane((int32_t)x, lane) | (uint64_t)(uint32_t)read_lane((int32_t)(x >> 32), lane) << 32);
 }
 
-struct Piece {
-    int32_t s, row_tile, index, count;  // which request, row tile, piece of its keys, and of how many
-    int32_t share;                      // tiles of keys of a piece
-    int64_t base;                       // units before the request
-    bool found;
+// The batch as a wavefront sees it: a lane has a request, of 64 at a time (what a batch of up to 64 needs is loaded once).
+struct Batch {
+    const AttentionArgs& a;
+    int height, block, lanes;
+    KvRequest r;
+    int32_t tiles, row_tiles;
+    int64_t size, end, total;  // tiles of the lane's request, and where it ends on the line
+    int32_t share;
+
+    __device__ __forceinline__ Batch(const AttentionArgs& args, int rows) : a(args), height(rows), lanes(min(args.S, 64)) {
+        total = 0;
+        for (int s = (a.S - 1) / 64 * 64; s >= 0; s -= 64) {  // (backwards: the first 64 stay loaded)
+            load(s);
+            scan(0);
+            total += read_lane(end, 63);
+        }
+        share = uniform(KvLine::share(total, a.workers_log2, kLeastShare));
+    }
+    __device__ __forceinline__ void load(int first) {
+        block = first;
+        const int s = first + (int)(threadIdx.x & 63);
+        r = KvRequest{0, 0, 0, 0};
+        if (s < a.S) r = KvRequest::make(a.row_offsets[s], a.row_offsets[s + 1], a.kv_lens[s], a.T, a.room);
+        tiles = r.tiles(a.window, a.causal);
+        row_tiles = r.row_tiles(a.group, height);
+        size = KvLine::request(tiles, row_tiles, a.cache.at.heads);
+    }
+    // (through the lanes by DPP: rows of 16, then pairs of rows, then halves; the LDS crossbar would take its latency twelve times)
+    __device__ __forceinline__ void scan(int64_t before) {
+        end = size;
+        end = add_from<0x111, 0xF>(end);  // row_shr:1, 2, 4, 8
+        end = add_from<0x112, 0xF>(end);
+        end = add_from<0x114, 0xF>(end);
+        end = add_from<0x118, 0xF>(end);
+        end = add_from<0x142, 0xA>(end);  // row_bcast:15 into rows 1 and 3
+        end = add_from<0x143, 0xC>(end);  // row_bcast:31 into rows 2 and 3
+        end += before;
+    }
+    template <int kControl, int kRows>
+    __device__ __forceinline__ static int64_t add_from(int64_t x) {
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kControl, kRows, 0xF, false);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(x >> 32), kControl, kRows, 0xF, false);
+        return x + (int64_t)((uint64_t)hi << 32 | lo);
+    }
+    // the lane that has the request that `mine` (of a lane) says, moving on through the blocks; -1: none has
+    template <typename F>
+    __device__ __forceinline__ int find(F&& mine) {
+        while (true) {
+            const uint64_t hit = __builtin_amdgcn_ballot_w64((int)(threadIdx.x & 63) < lanes && mine());
+            if (hit) return __builtin_ctzll(hit);
+            if (block + 64 >= a.S) return -1;
+            const int64_t before = read_lane(end, 63);
+            load(block + 64);
+            scan(before);
+        }
+    }
+    __device__ __forceinline__ KvRequest request(int lane) const {
+        return KvRequest{read_lane(r.first, lane), read_lane(r.rows, lane), read_lane(r.pos0, lane), read_lane(r.keys, lane)};
+    }
 };
-
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor((long long)x, m);
-    return x;
-}
-
-// The share of a piece, for the batch as it is.
-__device__ __forceinline__ int32_t share_of(const AttentionArgs& a, int height) {
-    const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    for (int s = lane; s < a.S; s += 64) {
-        const KvRequest r = request_of(a, s);
-        total += (int64_t)r.row_tiles(a.group, height) * r.tiles(a.window, a.causal);
-    }
-    return kv_share(wave_sum(total) * a.cache.at.heads, a.target, kLeastShare);
-}
-
-// The request whose units (row tiles x pieces; `row` >= 0: whose query rows) hold `unit`.
-__device__ __forceinline__ Piece locate(const AttentionArgs& a, int height, int64_t unit, int32_t row) {
-    const int lane = threadIdx.x & 63;
-    Piece p = {};
-    p.share = share_of(a, height);
-    int64_t before = 0;
-    for (int s0 = 0; s0 < a.S; s0 += 64) {
-        const int s = s0 + lane;
-        int64_t units = 0;
-        int32_t pieces = 0;
-        bool mine = false;
-        if (s < a.S) {
-            const KvRequest r = request_of(a, s);
-            pieces = kv_pieces(r.tiles(a.window, a.causal), p.share);
-            units = (int64_t)r.row_tiles(a.group, height) * pieces;
-            mine = row >= 0 && row >= r.first && row < r.first + r.rows;
-        }
-        int64_t sum = units;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t x = __shfl_up((long long)sum, d);
-            if (lane >= d) sum += x;
-        }
-        if (row < 0) mine = before + sum > unit;
-        const uint64_t hit = __builtin_amdgcn_ballot_w64(mine);
-        if (hit) {
-            const int at = __builtin_ctzll(hit);
-            p.s = s0 + at;
-            p.count = __builtin_amdgcn_readlane(pieces, at);
-            p.base = before + __shfl((long long)(sum - units), at);
-            p.found = true;
-            if (row < 0) {
-                const int32_t u = (int32_t)(unit - p.base);  // row tile fastest: the pieces of one range of keys run together
-                const int32_t tiles = (int32_t)(__shfl((long long)units, at) / p.count);
-                p.index = __builtin_amdgcn_readfirstlane(u / tiles);
-                p.row_tile = __builtin_amdgcn_readfirstlane(u - p.index * tiles);
-            }
-            p.s = __builtin_amdgcn_readfirstlane(p.s);
-            return p;
-        }
-        before += __shfl((long long)sum, 63);
-    }
-    return p;
-}
 
 // One tile of 64 keys of a head, as a lane holds it.
 template <int D, bool kMbs>
@@ -100,59 +93,90 @@ struct TileRegs {
     uint32_t kw[kMbs ? H::words : 1], vw[kMbs ? H::words : 1];  // MBS words of token `lane`
 };
 
-template <int D, bool kMbs>
-__device__ __forceinline__ void load_tile(TileRegs<D, kMbs>& r, const AttentionArgs& a, const int32_t (&page)[4], int32_t token0, int head) {
+// Where a lane's pieces of a tile lie: bytes from the first place of a subtile in a page's part of a head.
+template <int D>
+struct LaneOffsets {
     using H = HeadShape<D>;
-    const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
-    const KvLayout& at = a.cache.at;
-    const int32_t mask = at.page_size() - 1;
+    uint32_t k[H::parts], ks[H::parts], v[H::parts], vs[H::parts];
+    __device__ __forceinline__ explicit LaneOffsets(int shift) {
+        const uint32_t lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+#pragma unroll
+        for (int p = 0; p < H::parts; ++p) {
+            const uint32_t b0 = H::start(p) / 32, narrow = H::width(p) == 128 ? 0 : H::width(p) == 64 ? 1 : 2;  // lanes that share a block, log2
+            const uint32_t kb = b0 + (g >> narrow), vb = b0 + (n >> (2 + narrow));
+            const uint32_t own = H::width(p) == 128 ? 0 : H::width(p) == 64 ? (g & 1) * 8 : g * 4;
+            k[p] = (((kb << shift) + n) << 4) + own;
+            ks[p] = (kb << shift) + n;
+            v[p] = g * (2 * D) + (H::start(p) / 8 + (n >> narrow)) * 16;
+            vs[p] = (vb << shift) + 4 * g;
+        }
+    }
+};
+
+// The head's part of each array, and the bytes of a page.
+struct HeadArrays {
+    const uint8_t *kc, *ks, *km, *vc, *vs, *vm;
+    uint32_t code_page, scale_page, word_page;
+    __device__ __forceinline__ HeadArrays(const KvArrays& c, int head) {
+        const KvLayout& at = c.at;
+        kc = c.k_codes + at.k_block(0, head, 0, 0);
+        vc = c.v_codes + at.v_unit(0, head, 0, 0);
+        ks = c.k_scales + at.scale(0, head, 0, 0);
+        vs = c.v_scales + at.scale(0, head, 0, 0);
+        km = c.k_mbs + at.word(0, head, 0, 0);
+        vm = c.v_mbs + at.word(0, head, 0, 0);
+        code_page = (uint32_t)at.k_block(1, 0, 0, 0);
+        scale_page = (uint32_t)at.scale(1, 0, 0, 0);
+        word_page = (uint32_t)at.word(1, 0, 0, 0);
+    }
+};
+
+template <int D, bool kMbs>
+__device__ __forceinline__ void load_tile(TileRegs<D, kMbs>& r, const HeadArrays& a, const LaneOffsets<D>& off, int shift, const int32_t (&page)[4], int32_t token0) {
+    using H = HeadShape<D>;
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int32_t mask = (1 << shift) - 1;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const int32_t place = (token0 + 16 * t) & mask;
-        const uint8_t* kc = a.cache.k_codes + at.k_block(page[t], head, 0, place);
-        const uint8_t* ks = a.cache.k_scales + at.scale(page[t], head, 0, place);
-        const uint8_t* vc = a.cache.v_codes + at.v_unit(page[t], head, 0, place);
-        const uint8_t* vs = a.cache.v_scales + at.scale(page[t], head, 0, place);
+        const uint32_t place = (token0 + 16 * t) & mask;
+        const uint64_t code = (uint64_t)(uint32_t)page[t] * a.code_page, scale = (uint64_t)(uint32_t)page[t] * a.scale_page + place;
+        const uint8_t *kc = a.kc + (code + place * 16), *vc = a.vc + (code + place * (D / 2)), *ks = a.ks + scale, *vs = a.vs + scale;
         int step = 0;
 #pragma unroll
         for (int p = 0; p < H::parts; ++p) {
-            const int b0 = H::start(p) / 32;
-            {
-                if (H::width(p) == 128) {
-                    const int32_t b = b0 + g;
-                    const u32x4 x = *reinterpret_cast<const u32x4*>(kc + (((b << at.page_shift) + n) << 4));
-                    r.k[t][step] = x[0]; r.k[t][step + 1] = x[1]; r.k[t][step + 2] = x[2]; r.k[t][step + 3] = x[3];
-                    r.ks[t][p] = ks[(b << at.page_shift) + n];
-                    r.v[t][p] = *reinterpret_cast<const u32x4*>(vc + g * (2 * D) + (H::start(p) / 8 + n) * 16);
-                    r.vs[t][p] = *reinterpret_cast<const uint32_t*>(vs + ((b0 + (n >> 2)) << at.page_shift) + 4 * g);
-                    step += 4;
-                } else if (H::width(p) == 64) {
-                    const int32_t b = b0 + (g >> 1);
-                    const u32x2 x = *reinterpret_cast<const u32x2*>(kc + (((b << at.page_shift) + n) << 4) + (g & 1) * 8);
-                    r.k[t][step] = x[0]; r.k[t][step + 1] = x[1];
-                    r.ks[t][p] = ks[(b << at.page_shift) + n];
-                    r.v[t][p] = *reinterpret_cast<const u32x4*>(vc + g * (2 * D) + (H::start(p) / 8 + (n >> 1)) * 16);
-                    r.vs[t][p] = *reinterpret_cast<const uint32_t*>(vs + ((b0 + (n >> 3)) << at.page_shift) + 4 * g);
-                    step += 2;
-                } else {
-                    r.k[t][step] = *reinterpret_cast<const uint32_t*>(kc + (((b0 << at.page_shift) + n) << 4) + g * 4);
-                    r.ks[t][p] = ks[(b0 << at.page_shift) + n];
-                    r.v[t][p] = *reinterpret_cast<const u32x4*>(vc + g * (2 * D) + (H::start(p) / 8 + (n >> 2)) * 16);
-                    r.vs[t][p] = *reinterpret_cast<const uint32_t*>(vs + (b0 << at.page_shift) + 4 * g);
-                    step += 1;
-                }
+            if (H::width(p) == 128) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(kc + off.k[p]);
+                r.k[t][step] = x[0]; r.k[t][step + 1] = x[1]; r.k[t][step + 2] = x[2]; r.k[t][step + 3] = x[3];
+            } else if (H::width(p) == 64) {
+                const u32x2 x = *reinterpret_cast<const u32x2*>(kc + off.k[p]);
+                r.k[t][step] = x[0]; r.k[t][step + 1] = x[1];
+            } else {
+                r.k[t][step] = *reinterpret_cast<const uint32_t*>(kc + off.k[p]);
             }
+            step += H::width(p) / 32;
+            r.ks[t][p] = ks[off.ks[p]];
+            r.v[t][p] = *reinterpret_cast<const u32x4*>(vc + off.v[p]);
+            r.vs[t][p] = *reinterpret_cast<const uint32_t*>(vs + off.vs[p]);
         }
     }
     if constexpr (kMbs) {
-        const int32_t mine = g == 0 ? page[0] : g == 1 ? page[1] : g == 2 ? page[2] : page[3];
-        const int32_t place = (token0 + lane) & mask;
+        const uint32_t mine = g == 0 ? page[0] : g == 1 ? page[1] : g == 2 ? page[2] : page[3];
+        const uint64_t word = (uint64_t)mine * a.word_page + ((token0 + lane) & mask);
 #pragma unroll
         for (int w = 0; w < H::words; ++w) {
-            r.kw[w] = a.cache.k_mbs[at.word(mine, head, w, place)];
-            r.vw[w] = a.cache.v_mbs[at.word(mine, head, w, place)];
+            r.kw[w] = a.km[word + (w << shift)];
+            r.vw[w] = a.vm[word + (w << shift)];
         }
     }
+}
+
+// Tile i of a batch whose page ids the lanes hold; pages that are not there are read as page 0 (and masked).
+template <int D, bool kMbs>
+__device__ __forceinline__ void fetch_tile(TileRegs<D, kMbs>& r, const HeadArrays& a, const LaneOffsets<D>& off, int shift, int32_t ids, int i, int32_t first) {
+    int32_t page[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) page[t] = max(read_lane(ids, 4 * i + t), 0);
+    load_tile<D, kMbs>(r, a, off, shift, page, (first + i) * kKvTile);
 }
 
 // What a wavefront carries for 16 kTiles rows: O^T by column products, the running maximum (log2 units, the same in the four lanes
@@ -173,7 +197,7 @@ __device__ __forceinline__ void take_tile(State<D, kTiles>& st, TileRegs<D, kMbs
     if constexpr (kMbs) {
 #pragma unroll
         for (int w = 0; w < H::words; ++w) {
-            sigma[w][lane] = sigma_of(r.kw[w]);
+            sigma[w][lane] = sigma_of(r.kw[w]) * scale2;
             sigma[H::words + w][lane] = sigma_of(r.vw[w]);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (one wavefront's own table)
@@ -204,7 +228,7 @@ __device__ __forceinline__ void take_tile(State<D, kTiles>& st, TileRegs<D, kMbs
                 f32x4 x = sum[b][0] * *reinterpret_cast<const f32x4*>(&sigma[0][16 * t + 4 * g]);
 #pragma unroll
                 for (int w = 1; w < H::words; ++w) x += sum[b][w] * *reinterpret_cast<const f32x4*>(&sigma[w][16 * t + 4 * g]);
-                s[b][t] = x * scale2;
+                s[b][t] = x;
             } else {
                 f32x4 x = sum[b][0];
 #pragma unroll
@@ -375,32 +399,68 @@ __device__ __forceinline__ void take_tile(State<D, kTiles>& st, TileRegs<D, kMbs
     }
 }
 
-// floats of a piece in the workspace: m and l of its rows, then O by rows
+// The runs of neighbouring columns of its row that a lane of group g holds: f(first column, how many, values).
+template <int D, typename F>
+__device__ __forceinline__ void each_run(const f32x4 (&o)[HeadShape<D>::columns], int g, F&& f) {
+    using H = HeadShape<D>;
+    auto part = [&](auto index, auto first) __attribute__((always_inline)) {
+        constexpr int p = decltype(index)::value, c0 = decltype(first)::value, wide = H::width(p) / 16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x[wide];
+#pragma unroll
+            for (int c = 0; c < wide; ++c) x[c] = o[c0 + c][i];
+            f(H::start(p) + wide * (4 * g + i), std::integral_constant<int, wide>{}, x);
+        }
+    };
+    part(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+    if constexpr (H::parts > 1) part(std::integral_constant<int, 1>{}, std::integral_constant<int, H::width(0) / 16>{});
+    static_assert(H::parts <= 2, "heads of up to 256");
+}
+
+// floats of a partial result in the workspace: m and l of its rows, then O by rows
 template <int D, int kTiles>
-constexpr int kPieceFloats = 16 * kTiles * (D + 2);
+constexpr int kPartFloats = 16 * kTiles * (D + 2);
+// wavefronts of a launch: what the device holds at once, two a SIMD where the registers allow it
+template <int D, int kTiles>
+constexpr int kWorkersLog2 = D * kTiles <= 128 ? 11 : 10;
 
 template <int D, int kTiles, bool kMbs>
-__global__ __launch_bounds__(kThreads) void attention_rows_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, (kWorkersLog2<D, kTiles> - 9)) void attention_rows_kernel(AttentionArgs a) {
     using H = HeadShape<D>;
     constexpr int kHeight = 16 * kTiles;
-    __shared__ f32x4 joined[kWavesInGroup][8][kWave];
-    __shared__ float stats[kWavesInGroup][2][16];
     __shared__ float sigmas[kMbs ? kWavesInGroup : 1][2 * H::words][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, n = lane & 15;
-    const int heads = a.cache.at.heads;
-    const int head = blockIdx.x % heads;
-    const Piece piece = locate(a, kHeight, blockIdx.x / heads, -1);
-    if (!piece.found) return;
-    const KvRequest r = request_of(a, piece.s);
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, n = lane & 15;
+    const int shift = a.cache.at.page_shift;
+    const LaneOffsets<D> off(shift);
+    float (*sigma)[64] = sigmas[kMbs ? wave : 0];
+    const int32_t worker = blockIdx.x * kWavesInGroup + wave;
+    Batch batch(a, kHeight);
+    const int64_t line_begin = (int64_t)batch.share * worker, line_end = min(batch.total, line_begin + batch.share);
+    for (int64_t line = line_begin; line < line_end;) {
+    // the item that the line has here: request, head and row tile
+    const int who = batch.find([&] { return batch.end > line; });
+    if (who < 0) return;
+    const KvRequest r = batch.request(who);
+    const int32_t s = batch.block + who, item = KvLine::item(read_lane(batch.tiles, who)), row_tiles = read_lane(batch.row_tiles, who);
+    const int64_t begin = read_lane(batch.end, who) - read_lane(batch.size, who), past = line - begin;
+    const int32_t number = past >> 32 ? (int32_t)(past / item) : (int32_t)((uint32_t)past / (uint32_t)item);
+    const int64_t item_at = begin + (int64_t)number * item;
+    const int32_t head = row_tiles == 1 ? number : (int32_t)((uint32_t)number / (uint32_t)row_tiles), row_tile = number - head * row_tiles;
+    const bool direct = KvLine::whole(item_at, item, line_begin, line_end);
+    const int32_t stop = (int32_t)min((int64_t)item, line_end - item_at);
+    const int32_t from = KvLine::tiles_before((int32_t)(line - item_at)), upto = KvLine::tiles_before(stop);  // its tiles that are taken here
+    line = item_at + stop;
+
     const int32_t rows = r.rows * a.group;
-    const int32_t row0 = piece.row_tile * kHeight, row_last = min(row0 + kHeight, rows) - 1;
+    const int32_t row0 = row_tile * kHeight, row_last = min(row0 + kHeight, rows) - 1;
     const int32_t i_first = row0 / a.group, i_last = row_last / a.group;
     // keys that some row of the tile sees, and that all of them see
     const int32_t lo_all = r.lo(i_first, a.window), hi_all = r.hi(i_last, a.causal);
     const int32_t lo_each = r.lo(i_last, a.window), hi_each = r.hi(i_first, a.causal);
-    const int32_t tile0 = r.first_tile(a.window) + piece.index * piece.share;
-    const int32_t tile_end = min(tile0 + piece.share, (hi_all + kKvTile - 1) / kKvTile);
-    int32_t tile = max(tile0, lo_all / kKvTile) + wave;
+    const int32_t tile0 = r.first_tile(a.window);
+    const int32_t tile_end = min(tile0 + upto, (hi_all + kKvTile - 1) / kKvTile);
+    int32_t tile = max(tile0 + from, lo_all / kKvTile);
 
     int32_t lo[kTiles], hi[kTiles];
     u32x4 q[kTiles][H::steps];
@@ -428,202 +488,211 @@ __global__ __launch_bounds__(kThreads) void attention_rows_kernel(AttentionArgs 
         for (int c = 0; c < H::columns; ++c) st.o[b][c] = f32x4{0, 0, 0, 0};
     }
 
-    const int32_t* table = a.block_table + (int64_t)piece.s * a.max_pages;
-    int32_t page[4];
-    auto pages = [&](int32_t at) __attribute__((always_inline)) -> uint32_t {  // which subtiles of tile `at` have a page
-        uint32_t there = 0;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int32_t token = at * kKvTile + 16 * t;
-            int32_t p = -1;
-            if (token < r.keys) p = table[token >> a.cache.at.page_shift];
-            p = __builtin_amdgcn_readfirstlane(p);
-            const bool ok = p >= 0 && p < a.num_pages;
-            there |= (uint32_t)ok << t;
-            page[t] = ok ? p : 0;
+    // Tiles in batches of 16, whose page ids the lanes hold: lane 4 i + t has subtile t of tile i, -1 for a page that is not there.  Of a
+    // batch first those that some row does not see whole, then the others, with the next one's loads in flight.
+    const int32_t* table = a.block_table + (int64_t)s * a.max_pages;
+    const HeadArrays arrays(a.cache, head);
+    for (; tile < tile_end; tile += 16) {
+        int32_t ids = -1;
+        {
+            const int32_t t = tile + (lane >> 2), token = t * kKvTile + 16 * (lane & 3);
+            if (t < tile_end && token < r.keys) ids = table[token >> shift];
+            ids = ids < a.num_pages ? ids : -1;
         }
-        return there;
-    };
-    float (*sigma)[64] = sigmas[kMbs ? wave : 0];
-    TileRegs<D, kMbs> now;
-    for (; tile < tile_end; tile += kWavesInGroup) {
-        const uint32_t there = pages(tile);
-        const int32_t token0 = tile * kKvTile;
-        load_tile<D, kMbs>(now, a, page, token0, head);
-        const bool whole = token0 >= lo_each && token0 + kKvTile <= hi_each && there == 15u;
-        if (whole) take_tile<D, kTiles, kMbs, false>(st, now, q, sigma, a.scale2, token0, lo, hi, lo_all, hi_all, there);
-        else take_tile<D, kTiles, kMbs, true>(st, now, q, sigma, a.scale2, token0, lo, hi, lo_all, hi_all, there);
+        uint32_t there = 0, whole = 0;  // of each tile the first subtile's lane says whether all are there
+        {
+            const uint64_t have = __builtin_amdgcn_ballot_w64(ids >= 0);
+            const int32_t t = tile + lane, token = t * kKvTile;
+            const bool all = lane < 16 && t < tile_end && token >= lo_each && token + kKvTile <= hi_each && (have >> (4 * (lane & 15)) & 15) == 15;
+            whole = (uint32_t)__builtin_amdgcn_ballot_w64(all);
+            there = (uint32_t)__builtin_amdgcn_ballot_w64(lane < 16 && t < tile_end) & ~whole;  // the others
+            for (; there; there &= there - 1) {
+                const int i = __builtin_ctz(there);
+                TileRegs<D, kMbs> regs;
+                fetch_tile(regs, arrays, off, shift, ids, i, tile);
+                take_tile<D, kTiles, kMbs, true>(st, regs, q, sigma, a.scale2, (tile + i) * kKvTile, lo, hi, lo_all, hi_all, (uint32_t)(have >> (4 * i)) & 15u);
+            }
+        }
+        if constexpr (kTiles > 1 || (D != 64 && D != 128)) {  // (two tiles of codes do not fit the registers beside the rest)
+            for (; whole; whole &= whole - 1) {
+                TileRegs<D, kMbs> regs;
+                fetch_tile(regs, arrays, off, shift, ids, __builtin_ctz(whole), tile);
+                take_tile<D, kTiles, kMbs, false>(st, regs, q, sigma, a.scale2, 0, lo, hi, lo_all, hi_all, 15u);
+            }
+        } else if (whole) {
+            // (the last tile is loaded twice: a load that may be left out would make every wait one for all loads)
+            TileRegs<D, kMbs> even, odd;
+            int i = __builtin_ctz(whole);
+            fetch_tile(even, arrays, off, shift, ids, i, tile);
+            while (true) {
+                whole &= whole - 1;
+                i = whole ? __builtin_ctz(whole) : i;
+                fetch_tile(odd, arrays, off, shift, ids, i, tile);
+                take_tile<D, kTiles, kMbs, false>(st, even, q, sigma, a.scale2, 0, lo, hi, lo_all, hi_all, 15u);
+                if (!whole) break;
+                whole &= whole - 1;
+                i = whole ? __builtin_ctz(whole) : i;
+                fetch_tile(even, arrays, off, shift, ids, i, tile);
+                take_tile<D, kTiles, kMbs, false>(st, odd, q, sigma, a.scale2, 0, lo, hi, lo_all, hi_all, 15u);
+                if (!whole) break;
+            }
+        }
     }
 
-    // join the wavefronts, 16 rows and 128 of D at a time
-    const bool direct = piece.count == 1;
-    float* slot = a.partial + (int64_t)blockIdx.x * kPieceFloats<D, kTiles>;
+    float* slot = a.partial + (int64_t)KvLine::place(item_at, line_begin, worker) * kPartFloats<D, kTiles>;
 #pragma unroll
     for (int b = 0; b < kTiles; ++b) {
         const float l = column_sum(st.l[b]);
-        __syncthreads();
-        if (g == 0) { stats[wave][0][n] = st.m[b]; stats[wave][1][n] = l; }
-        __syncthreads();
-        float m = stats[0][0][n];
+        const int32_t row = row0 + 16 * b + n;
+        if (row >= rows) continue;
+        if (direct) {
+            const int32_t i = row / a.group;
+            const int64_t t = r.first + i;
+            const int h = head * a.group + (row - i * a.group);
+            const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+            if (a.lse && g == 0) a.lse[t * a.Hq + h] = l == 0.0f ? -__builtin_inff() : (st.m[b] + __builtin_log2f(l)) * kLn2;
+            uint16_t* o = a.out + t * a.ldo + (int64_t)h * D;
+            each_run<D>(st.o[b], g, [&](int d, auto wide, const float* x) __attribute__((always_inline)) {
+                uint32_t w[4];
 #pragma unroll
-        for (int w = 1; w < kWavesInGroup; ++w) m = fmaxf(m, stats[w][0][n]);
-        const float shrink = __builtin_amdgcn_exp2f(st.m[b] - m);
-        // a thread: row rn, and the columns that one (lane group, register) of each part holds
-        const int rn = threadIdx.x & 15, rest = threadIdx.x >> 4, rg = rest >> 2, ri = rest & 3;
-        const int32_t row = row0 + 16 * b + rn, i = row / a.group;
-        const int64_t t = r.first + i;
-        const int h = head * a.group + (row - i * a.group);
-        float sum_l = 0.0f, top = kLowest;
-#pragma unroll
-        for (int w = 0; w < kWavesInGroup; ++w) top = fmaxf(top, stats[w][0][rn]);
-#pragma unroll
-        for (int w = 0; w < kWavesInGroup; ++w) sum_l += stats[w][1][rn] * __builtin_amdgcn_exp2f(stats[w][0][rn] - top);
-        const float inverse = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
-        if (row < rows && rest == 0) {
-            if (!direct) {
-                slot[16 * b + rn] = top;
-                slot[kHeight + 16 * b + rn] = sum_l;
-            } else if (a.lse) {
-                a.lse[t * a.Hq + h] = sum_l == 0.0f ? -__builtin_inff() : (top + __builtin_log2f(sum_l)) * kLn2;
+                for (int c = 0; c < decltype(wide)::value / 2; ++c) w[c] = pack_bf16(x[2 * c] * inverse, x[2 * c + 1] * inverse);
+                if constexpr (decltype(wide)::value == 8) *reinterpret_cast<u32x4*>(o + d) = u32x4{w[0], w[1], w[2], w[3]};
+                else if constexpr (decltype(wide)::value == 4) *reinterpret_cast<u32x2*>(o + d) = u32x2{w[0], w[1]};
+                else *reinterpret_cast<uint32_t*>(o + d) = w[0];
+            });
+        } else {
+            if (g == 0) {
+                slot[16 * b + n] = st.m[b];
+                slot[kHeight + 16 * b + n] = l;
             }
+            float* o = slot + 2 * kHeight + (16 * b + n) * D;
+            each_run<D>(st.o[b], g, [&](int d, auto wide, const float* x) __attribute__((always_inline)) {
+                constexpr int kWide = decltype(wide)::value;
+                if constexpr (kWide == 2) *reinterpret_cast<f32x2*>(o + d) = f32x2{x[0], x[1]};
+                else
+#pragma unroll
+                    for (int c = 0; c < kWide; c += 4) *reinterpret_cast<f32x4*>(o + d + c) = f32x4{x[c], x[c + 1], x[c + 2], x[c + 3]};
+            });
         }
-        int column = 0;
-#pragma unroll
-        for (int p = 0; p < H::parts; ++p) {
-            const int wide = H::width(p) / 16;
-            if (p) __syncthreads();
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-                if (c < wide) joined[wave][c][lane] = st.o[b][column + c] * shrink;
-            column += wide;
-            __syncthreads();
-            if (row < rows) {
-                float x[8] = {};
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    if (c >= wide) break;
-#pragma unroll
-                    for (int w = 0; w < kWavesInGroup; ++w) x[c] += joined[w][c][rg * 16 + rn][ri];
-                }
-                const int d = H::start(p) + wide * (4 * rg + ri);
-                if (direct) {
-                    uint16_t* o = a.out + t * a.ldo + (int64_t)h * D + d;
-#pragma unroll
-                    for (int c = 0; c < 8; c += 2)
-                        if (c < wide) *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(x[c] * inverse, x[c + 1] * inverse);
-                } else {
-                    float* o = slot + 2 * kHeight + (16 * b + rn) * D + d;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        if (c < wide) o[c] = x[c];
-                }
-            }
-        }
+    }
     }
 }
 
-// Rows that were cut into pieces: a wavefront a row.
-template <int D, int kTiles>
+// Rows that were cut into pieces, kWaves wavefronts a row: lanes have 4 columns each and the parts are dealt to the groups of lanes.
+template <int D, int kTiles, int kWaves>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionArgs a) {
-    constexpr int kHeight = 16 * kTiles, kQuads = D / 4, kSides = 64 / kQuads > 0 ? 64 / kQuads : 1;
-    static_assert(kQuads <= 64, "a row in one wavefront");
-    const int lane = threadIdx.x & 63;
-    const int64_t id = __builtin_amdgcn_readfirstlane(blockIdx.x * kWavesInGroup + (threadIdx.x >> 6));
-    const int32_t t = (int32_t)(id / a.Hq);
+    constexpr int kHeight = 16 * kTiles, kQuads = D / 4, kSides = 64 / kQuads, kDeal = kSides * kWaves;
+    __shared__ f32x4 sums[kWaves > 1 ? kWaves : 1][kQuads];
+    __shared__ float weights[kWaves > 1 ? kWaves : 1];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), part_of_row = kWaves > 1 ? wave : 0;
+    const int64_t id = kWaves > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kWavesInGroup + wave;
+    const int32_t t = uniform((int32_t)((uint32_t)id / (uint32_t)a.Hq));
     const int h = (int)(id - (int64_t)t * a.Hq);
     if (t >= a.T) return;
-    const Piece p = locate(a, kHeight, 0, t);
-    if (!p.found || p.count == 1) return;
-    const KvRequest r = request_of(a, p.s);
-    const int heads = a.cache.at.heads, head = h / a.group;
-    const int32_t row = (t - r.first) * a.group + (h - head * a.group);
-    const int32_t row_tile = row / kHeight, at = row - row_tile * kHeight, row_tiles = r.row_tiles(a.group, kHeight);
-    // piece i of the row tile: unit base + i * row_tiles + row_tile
-    const int64_t at0 = (p.base + row_tile) * heads + head;
-    // (offsets that overlap make more units than the grid and the workspace have room for)
-    if (at0 + (int64_t)(p.count - 1) * row_tiles * heads >= a.slots) return;
-    const float* slot = a.partial + at0 * kPieceFloats<D, kTiles>;
-    const int64_t step = (int64_t)row_tiles * heads * kPieceFloats<D, kTiles>;
+    Batch batch(a, kHeight);
+    const int who = batch.find([&] { return t >= batch.r.first && t < batch.r.first + batch.r.rows; });
+    if (who < 0) return;
+    const KvRequest r = batch.request(who);
+    const int32_t item = KvLine::item(read_lane(batch.tiles, who)), row_tiles = read_lane(batch.row_tiles, who), head = h / a.group;
+    const int32_t row = (t - r.first) * a.group + (h - head * a.group), row_tile = row / kHeight, at = row - row_tile * kHeight;
+    const int64_t item_at = read_lane(batch.end, who) - read_lane(batch.size, who) + (int64_t)(head * row_tiles + row_tile) * item;
+    const KvLine::Parts parts = KvLine::parts(item_at, item, batch.share);
+    const int32_t count = parts.count;
+    if (count == 1) return;
+    auto part = [&](int32_t i) __attribute__((always_inline)) {
+        return a.partial + (int64_t)(2 * (parts.first + i) + (i == 0 ? parts.late : 0)) * kPartFloats<D, kTiles>;
+    };
     float m = kLowest;
-    for (int i = lane; i < p.count; i += 64) m = fmaxf(m, slot[i * step + at]);
+    for (int i = lane; i < count; i += 64) m = fmaxf(m, part(i)[at]);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
     float l = 0.0f;
     f32x4 o = {0, 0, 0, 0};
-    const int side = lane / kQuads, d = (lane - side * kQuads) * 4;
+    const int side = lane / kQuads, quad = lane - side * kQuads;
     if (side < kSides) {
-#pragma unroll 4
-        for (int i = side; i < p.count; i += kSides) {
-            const float* s = slot + i * step;
+#pragma unroll 8
+        for (int i = part_of_row * kSides + side; i < count; i += kDeal) {
+            const float* s = part(i);
             const float w = __builtin_amdgcn_exp2f(s[at] - m);
             l += w * s[kHeight + at];
-            o += w * *reinterpret_cast<const f32x4*>(s + 2 * kHeight + at * D + d);
+            o += w * *reinterpret_cast<const f32x4*>(s + 2 * kHeight + at * D + 4 * quad);
         }
     }
+    const float own_l = l;
+    const f32x4 own = o;
 #pragma unroll
-    for (int x = 1; x < kSides; ++x) {
+    for (int x = 1; x < kSides; ++x) {  // (only the first side's sums are used)
         const int from = (lane + x * kQuads) & 63;
-        const float l1 = __shfl(l, from);
-        f32x4 o1;
+        l += __shfl(own_l, from);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o1[c] = __shfl(o[c], from);
-        // (lane sets are added in the order of the pieces' remainders, only side 0 is used)
-        if (side == 0) { l += l1; o += o1; }
+        for (int c = 0; c < 4; ++c) o[c] += __shfl(own[c], from);
+    }
+    if constexpr (kWaves > 1) {
+        if (side == 0) sums[wave][quad] = o;
+        if (lane == 0) weights[wave] = l;
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+            if (side == 0) o += sums[w][quad];
+            l += weights[w];
+        }
     }
     if (side == 0) {
         const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
-        u32x2 w = {pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse)};
-        *reinterpret_cast<u32x2*>(a.out + (int64_t)t * a.ldo + (int64_t)h * D + d) = w;
+        *reinterpret_cast<u32x2*>(a.out + (int64_t)t * a.ldo + (int64_t)h * D + 4 * quad) =
+            u32x2{pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse)};
         if (a.lse && lane == 0) a.lse[(int64_t)t * a.Hq + h] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
     }
 }
 
-constexpr int32_t kTarget = 1024;
+// Two row tiles where most requests bring more than one tile's rows.  (Heads above 128 keep to one: two do not fit the registers.)
+int row_tiles_of(int64_t S, int64_t T, int64_t group, int64_t D) { return T * group > 24 * S && D <= 128 ? 2 : 1; }
 
-int row_tiles_of(int64_t S, int64_t T, int64_t group) { return T * group > 24 * S ? 2 : 1; }
-
-int64_t units_of(int64_t S, int64_t T, int64_t group, int height) { return S + (T * group + height - 1) / height; }
+template <int D, int kTiles>
+int64_t workspace_of() { return ((int64_t)2 << kWorkersLog2<D, kTiles>) * kPartFloats<D, kTiles> * 4; }
 
 template <int D, int kTiles>
 int launch_tiles(const AttentionArgs& args, hipStream_t s) {
-    const int64_t heads = args.cache.at.heads;
-    const int64_t groups = kTarget + units_of(args.S, args.T, args.group, 16 * kTiles) * heads;
-    if (groups >= (int64_t)1 << 24 || (int64_t)args.T * args.Hq >= (int64_t)1 << 26) return MX_EINVAL;
-    const dim3 grid((unsigned)groups);
     AttentionArgs a = args;
-    a.slots = groups;
+    a.workers_log2 = kWorkersLog2<D, kTiles>;
+    const dim3 grid((1 << a.workers_log2) / kWavesInGroup);
     if (a.cache.k_mbs) hipLaunchKernelGGL((attention_rows_kernel<D, kTiles, true>), grid, dim3(kThreads), 0, s, a);
     else hipLaunchKernelGGL((attention_rows_kernel<D, kTiles, false>), grid, dim3(kThreads), 0, s, a);
     if (int st = launch_status()) return st;
-    if (a.room > kLeastShare * kKvTile) {
-        const int64_t waves = (int64_t)a.T * a.Hq;
-        hipLaunchKernelGGL((attention_join_kernel<D, kTiles>), dim3((unsigned)((waves + kWavesInGroup - 1) / kWavesInGroup)), dim3(kThreads), 0, s, a);
-    }
+    // few rows are cut into many parts (of 2048 workers' shares), many rows into few
+    const int64_t rows = (int64_t)a.T * a.Hq;
+    if (rows <= 1024) hipLaunchKernelGGL((attention_join_kernel<D, kTiles, kWavesInGroup>), dim3((unsigned)rows), dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((attention_join_kernel<D, kTiles, 1>), dim3((unsigned)((rows + kWavesInGroup - 1) / kWavesInGroup)), dim3(kThreads), 0, s, a);
     return launch_status();
 }
-template <int D>
-int launch_dim(const AttentionArgs& a, hipStream_t s) {
-    return row_tiles_of(a.S, a.T, a.group) == 2 ? launch_tiles<D, 2>(a, s) : launch_tiles<D, 1>(a, s);
+template <int D, typename F>
+auto with_tiles(int64_t S, int64_t T, int64_t group, F&& f) {
+    if constexpr (D <= 128)
+        if (row_tiles_of(S, T, group, D) == 2) return f(std::integral_constant<int, D>{}, std::integral_constant<int, 2>{});
+    return f(std::integral_constant<int, D>{}, std::integral_constant<int, 1>{});
+}
+template <typename F>
+auto with_shape(int64_t S, int64_t T, int64_t group, int64_t D, F&& f) {
+    switch (D) {
+        case 64: return with_tiles<64>(S, T, group, f);
+        case 96: return with_tiles<96>(S, T, group, f);
+        case 128: return with_tiles<128>(S, T, group, f);
+        case 192: return with_tiles<192>(S, T, group, f);
+        default: return with_tiles<256>(S, T, group, f);
+    }
 }
 
 }  // namespace
 
 int64_t attention_rows_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
-    const int64_t group = Hq / Hkv, tiles = row_tiles_of(S, T, group);
-    return (kTarget + units_of(S, T, group, 16 * (int)tiles) * Hkv) * 16 * tiles * (D + 2) * 4;
+    return with_shape(S, T, Hq / Hkv, D, [](auto d, auto tiles) { return workspace_of<decltype(d)::value, decltype(tiles)::value>(); });
 }
 
-int launch_attention_rows(const AttentionArgs& args, hipStream_t stream) {
-    AttentionArgs a = args;
-    a.target = kTarget;
-    switch (a.cache.at.D) {
-        case 64: return launch_dim<64>(a, stream);
-        case 96: return launch_dim<96>(a, stream);
-        case 128: return launch_dim<128>(a, stream);
-        case 192: return launch_dim<192>(a, stream);
-        case 256: return launch_dim<256>(a, stream);
-        default: return MX_EUNSUPPORTED;
-    }
+int launch_attention_rows(const AttentionArgs& a, hipStream_t stream) {
+    if ((int64_t)a.T * a.Hq >= (int64_t)1 << 26) return MX_EINVAL;  // (a launch of fewer than 2^32 work-items)
+    return with_shape(a.S, a.T, a.group, a.cache.at.D,
+                      [&](auto d, auto tiles) { return launch_tiles<decltype(d)::value, decltype(tiles)::value>(a, stream); });
 }
 
 }  // namespace mx

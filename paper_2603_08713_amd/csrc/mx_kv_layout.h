@@ -81,12 +81,40 @@ struct KvRequest {
     MX_HD int32_t row_tiles(int32_t group, int32_t height) const { return (int32_t)(((int64_t)rows * group + height - 1) / height); }
 };
 
-// Pieces of a request along its keys, `share` tiles each; one at least, so that rows without keys are written too.
-MX_HD int32_t kv_pieces(int32_t tiles, int32_t share) { return tiles <= share ? 1 : (tiles + share - 1) / share; }
-// The share that cuts `total` tiles (of all requests, heads and row tiles) into about `target` pieces.
-MX_HD int32_t kv_share(int64_t total, int32_t target, int32_t least) {
-    const int64_t s = (total + target - 1) / target;
-    return s < least ? least : kv_clamp(s, 1, kKvMostKeys / kKvTile);
-}
+// The work of a batch in one line: request after request, of each its items (key heads x row tiles), of each a fixed length that stands for
+// what an item costs besides (and lets rows without keys be written too) and then its tiles of keys.  A worker takes `share` of that
+// line, from share * its number on; an item that it does not take whole leaves a partial result, of which a worker has two places:
+// one for the item that it begins with, one for an item that it only begins.
+struct KvLine {
+    static constexpr int32_t kItemCost = 2;  // in tiles
+    // length of an item, and how many of its tiles lie before a place in it
+    MX_HD static int32_t item(int32_t tiles) { return tiles + kItemCost; }
+    MX_HD static int32_t tiles_before(int32_t place) { return kv_max(place - kItemCost, 0); }
+    // length of a request
+    MX_HD static int64_t request(int32_t tiles, int32_t row_tiles, int32_t heads) { return (int64_t)item(tiles) * row_tiles * heads; }
+    MX_HD static int32_t share(int64_t total, int32_t workers_log2, int32_t least) {
+        return kv_clamp((total + ((int64_t)1 << workers_log2) - 1) >> workers_log2, least, INT32_MAX);
+    }
+    // for the worker whose share is [begin, end): whether it takes all of the item at [at, at + item), and where its part of it goes if not
+    MX_HD static bool whole(int64_t at, int32_t item, int64_t begin, int64_t end) { return at >= begin && at + item <= end; }
+    MX_HD static int32_t place(int64_t at, int64_t begin, int32_t worker) { return 2 * worker + (at > begin); }
+    // the same from the item's side: its parts are those of the workers first, first + 1, .. (count of them; 1: it is whole), the part of
+    // the first in place 2 first + late, of another w in place 2 w
+    struct Parts {
+        int32_t first, count, late;
+    };
+    MX_HD static Parts parts(int64_t at, int32_t item, int32_t share) {
+        Parts p;
+        if ((at + item) >> 32) {  // (a division of 64 bits is some hundred instructions)
+            p.first = (int32_t)(at / share);
+            p.count = (int32_t)((at + item - 1) / share) - p.first + 1;
+        } else {
+            p.first = (int32_t)((uint32_t)at / (uint32_t)share);
+            p.count = (int32_t)((uint32_t)(at + item - 1) / (uint32_t)share) - p.first + 1;
+        }
+        p.late = at > (int64_t)p.first * share;
+        return p;
+    }
+};
 
 }  // namespace mx

@@ -290,7 +290,7 @@ int check_turn(const RowsArgs& a, mx_rope_t style, int64_t T, int64_t Hq, int64_
 int KvArrays::check(int64_t num_pages, int64_t page_size, int64_t Hkv, int64_t D) const {
     if (num_pages < 0 || Hkv <= 0 || Hkv > kKvMostHeads || page_size <= 0) return MX_EINVAL;
     if (!kv_head_dim(D) || page_size < 16 || page_size > 4096 || (page_size & (page_size - 1)) != 0) return MX_EUNSUPPORTED;
-    if (num_pages > ((int64_t)1 << 40) / (Hkv * page_size)) return MX_EINVAL;
+    if (num_pages > ((int64_t)1 << 40) / (Hkv * page_size) || Hkv * page_size * D >= (int64_t)1 << 32) return MX_EINVAL;  // (a page is below 2 GiB)
     if (!!k_mbs != !!v_mbs) return MX_EINVAL;
     if (num_pages == 0) return MX_OK;
     if (!k_codes || !k_scales || !v_codes || !v_scales) return MX_ENULL;

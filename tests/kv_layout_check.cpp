@@ -72,30 +72,47 @@ static void request(int64_t begin, int64_t end, int64_t len, int32_t T, int32_t 
 static void batch(std::mt19937& rng) {
     auto pick = [&](int lo, int hi) { return lo + (int)(rng() % (unsigned)(hi - lo + 1)); };
     const int S = pick(1, 40), group = pick(1, 9), heads = pick(1, 8), height = 16 * pick(1, 8), window = pick(0, 1) * pick(1, 3000), least = pick(1, 8);
-    const int target = pick(1, 1) * 1024;
-    std::vector<int64_t> offsets = {0};
-    std::vector<int> lens;
+    const int log2 = pick(0, 11), workers = 1 << log2;
+    const int64_t far = log2 < 6 || pick(0, 3) ? 0 : (int64_t)pick(1, 9) << 31;  // (positions beyond 32 bits are reached with one long request in front)
+    int64_t begin = 0, total = far;
+    struct Item { int64_t at; int32_t tiles; };
+    std::vector<Item> items;
     for (int s = 0; s < S; ++s) {
-        offsets.push_back(offsets.back() + pick(0, pick(0, 1) ? 1 : 200));
-        lens.push_back(pick(0, pick(0, 1) ? 20 : 40000));
+        const int n = pick(0, pick(0, 1) ? 1 : 200), len = pick(0, pick(0, 1) ? 20 : 40000);
+        const KvRequest r = KvRequest::make(begin, begin + n, len, 1 << 20, 1 << 20);
+        begin += n;
+        const int32_t tiles = r.tiles(window, 1), row_tiles = r.row_tiles(group, height);
+        CHECK((int64_t)row_tiles * height >= (int64_t)r.rows * group && (int64_t)(row_tiles - 1) * height < (int64_t)r.rows * group, "row tiles");
+        for (int i = 0; i < row_tiles * heads; ++i) items.push_back({total + (int64_t)i * KvLine::item(tiles), KvLine::item(tiles)});
+        total += KvLine::request(tiles, row_tiles, heads);
     }
-    const int32_t T = (int32_t)offsets.back();
-    int64_t total = 0, row_tiles = 0;
-    std::vector<KvRequest> r;
-    for (int s = 0; s < S; ++s) {
-        r.push_back(KvRequest::make(offsets[s], offsets[s + 1], lens[s], T, 1 << 20));
-        total += (int64_t)r[s].row_tiles(group, height) * r[s].tiles(window, 1);
-        row_tiles += r[s].row_tiles(group, height);
+    const int32_t share = KvLine::share(total, log2, least);
+    CHECK((int64_t)share * workers >= total && share >= least, "the groups take all");
+    std::vector<int> used(2 * workers), taken(items.size());
+    size_t item = 0;
+    for (int w = 0; w < workers; ++w) {  // as the workers go along the line
+        const int64_t first = (int64_t)share * w, end = std::min(total, first + share);
+        for (int64_t at = std::max(far, std::min(total, first)); at < end;) {
+            while (item < items.size() && items[item].at + items[item].tiles <= at) ++item;
+            const Item& x = items[item];
+            const int64_t stop = std::min(end, x.at + x.tiles);
+            const KvLine::Parts parts = KvLine::parts(x.at, x.tiles, share);
+            CHECK(at == std::max(x.at, first) && w >= parts.first && w < parts.first + parts.count, "worker %d of %d + %d", w, parts.first, parts.count);
+            const bool whole = KvLine::whole(x.at, x.tiles, first, first + share);
+            CHECK(whole == (parts.count == 1) && whole == (at == x.at && stop == x.at + x.tiles), "whole or not");
+            if (!whole) {
+                const int32_t place = KvLine::place(x.at, first, w);
+                CHECK(place == 2 * w + (w == parts.first ? parts.late : 0), "place %d", place);
+                CHECK(place >= 0 && place < 2 * workers, "place %d", place);
+                if (place >= 0 && place < 2 * workers) CHECK(++used[place] == 1, "place %d used twice", place);
+            }
+            // the tiles of an item go to its workers in order, none twice
+            CHECK(KvLine::tiles_before((int32_t)(at - x.at)) == taken[item], "tiles");
+            taken[item] = KvLine::tiles_before((int32_t)(stop - x.at));
+            at = stop;
+        }
     }
-    CHECK(row_tiles <= S + ((int64_t)T * group + height - 1) / height, "row tiles");
-    const int32_t share = kv_share(total * heads, target, least);
-    int64_t units = 0;
-    for (int s = 0; s < S; ++s) {
-        const int32_t tiles = r[s].tiles(window, 1), pieces = kv_pieces(tiles, share);
-        CHECK(pieces >= 1 && (int64_t)pieces * share >= tiles && (int64_t)(pieces - 1) * share < (tiles ? tiles : 1), "pieces");
-        units += (int64_t)r[s].row_tiles(group, height) * pieces;
-    }
-    CHECK(units * heads <= target + (S + ((int64_t)T * group + height - 1) / height) * heads, "the grid holds %lld units", (long long)units);
+    for (size_t i = 0; i < items.size(); ++i) CHECK(taken[i] == items[i].tiles - KvLine::kItemCost, "all tiles of item %zu", i);
 }
 
 int main() {

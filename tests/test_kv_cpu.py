@@ -37,8 +37,10 @@ def test_layout_requests_and_pieces(tmp_path):
     ("unit * 16 + (place & 3) * 4", "unit * 16 + (place & 1) * 4"),                                    # two tokens on the same bytes
     ("kv_clamp(end, r.first, T) - r.first", "kv_clamp(end, r.first, T + 1) - r.first"),                # a row behind the tensor
     ("kv_min(pos0 + i, kKvMostKeys) - (window - 1)", "kv_min(pos0 + i, kKvMostKeys) - window"),        # a window of one key more
-    ("(tiles + share - 1) / share", "tiles / share"),                                                  # the last piece is lost
-    ("(total + target - 1) / target", "total / (3 * target)"),                                         # more pieces than the grid holds
+    ("(uint32_t)(at + item - 1) / (uint32_t)share", "(uint32_t)(at + item) / (uint32_t)share"),        # a part too many
+    ("(total + ((int64_t)1 << workers_log2) - 1)", "(total)"),                                         # the last tiles are lost
+    ("2 * worker + (at > begin)", "2 * worker"),                                                       # two results in one place
+    ("if ((at + item) >> 32)", "if ((at + item) >> 40)"),                                              # positions cut off
 ])
 def test_a_planted_mistake_is_found(tmp_path, right, wrong):
     text = open(os.path.join(CSRC, "mx_kv_layout.h")).read()
