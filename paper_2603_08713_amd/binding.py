@@ -109,6 +109,10 @@ def load_library() -> ctypes.CDLL:
     L.mx_attention_kv.restype = ci
     L.mx_attention_kv.argtypes = [vp, i64, vp, ip, ip, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, i64, f, ci, i64, vp, i64, vp,
                                   vp, i64, vp]
+    L.mx_internal_attention_kv.restype = ci
+    L.mx_internal_attention_kv.argtypes = [ci] + L.mx_attention_kv.argtypes
+    L.mx_internal_attention_kv_workspace.restype = i64
+    L.mx_internal_attention_kv_workspace.argtypes = [ci, i64, i64, i64, i64, i64]
     L.mx_attention_kv_workspace.restype = i64
     L.mx_attention_kv_workspace.argtypes = [i64, i64, i64, i64, i64]
     _lib = L
@@ -135,8 +139,8 @@ def forced(**choices):
     """quantize_hw / quantize_elem_hw = 0 or 1 (rounding implementation), gemm_shape = a kernel form and
     tile shape code of mx_gemm.hip, gemm_elem = which kernel takes an 8-/6-bit GEMM (1 = the main kernel's general
     form, 2 = the main kernel in the form the problem allows, 3 = the few-row kernel, 16 / 17 / 18 = the main kernel on 256 x 128 /
-    128 x 128 / 64 x 128 tiles, the last two for K >= 512)."""
-    allowed = {"quantize_hw", "quantize_elem_hw", "gemm_shape", "gemm_elem"}
+    128 x 128 / 64 x 128 tiles, the last two for K >= 512), attention = 1 or 2 (the kernel for few or for many rows)."""
+    allowed = {"quantize_hw", "quantize_elem_hw", "gemm_shape", "gemm_elem", "attention"}
     if set(choices) - allowed:
         raise TypeError("unknown choice: %s" % sorted(set(choices) - allowed))
     old = getattr(_dev, "choices", {})
@@ -826,7 +830,7 @@ def mx_kv_read(slots, k_cache, v_cache, out_dtype="bf16", k_out=None, v_out=None
 
 def mx_attention_kv_workspace(num_seqs, total_tokens, q_heads, kv_heads, head_dim) -> int:
     """Bytes of workspace that mx_attention_kv wants for these sizes, whatever the lengths."""
-    need = (_lib or load_library()).mx_attention_kv_workspace(num_seqs, total_tokens, q_heads, kv_heads, head_dim)
+    need = (_lib or load_library()).mx_internal_attention_kv_workspace(_forced("attention") or 0, num_seqs, total_tokens, q_heads, kv_heads, head_dim)
     _check(min(need, 0), "mx_attention_kv_workspace")
     return need
 
@@ -835,7 +839,7 @@ def mx_attention_kv(q, row_offsets, kv_lens, block_table, k_cache, v_cache, scal
     """Attention of q [T, Hq, D] (bf16; request s has the rows row_offsets[s] .. row_offsets[s+1]-1) over the cache: request s has kv_lens[s]
     keys in the pages block_table[s].  scale: 1 / sqrt(D) if None.  lse: fp32 [T, Hq], filled if given.  workspace: uint8, if the caller keeps
     one (calls that can run at the same time need one each); else it comes from the allocator.  Returns out, bf16 [T, Hq, D]."""
-    if _native is not None and out is not None and _done(
+    if _native is not None and out is not None and not getattr(_dev, "choices", None) and _done(
             _native.attention_kv(q, row_offsets, kv_lens, block_table, *k_cache, *v_cache, q.shape[-1] ** -0.5 if scale is None else scale, causal, window, out,
                                  lse, workspace), "mx_attention_kv"):
         return out
@@ -858,8 +862,11 @@ def mx_attention_kv(q, row_offsets, kv_lens, block_table, k_cache, v_cache, scal
         workspace = torch.empty(mx_attention_kv_workspace(S, T, Hq, heads, D), dtype=torch.uint8, device=q.device)
     else:
         _here(workspace, torch.uint8, "workspace", 1)
-    _check((_lib or load_library()).mx_attention_kv(_ptr(q), ldq, _ptr(row_offsets), _ptr(kv_lens), _ptr(block_table), block_table.shape[1], *pointers,
-                                                    pages, page, S, T, Hq, heads, D, D ** -0.5 if scale is None else scale, int(bool(causal)),
-                                                    int(window), _ptr(out), ldo, _ptr(lse), _ptr(workspace), workspace.numel(), _stream()),
-           "mx_attention_kv")
+    arguments = (_ptr(q), ldq, _ptr(row_offsets), _ptr(kv_lens), _ptr(block_table), block_table.shape[1], *pointers, pages, page, S, T, Hq, heads, D,
+                 D ** -0.5 if scale is None else scale, int(bool(causal)), int(window), _ptr(out), ldo, _ptr(lse), _ptr(workspace), workspace.numel(), _stream())
+    force = _forced("attention")
+    if force:
+        _check((_lib or load_library()).mx_internal_attention_kv(int(force), *arguments), "mx_attention_kv (mx_internal_attention_kv)")
+    else:
+        _check((_lib or load_library()).mx_attention_kv(*arguments), "mx_attention_kv")
     return out

@@ -43,6 +43,10 @@ struct AttentionArgs {
     float scale2;             // scale * log2(e)
 };
 
+// kernel of mx_attention_prompt.hip, and row tiles that its launch makes of a key head
+int launch_attention_prompt(const AttentionArgs& a, hipStream_t stream);
+int64_t prompt_row_tiles(int64_t S, int64_t T, int64_t group, int64_t D);
+
 // kernels of mx_attention_rows.hip
 int launch_attention_rows(const AttentionArgs& a, hipStream_t stream);
 int64_t attention_rows_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
@@ -81,6 +85,35 @@ __device__ __forceinline__ float column_sum(float x) {
 }
 __device__ __forceinline__ float scale_of(uint32_t E) { return __uint_as_float(E << 23); }
 __device__ __forceinline__ float sigma_of(uint32_t m8) { return __builtin_amdgcn_rcpf(__uint_as_float(0x3F800000u | (m8 << 15))); }
+
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int32_t read_lane(int32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ int64_t read_lane(int64_t x, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)read_lane((int32_t)x, lane) | (uint64_t)(uint32_t)read_lane((int32_t)(x >> 32), lane) << 32);
+}
+
+// Sum over the lanes up to each one.  (By DPP: within rows of 16, then over pairs of rows, then halves; the LDS crossbar would take its latency
+// twelve times.)
+template <int kControl, int kRows>
+__device__ __forceinline__ int64_t add_lane(int64_t x) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kControl, kRows, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(x >> 32), kControl, kRows, 0xF, false);
+    return x + (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+    x = add_lane<0x111, 0xF>(x);  // row_shr:1, 2, 4, 8
+    x = add_lane<0x112, 0xF>(x);
+    x = add_lane<0x114, 0xF>(x);
+    x = add_lane<0x118, 0xF>(x);
+    x = add_lane<0x142, 0xA>(x);  // row_bcast:15 into rows 1 and 3
+    return add_lane<0x143, 0xC>(x);  // row_bcast:31 into rows 2 and 3
+}
+// Request s of the batch; without rows or keys at and beyond its end.
+__device__ __forceinline__ KvRequest request_of(const AttentionArgs& a, int s) {
+    KvRequest r = {0, 0, 0, 0};
+    if (s < a.S) r = KvRequest::make(a.row_offsets[s], a.row_offsets[s + 1], a.kv_lens[s], a.T, a.room);
+    return r;
+}
 
 // How a head of D elements is taken: 128 at a time, then 64, then 32.  Of 128, lane group g has block g of a key, and lane n of 16
 // has 8 neighbouring columns of V; of 64, half a block and 4 columns; of 32, 8 elements and 2 columns.

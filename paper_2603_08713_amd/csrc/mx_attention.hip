@@ -1,5 +1,6 @@
 // Argument checks and dispatch of the attention over the paged MXFP4 cache.
 #include "mx_attention.h"
+#include "mx_internal.h"
 
 namespace mx {
 namespace {
@@ -8,28 +9,25 @@ bool good_shape(int64_t S, int64_t T, int64_t Hq, int64_t Hkv) {
     return S >= 0 && T >= 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && S <= kKvMost && T <= kKvMost && Hq <= kKvMostHeads;
 }
 
+// Many rows a key head: tiles of 256 rows that share a tile of expanded keys, as far as they fill the device.
+bool is_prompt(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    const int64_t group = Hq / Hkv;
+    return T * group > 64 * S && prompt_row_tiles(0, T, group, D) * Hkv >= 128;
+}
+
 }  // namespace
 }  // namespace mx
 
-extern "C" int64_t mx_attention_kv_workspace(int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
-    using namespace mx;
-    if (!good_shape(num_seqs, T, Hq, Hkv)) return MX_EINVAL;
-    if (!kv_head_dim(D)) return MX_EUNSUPPORTED;
-    return num_seqs && T ? attention_rows_workspace(num_seqs, T, Hq, Hkv, D) : 0;
-}
+namespace mx {
+namespace {
 
-extern "C" int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,
-                               int64_t max_pages, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* k_mbs_or_null,
-                               const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs_or_null, int64_t num_pages,
-                               int64_t page_size, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, float scale, int causal,
-                               int64_t window, void* out_bf16, int64_t ldo, float* lse_or_null, void* workspace, int64_t workspace_bytes,
-                               void* stream) {
-    using namespace mx;
-    AttentionArgs a = {};
-    a.cache = {const_cast<uint8_t*>(k_codes), const_cast<uint8_t*>(k_scales), const_cast<uint8_t*>(k_mbs_or_null),
-               const_cast<uint8_t*>(v_codes), const_cast<uint8_t*>(v_scales), const_cast<uint8_t*>(v_mbs_or_null), {}};
-    if (!good_shape(num_seqs, T, Hq, Hkv) || max_pages < 0 || window < 0 || (window && !causal)) return MX_EINVAL;
-    if (int st = a.cache.check(num_pages, page_size, Hkv, D)) return st;
+// force: 0 = the kernel that is_prompt picks, 1 = the one for few rows, 2 = the one for many
+int attention(int force, const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,
+              int64_t max_pages, const KvArrays& cache, int64_t num_pages, int64_t page_size, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv,
+              int64_t D, float scale, int causal, int64_t window, void* out_bf16, int64_t ldo, float* lse_or_null, void* workspace,
+              int64_t workspace_bytes, void* stream) {
+    if (!good_shape(num_seqs, T, Hq, Hkv) || max_pages < 0 || window < 0 || (window && !causal) || force < 0 || force > 2) return MX_EINVAL;
+    if (int st = cache.check(num_pages, page_size, Hkv, D)) return st;
     if (num_pages > INT32_MAX || max_pages > kKvMostKeys / page_size) return MX_EINVAL;
     if (num_seqs == 0 || T == 0) return MX_OK;
     if (ldq < Hq * D || ldo < Hq * D) return MX_EINVAL;
@@ -37,14 +35,17 @@ extern "C" int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* r
     if (!aligned(q_bf16, 16) || ldq % 8 || !aligned(out_bf16, 16) || ldo % 8 || !aligned(row_offsets, 8) || !aligned(kv_lens, 4) ||
         !aligned(block_table, 4) || !aligned(lse_or_null, 4) || !aligned(workspace, 16))
         return MX_EALIGN;
-    const int64_t need = attention_rows_workspace(num_seqs, T, Hq, Hkv, D);
+    const bool prompt = force ? force == 2 : is_prompt(num_seqs, T, Hq, Hkv, D);
+    const int64_t need = prompt ? 0 : attention_rows_workspace(num_seqs, T, Hq, Hkv, D);
     if (workspace_bytes < need) return MX_EINVAL;
     if (need && !workspace) return MX_ENULL;
     if (int st = check_device()) return st;
+    AttentionArgs a = {};
     a.q = static_cast<const uint16_t*>(q_bf16);
     a.row_offsets = row_offsets;
     a.kv_lens = kv_lens;
     a.block_table = block_table;
+    a.cache = cache;
     a.cache.shape(page_size, Hkv, D);
     a.out = static_cast<uint16_t*>(out_bf16);
     a.lse = lse_or_null;
@@ -61,5 +62,48 @@ extern "C" int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* r
     a.window = (int32_t)(window < kKvMostKeys ? window : kKvMostKeys);
     a.causal = causal != 0;
     a.scale2 = scale * 1.4426950408889634f;
-    return launch_attention_rows(a, static_cast<hipStream_t>(stream));
+    return prompt ? launch_attention_prompt(a, static_cast<hipStream_t>(stream)) : launch_attention_rows(a, static_cast<hipStream_t>(stream));
+}
+
+KvArrays arrays(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* k_mbs, const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs) {
+    return {const_cast<uint8_t*>(k_codes), const_cast<uint8_t*>(k_scales), const_cast<uint8_t*>(k_mbs),
+            const_cast<uint8_t*>(v_codes), const_cast<uint8_t*>(v_scales), const_cast<uint8_t*>(v_mbs), {}};
+}
+
+}  // namespace
+}  // namespace mx
+
+extern "C" int64_t mx_attention_kv_workspace(int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    using namespace mx;
+    if (!good_shape(num_seqs, T, Hq, Hkv)) return MX_EINVAL;
+    if (!kv_head_dim(D)) return MX_EUNSUPPORTED;
+    return num_seqs && T && !is_prompt(num_seqs, T, Hq, Hkv, D) ? attention_rows_workspace(num_seqs, T, Hq, Hkv, D) : 0;
+}
+
+extern "C" int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,
+                               int64_t max_pages, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* k_mbs_or_null,
+                               const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs_or_null, int64_t num_pages,
+                               int64_t page_size, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, float scale, int causal,
+                               int64_t window, void* out_bf16, int64_t ldo, float* lse_or_null, void* workspace, int64_t workspace_bytes,
+                               void* stream) {
+    return mx::attention(0, q_bf16, ldq, row_offsets, kv_lens, block_table, max_pages,
+                         mx::arrays(k_codes, k_scales, k_mbs_or_null, v_codes, v_scales, v_mbs_or_null), num_pages, page_size, num_seqs, T, Hq, Hkv, D,
+                         scale, causal, window, out_bf16, ldo, lse_or_null, workspace, workspace_bytes, stream);
+}
+
+extern "C" int mx_internal_attention_kv(int force, const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens,
+                                        const int32_t* block_table, int64_t max_pages, const uint8_t* k_codes, const uint8_t* k_scales,
+                                        const uint8_t* k_mbs_or_null, const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs_or_null,
+                                        int64_t num_pages, int64_t page_size, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D,
+                                        float scale, int causal, int64_t window, void* out_bf16, int64_t ldo, float* lse_or_null, void* workspace,
+                                        int64_t workspace_bytes, void* stream) {
+    return mx::attention(force, q_bf16, ldq, row_offsets, kv_lens, block_table, max_pages,
+                         mx::arrays(k_codes, k_scales, k_mbs_or_null, v_codes, v_scales, v_mbs_or_null), num_pages, page_size, num_seqs, T, Hq, Hkv, D,
+                         scale, causal, window, out_bf16, ldo, lse_or_null, workspace, workspace_bytes, stream);
+}
+
+extern "C" int64_t mx_internal_attention_kv_workspace(int force, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    using namespace mx;
+    const int64_t size = mx_attention_kv_workspace(num_seqs, T, Hq, Hkv, D);
+    return size < 0 || !num_seqs || !T || force == 0 ? size : force == 1 ? attention_rows_workspace(num_seqs, T, Hq, Hkv, D) : 0;
 }

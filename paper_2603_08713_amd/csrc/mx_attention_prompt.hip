@@ -1,0 +1,413 @@
+// Attention over the paged MXFP4 cache for many query rows per key head: prompts and chunks of prompts.
+//
+// A workgroup takes 32 rows for each of its wavefronts - (token, query head of the key head) - and goes through the keys that any of
+// them sees, 64 at a time.  The codes of a tile are expanded once for the workgroup: each wavefront turns its part of K or V into operands of
+// the matrix instruction (32 x 32 x 16, transposed as in mx_attention.h) and writes them to LDS in the order in which a lane reads
+// them, 16 bytes a lane, so that reads meet no conflicts and K and V need no further shuffling.  Two tiles in LDS: while one is multiplied the
+// next is expanded from codes that were loaded a tile earlier; one barrier a tile.
+//
+// Per tile a wavefront issues D/4 matrix instructions (32 clocks each), reads the tile from LDS (D/4 KiB; a compute unit's wavefronts
+// together as long as their matrix instructions take) and does 9 vector operations for each of 32 scores a lane: the three run beside each
+// other in the two wavefronts of a SIMD.
+//
+// Lane l has query row l mod 32 and, of 32 keys, those with bit 2 = l / 32: a row's maximum and sum need one exchange.  V's columns are dealt to
+// the 32 rows of an operand so that a lane ends with runs of neighbouring columns of its row.
+#include "mx_attention.h"
+#include "mx_gemm_shared.h"
+
+namespace mx {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// What the workgroup has written to LDS is there for all of it (loads into registers stay in flight).
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <int D>
+struct PromptShape {
+    static constexpr int waves = D <= 128 ? 8 : 4;  // (two wavefronts a SIMD as far as the registers go)
+    static constexpr int threads = waves * kWave, rows = waves * 32;
+    static constexpr int steps = D / 16;      // products along D for 32 keys
+    static constexpr int columns = D / 32;    // products for 32 columns each
+    static constexpr int words = (D + 127) / 128;
+    static constexpr int units = D / 8;       // units of V: 8 codes of 4 tokens
+    static constexpr int parts = D / 16;      // of a tile's codes, one wavefront's load each: the blocks of K, then V in pieces of 64 units
+    static constexpr int turns = (parts + waves - 1) / waves;
+    // columns: operand t, row r <-> column 128 (t / 4) + f r + t mod 4, f = how many operands the 128 columns have
+    static constexpr int run(int t) { return D / 32 - t / 4 * 4 < 4 ? D / 32 - t / 4 * 4 : 4; }
+};
+
+template <int D, bool kMbs>
+struct PromptLds {  // of one tile
+    u32x4 k[D / 8][kWave], v[D / 8][kWave];
+    float ks[(D + 127) / 128][kKvTile], vs[(D + 127) / 128][kKvTile];  // scale2 / F of a key, 1 / F of a value
+    uint32_t bad[kKvTile];                                            // blocks of a value that are NaN
+    uint32_t any_bad, there;                                          // whether any is; subtiles whose page exists
+};
+
+// One wavefront's share of a tile's codes, in flight.
+template <int D, bool kMbs>
+struct PromptCodes {
+    using P = PromptShape<D>;
+    u32x4 codes[P::turns];
+    uint32_t scales[P::turns];
+    uint32_t kw[kMbs ? P::words : 1], vw[kMbs ? P::words : 1];
+};
+
+template <int D, bool kMbs>
+__global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4)) void attention_prompt_kernel(AttentionArgs a) {
+    using P = PromptShape<D>;
+    extern __shared__ u32x4 lds_raw[];
+    PromptLds<D, kMbs>* lds = reinterpret_cast<PromptLds<D, kMbs>*>(lds_raw);  // [2]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
+    const int heads = a.cache.at.heads, shift = a.cache.at.page_shift;
+    const int head = blockIdx.x % heads;  // (the row tiles of one key head on one XCD, as far as the heads are 8 or so)
+
+    // the request and row tile: the last of the batch first, for under the causal rule a request's last rows see most
+    KvRequest r;
+    int32_t s = -1, row_tile = 0;
+    {
+        int64_t total = 0;
+        for (int s0 = (a.S - 1) / 64 * 64; s0 >= 0; s0 -= 64) {
+            const KvRequest x = request_of(a, s0 + lane);
+            total += read_lane(wave_scan(x.row_tiles(a.group, P::rows)), 63);
+        }
+        const int64_t tile = total - 1 - blockIdx.x / heads;
+        if (tile < 0) return;
+        int64_t before = 0;
+        for (int s0 = 0; s0 < a.S; s0 += 64) {
+            const KvRequest x = request_of(a, s0 + lane);
+            const int64_t mine = x.row_tiles(a.group, P::rows), end = before + wave_scan(mine);
+            const uint64_t hit = __builtin_amdgcn_ballot_w64(end > tile);
+            if (hit) {
+                const int at = __builtin_ctzll(hit);
+                s = s0 + at;
+                row_tile = (int32_t)(tile - (read_lane(end, at) - read_lane(mine, at)));
+                r = KvRequest{read_lane(x.first, at), read_lane(x.rows, at), read_lane(x.pos0, at), read_lane(x.keys, at)};
+                break;
+            }
+            before = read_lane(end, 63);
+        }
+        if (s < 0) return;
+    }
+    const int32_t rows = r.rows * a.group;
+    const int32_t row0 = row_tile * P::rows, row_last = min(row0 + P::rows, rows) - 1;
+    const int32_t lo_all = r.lo(row0 / a.group, a.window), hi_all = r.hi(row_last / a.group, a.causal);
+    const int32_t tile0 = lo_all / kKvTile, tile_end = (hi_all + kKvTile - 1) / kKvTile;
+    // the wavefront's rows: keys that some of them sees, and that all of them see
+    const int32_t my_row = row0 + 32 * wave + n;
+    const bool real = my_row < rows;
+    const int32_t wave_first = min(row0 + 32 * wave, rows - 1), wave_last = min(row0 + 32 * wave + 31, rows - 1);
+    const bool idle = row0 + 32 * wave >= rows;
+    const int32_t lo_some = r.lo(wave_first / a.group, a.window), hi_some = idle ? 0 : r.hi(wave_last / a.group, a.causal);
+    const int32_t lo_each = r.lo(wave_last / a.group, a.window), hi_each = r.hi(wave_first / a.group, a.causal);
+    const int32_t token = real ? my_row / a.group : 0;
+    const int q_head = head * a.group + (real ? my_row - token * a.group : 0);
+    const int32_t lo = real ? r.lo(token, a.window) : 0, hi = real ? r.hi(token, a.causal) : 0;
+
+    u32x4 q[P::steps];
+    {
+        const uint16_t* x = a.q + (int64_t)(r.first + token) * a.ldq + (int64_t)q_head * D + 8 * half;
+#pragma unroll
+        for (int e = 0; e < P::steps; ++e) q[e] = real ? *reinterpret_cast<const u32x4*>(x + 16 * e) : u32x4{0, 0, 0, 0};
+    }
+    f32x16 o[P::columns];
+#pragma unroll
+    for (int t = 0; t < P::columns; ++t) o[t] = f32x16{};
+    float m = kLowest, l = 0.0f;
+
+    // ---- codes of a tile: page id, load, expansion -----------------------------------------------------------------
+    const int32_t* table = a.block_table + (int64_t)s * a.max_pages;
+    const KvLayout& at = a.cache.at;
+    // where the lane's unit of turn i lies in a tile: K: (block, token = lane); V: 4 tokens 4 group .., unit of 8 columns
+    auto part_of = [&](int i) __attribute__((always_inline)) { return wave + P::waves * i; };
+    auto v_index = [&](int i) __attribute__((always_inline)) { return (part_of(i) - D / 32) * 64 + lane; };
+    auto subtile = [&](int i) __attribute__((always_inline)) { return part_of(i) < D / 32 ? lane >> 4 : v_index(i) / P::units >> 2; };
+    auto page_of = [&](int32_t tile, int sub) __attribute__((always_inline)) -> int32_t {  // -1: not there
+        const int32_t key = tile * kKvTile + 16 * sub;
+        int32_t p = -1;
+        if (tile < tile_end && key < r.keys) p = table[key >> shift];
+        return p < a.num_pages ? p : -1;
+    };
+    auto load = [&](PromptCodes<D, kMbs>& c, int32_t tile, const int32_t (&page)[P::turns], int32_t word_page) __attribute__((always_inline)) {
+        const int32_t mask = (1 << shift) - 1;
+#pragma unroll
+        for (int i = 0; i < P::turns; ++i) {
+            if (part_of(i) >= P::parts) continue;  // wave-uniform
+            const bool key = part_of(i) < D / 32;
+            const int64_t p = max(page[i], 0);
+            if (key) {
+                const int32_t place = (tile * kKvTile + lane) & mask;
+                c.codes[i] = *reinterpret_cast<const u32x4*>(a.cache.k_codes + at.k_block(p, head, part_of(i), place));
+                c.scales[i] = a.cache.k_scales[at.scale(p, head, part_of(i), place)];
+            } else {
+                const int32_t group = v_index(i) / P::units, unit = v_index(i) % P::units, place = (tile * kKvTile + 4 * group) & mask;
+                c.codes[i] = *reinterpret_cast<const u32x4*>(a.cache.v_codes + at.v_unit(p, head, unit, place));
+                c.scales[i] = *reinterpret_cast<const uint32_t*>(a.cache.v_scales + at.scale(p, head, unit >> 2, place));
+            }
+        }
+        if constexpr (kMbs) {
+            if (wave == P::waves - 1) {
+                const int32_t place = (tile * kKvTile + lane) & mask;
+                const int64_t p = max(word_page, 0);
+#pragma unroll
+                for (int w = 0; w < P::words; ++w) {
+                    c.kw[w] = a.cache.k_mbs[at.word(p, head, w, place)];
+                    c.vw[w] = a.cache.v_mbs[at.word(p, head, w, place)];
+                }
+            }
+        }
+    };
+    auto spread = [&](PromptLds<D, kMbs>& to, PromptCodes<D, kMbs>& c, int32_t tile, const int32_t (&page)[P::turns], int32_t word_page) __attribute__((always_inline)) {
+        const int32_t key0 = tile * kKvTile;
+#pragma unroll
+        for (int i = 0; i < P::turns; ++i) {
+            if (part_of(i) >= P::parts) continue;
+            if (part_of(i) < D / 32) {
+                // block b of key `lane`: elements 32 b + 8 j, j = 0..3, are step 2 b + j / 2, half j mod 2
+                const int b = part_of(i);
+                const float scale = scale_of(c.scales[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) to.k[(lane >> 5) * P::steps + 2 * b + (j >> 1)][32 * (j & 1) + n] = expand8(c.codes[i][j], scale);
+            } else {
+                const int32_t group = v_index(i) / P::units, unit = v_index(i) % P::units;
+                float scale[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int32_t key = key0 + 4 * group + t;
+                    uint32_t E = c.scales[i] >> (8 * t) & 0xFFu;
+                    // keys that nobody sees hold anything; NaN blocks go into the rows that see them, not through the product
+                    const bool used = key >= lo_all && key < hi_all && page[i] >= 0;
+                    if (used && E == 255u) {
+                        atomicOr(&to.bad[4 * group + t], 1u << (unit >> 2));
+                        to.any_bad = 1;
+                    }
+                    if (!used || E == 255u) {
+                        E = 127u;
+                        c.codes[i][t] = 0;
+                    }
+                    scale[t] = scale_of(E);
+                }
+                // group = 4 u + 2 w + h: keys of step u, half h, and of its eight the first or second four (w)
+                const int u = group >> 2, h = group & 1, w = group >> 1 & 1;
+                auto pair = [&](auto byte) __attribute__((always_inline)) {
+                    constexpr int kByte = decltype(byte)::value;
+                    uint32_t x[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) x[t] = expand<kByte>(c.codes[i][t], scale[t]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t which = e ? 0x07060302u : 0x05040100u;
+                        const int column = 8 * unit + 2 * kByte + e, c0 = column >> 7 << 2, f = min(D / 32 - c0, 4), d = column & 127;
+                        const int operand = c0 + d % f, row = d / f;
+                        reinterpret_cast<u32x2*>(&to.v[operand * 4 + u][32 * h + row])[w] =
+                            u32x2{__builtin_amdgcn_perm(x[1], x[0], which), __builtin_amdgcn_perm(x[3], x[2], which)};
+                    }
+                };
+                pair(std::integral_constant<int, 0>{});
+                pair(std::integral_constant<int, 1>{});
+                pair(std::integral_constant<int, 2>{});
+                pair(std::integral_constant<int, 3>{});
+            }
+        }
+        if (wave == P::waves - 1) {
+            const uint64_t have = __builtin_amdgcn_ballot_w64(word_page >= 0);
+            if (lane == 0) to.there = (uint32_t)(have & 1) | (uint32_t)(have >> 16 & 1) << 1 | (uint32_t)(have >> 32 & 1) << 2 | (uint32_t)(have >> 48 & 1) << 3;
+            if constexpr (kMbs) {
+#pragma unroll
+                for (int w = 0; w < P::words; ++w) {
+                    to.ks[w][lane] = sigma_of(c.kw[w]) * a.scale2;
+                    to.vs[w][lane] = sigma_of(c.vw[w]);
+                }
+            }
+        }
+    };
+
+    // ---- a tile from LDS ------------------------------------------------------------------------------------------------
+    auto take = [&](const PromptLds<D, kMbs>& from, int32_t tile) __attribute__((always_inline)) {
+        const int32_t key0 = tile * kKvTile;
+        if (key0 >= hi_some || key0 + kKvTile <= lo_some) return;
+        float x[32];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            f32x16 sum[P::words];
+#pragma unroll
+            for (int w = 0; w < P::words; ++w) {
+                sum[w] = f32x16{};
+#pragma unroll
+                for (int e = 8 * w; e < 8 * w + 8; ++e)
+                    if (e < P::steps) sum[w] = mfma32(from.k[kb * P::steps + e][lane], q[e], sum[w]);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = 32 * kb + 8 * (i >> 2) + (i & 3);  // + 4 half
+                if constexpr (kMbs) {
+                    float y = sum[0][i] * from.ks[0][key + 4 * half];
+#pragma unroll
+                    for (int w = 1; w < P::words; ++w) y += sum[w][i] * from.ks[w][key + 4 * half];
+                    x[16 * kb + i] = y;
+                } else {
+                    float y = sum[0][i];
+#pragma unroll
+                    for (int w = 1; w < P::words; ++w) y += sum[w][i];
+                    x[16 * kb + i] = y * a.scale2;
+                }
+            }
+        }
+        const uint32_t there = __builtin_amdgcn_readfirstlane(from.there);
+        if (!(key0 >= lo_each && key0 + kKvTile <= hi_each && there == 15u)) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int in_tile = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3), key = key0 + in_tile + 4 * half;
+                x[i] = key >= lo && key < hi && (there >> (in_tile >> 4) & 1) ? x[i] : -__builtin_inff();
+            }
+        }
+        if (__builtin_amdgcn_readfirstlane(from.any_bad)) {
+            uint32_t bad = 0;
+            for (int j = 0; j < kKvTile; ++j)
+                if (key0 + j >= lo && key0 + j < hi) bad |= from.bad[j];
+#pragma unroll
+            for (int t = 0; t < P::columns; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int column = 128 * (t / 4) + P::run(t) * (8 * (i >> 2) + 4 * half + (i & 3)) + t % 4;
+                    if (bad >> (column >> 5) & 1) o[t][i] = __builtin_nanf("");
+                }
+        }
+        float top = fmaxf(x[0], x[1]);
+#pragma unroll
+        for (int i = 2; i < 32; ++i) top = fmaxf(top, x[i]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__builtin_amdgcn_ballot_w64(top > m + 8.0f)) {
+            const float higher = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - higher);
+            m = higher;
+            l *= shrink;
+#pragma unroll
+            for (int t = 0; t < P::columns; ++t) o[t] *= shrink;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            x[i] = __builtin_amdgcn_exp2f(x[i] - m);
+            l += x[i];
+        }
+#pragma unroll
+        for (int w = 0; w < (kMbs ? P::words : 1); ++w) {
+            u32x4 weight[4];  // of 16 keys each, as the second operand
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float y0 = x[8 * u + 2 * j], y1 = x[8 * u + 2 * j + 1];
+                    if constexpr (kMbs) {
+                        const int key = 16 * u + 8 * (j >> 1) + 2 * (j & 1) + 4 * half;
+                        y0 *= from.vs[w][key];
+                        y1 *= from.vs[w][key + 1];
+                    }
+                    weight[u][j] = pack_bf16(y0, y1);
+                }
+            }
+#pragma unroll
+            for (int t = (kMbs ? 4 * w : 0); t < (kMbs ? 4 * w + 4 : P::columns); ++t) {
+                if (t >= P::columns) break;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) o[t] = mfma32(from.v[t * 4 + u][lane], weight[u], o[t]);
+            }
+        }
+    };
+
+    // ---- the loop: tile t multiplied, t + 1 expanded, t + 2 loaded, page ids of t + 3 ------------------------------------
+    if (tile0 < tile_end) {
+        int32_t page[P::turns], page_next[P::turns], word_page, word_page_next;
+        PromptCodes<D, kMbs> codes;
+        auto ids = [&](int32_t tile, int32_t (&p)[P::turns], int32_t& w) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < P::turns; ++i) p[i] = page_of(tile, subtile(i));
+            w = page_of(tile, lane >> 4);
+        };
+        for (int b = 0; b < 2; ++b) {
+            if (threadIdx.x < kKvTile) lds[b].bad[threadIdx.x] = 0;
+            if (threadIdx.x == 0) lds[b].any_bad = 0;
+        }
+        ids(tile0, page, word_page);
+        load(codes, tile0, page, word_page);
+        ids(tile0 + 1, page_next, word_page_next);
+        meet();
+        spread(lds[0], codes, tile0, page, word_page);
+        for (int32_t tile = tile0; tile < tile_end; ++tile) {
+            PromptLds<D, kMbs>&now = lds[(tile - tile0) & 1], &next = lds[(tile - tile0 + 1) & 1];
+#pragma unroll
+            for (int i = 0; i < P::turns; ++i) page[i] = page_next[i];
+            word_page = word_page_next;
+            if (tile + 1 < tile_end) load(codes, tile + 1, page, word_page);
+            ids(tile + 2, page_next, word_page_next);
+            meet();  // `now` is written, and nobody reads `next` any more
+            take(now, tile);
+            const bool was_bad = __builtin_amdgcn_readfirstlane(now.any_bad);
+            if (tile + 1 < tile_end) spread(next, codes, tile + 1, page, word_page);
+            if (was_bad) {  // (rare) cleared once everybody has read it
+                meet();
+                if (threadIdx.x < kKvTile) now.bad[threadIdx.x] = 0;
+                if (threadIdx.x == 0) now.any_bad = 0;
+            }
+        }
+    }
+
+    l += __shfl_xor(l, 32);
+    if (!real) return;
+    const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t t = r.first + token;
+    if (a.lse && half == 0) a.lse[t * a.Hq + q_head] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
+    uint16_t* out = a.out + t * a.ldo + (int64_t)q_head * D;
+#pragma unroll
+    for (int c = 0; c < P::columns; c += 4) {
+        constexpr int kMost = 16;
+        const int f = P::run(c);
+#pragma unroll
+        for (int i0 = 0; i0 < 16; i0 += 4) {
+            float y[kMost];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < f) y[f * b + e] = o[c + e < P::columns ? c + e : 0][i0 + b] * inverse;
+            uint16_t* to = out + 32 * c + f * (2 * i0 + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4 * f; e += 4) *reinterpret_cast<u32x2*>(to + e) = u32x2{pack_bf16(y[e], y[e + 1]), pack_bf16(y[e + 2], y[e + 3])};
+        }
+    }
+}
+
+template <int D, bool kMbs>
+int launch_prompt(const AttentionArgs& a, hipStream_t s) {
+    using P = PromptShape<D>;
+    constexpr int kBytes = 2 * sizeof(PromptLds<D, kMbs>);
+    static LdsOptIn opt_in;
+    if (int st = opt_in.ensure(reinterpret_cast<const void*>(&attention_prompt_kernel<D, kMbs>), kBytes)) return st;
+    const int64_t groups = prompt_row_tiles(a.S, a.T, a.group, D) * a.cache.at.heads;
+    if (groups >= (int64_t)1 << 23) return MX_EINVAL;  // (a launch of fewer than 2^32 work-items)
+    hipLaunchKernelGGL((attention_prompt_kernel<D, kMbs>), dim3((unsigned)groups), dim3(P::threads), kBytes, s, a);
+    return launch_status();
+}
+
+}  // namespace
+
+int64_t prompt_row_tiles(int64_t S, int64_t T, int64_t group, int64_t D) {
+    const int64_t rows = D <= 128 ? PromptShape<128>::rows : PromptShape<256>::rows;
+    return S + (T * group + rows - 1) / rows;  // one partial tile a request at most
+}
+
+int launch_attention_prompt(const AttentionArgs& a, hipStream_t stream) {
+    const bool mbs = a.cache.k_mbs != nullptr;
+    switch (a.cache.at.D) {
+        case 64: return mbs ? launch_prompt<64, true>(a, stream) : launch_prompt<64, false>(a, stream);
+        case 96: return mbs ? launch_prompt<96, true>(a, stream) : launch_prompt<96, false>(a, stream);
+        case 128: return mbs ? launch_prompt<128, true>(a, stream) : launch_prompt<128, false>(a, stream);
+        case 192: return mbs ? launch_prompt<192, true>(a, stream) : launch_prompt<192, false>(a, stream);
+        default: return mbs ? launch_prompt<256, true>(a, stream) : launch_prompt<256, false>(a, stream);
+    }
+}
+
+}  // namespace mx

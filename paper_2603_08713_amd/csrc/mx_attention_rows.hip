@@ -15,12 +15,6 @@ namespace {
 constexpr int kThreads = 256, kWavesInGroup = kThreads / kWave;
 constexpr int32_t kLeastShare = 1;
 
-__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int32_t read_lane(int32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-__device__ __forceinline__ int64_t read_lane(int64_t x, int lane) {
-    return (int64_t)((uint64_t)(uint32_t)read_lane((int32_t)x, lane) | (uint64_t)(uint32_t)read_lane((int32_t)(x >> 32), lane) << 32);
-}
-
 // The batch as a wavefront sees it: a lane has a request, of 64 at a time (what a batch of up to 64 needs is loaded once).
 struct Batch {
     const AttentionArgs& a;
@@ -41,30 +35,12 @@ struct Batch {
     }
     __device__ __forceinline__ void load(int first) {
         block = first;
-        const int s = first + (int)(threadIdx.x & 63);
-        r = KvRequest{0, 0, 0, 0};
-        if (s < a.S) r = KvRequest::make(a.row_offsets[s], a.row_offsets[s + 1], a.kv_lens[s], a.T, a.room);
+        r = request_of(a, first + (int)(threadIdx.x & 63));
         tiles = r.tiles(a.window, a.causal);
         row_tiles = r.row_tiles(a.group, height);
         size = KvLine::request(tiles, row_tiles, a.cache.at.heads);
     }
-    // (through the lanes by DPP: rows of 16, then pairs of rows, then halves; the LDS crossbar would take its latency twelve times)
-    __device__ __forceinline__ void scan(int64_t before) {
-        end = size;
-        end = add_from<0x111, 0xF>(end);  // row_shr:1, 2, 4, 8
-        end = add_from<0x112, 0xF>(end);
-        end = add_from<0x114, 0xF>(end);
-        end = add_from<0x118, 0xF>(end);
-        end = add_from<0x142, 0xA>(end);  // row_bcast:15 into rows 1 and 3
-        end = add_from<0x143, 0xC>(end);  // row_bcast:31 into rows 2 and 3
-        end += before;
-    }
-    template <int kControl, int kRows>
-    __device__ __forceinline__ static int64_t add_from(int64_t x) {
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kControl, kRows, 0xF, false);
-        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(x >> 32), kControl, kRows, 0xF, false);
-        return x + (int64_t)((uint64_t)hi << 32 | lo);
-    }
+    __device__ __forceinline__ void scan(int64_t before) { end = before + wave_scan(size); }
     // the lane that has the request that `mine` (of a lane) says, moving on through the blocks; -1: none has
     template <typename F>
     __device__ __forceinline__ int find(F&& mine) {

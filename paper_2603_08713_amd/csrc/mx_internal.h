@@ -44,6 +44,15 @@ int mx_internal_gemm_elem(mx_elem_t a_elem, const uint8_t* a_codes, const uint8_
                           int64_t M, int64_t N, int64_t K, mx_dtype_t c_dtype, void* C, int64_t ldc, int force,
                           void* stream);
 
+// mx_attention_kv with the kernel chosen: 0 = as mx_attention_kv, 1 = the one for few rows, 2 = the one for many; and the workspace that it wants.
+int mx_internal_attention_kv(int force, const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens,
+                             const int32_t* block_table, int64_t max_pages, const uint8_t* k_codes, const uint8_t* k_scales,
+                             const uint8_t* k_mbs_or_null, const uint8_t* v_codes, const uint8_t* v_scales, const uint8_t* v_mbs_or_null,
+                             int64_t num_pages, int64_t page_size, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, float scale,
+                             int causal, int64_t window, void* out_bf16, int64_t ldo, float* lse_or_null, void* workspace,
+                             int64_t workspace_bytes, void* stream);
+int64_t mx_internal_attention_kv_workspace(int force, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,14 +8,16 @@ import kv_reference as ref  # noqa: E402
 pytestmark = pytest.mark.gpu
 
 
-@pytest.fixture(scope="module")
-def mx():
+@pytest.fixture(params=["few rows", "many rows"])
+def mx(request):
+    """Every test with either kernel: which of them a call takes goes by its sizes."""
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     import paper_2603_08713_amd as mx_
 
     mx_.load_library()
-    return mx_
+    with mx_.forced(attention=1 if request.param == "few rows" else 2):
+        yield mx_
 
 
 class Batch:
@@ -208,8 +210,9 @@ def test_workspaces_streams_and_graphs(mx, n, keys):
     work = torch.full((size + 64,), 0xFF, dtype=torch.uint8, device="cuda")
     got = b.run(workspace=work[:size])
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool((work[size:] == 0xFF).all())
-    with pytest.raises(mx.MxError):
-        b.run(workspace=work[:size - 16])
+    if size:
+        with pytest.raises(mx.binding.MxError):
+            b.run(workspace=work[:size - 16])
     out, lse = torch.zeros_like(want[0]), torch.zeros_like(want[1])
 
     def call():
