@@ -40,12 +40,14 @@ struct PromptShape {
     static constexpr int run(int t) { return D / 32 - t / 4 * 4 < 4 ? D / 32 - t / 4 * 4 : 4; }
 };
 
-template <int D, bool kMbs>
-struct PromptLds {  // of one tile
-    u32x4 k[D / 8][kWave], v[D / 8][kWave];
-    float ks[(D + 127) / 128][kKvTile], vs[(D + 127) / 128][kKvTile];  // scale2 / F of a key, 1 / F of a value
-    uint32_t bad[kKvTile];                                            // blocks of a value that are NaN
-    uint32_t any_bad, there;                                          // whether any is; subtiles whose page exists
+template <int D>
+struct PromptLds {
+    u32x4 k[2][D / 8][kWave], v[2][D / 8][kWave];  // by tile mod 2
+    struct {                                       // by tile mod 3
+        float ks[(D + 127) / 128][kKvTile], vs[(D + 127) / 128][kKvTile];  // scale2 / F of a key, 1 / F of a value
+        uint32_t there;                                                    // subtiles whose page exists
+    } of[3];
+    uint32_t bad[2][kKvTile], any_bad[2];  // blocks of a value that are NaN, and whether any is
 };
 
 // One wavefront's share of a tile's codes, in flight.
@@ -61,7 +63,7 @@ template <int D, bool kMbs>
 __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4)) void attention_prompt_kernel(AttentionArgs a) {
     using P = PromptShape<D>;
     extern __shared__ u32x4 lds_raw[];
-    PromptLds<D, kMbs>* lds = reinterpret_cast<PromptLds<D, kMbs>*>(lds_raw);  // [2]
+    PromptLds<D>& lds = *reinterpret_cast<PromptLds<D>*>(lds_raw);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
     const int heads = a.cache.at.heads, shift = a.cache.at.page_shift;
     const int head = blockIdx.x % heads;  // (the row tiles of one key head on one XCD, as far as the heads are 8 or so)
@@ -129,9 +131,10 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
     auto page_of = [&](int32_t tile, int sub) __attribute__((always_inline)) -> int32_t {  // -1: not there
         const int32_t key = tile * kKvTile + 16 * sub;
         int32_t p = -1;
-        if (tile < tile_end && key < r.keys) p = table[key >> shift];
+        if (tile >= tile0 && tile < tile_end && key < r.keys) p = table[key >> shift];
         return p < a.num_pages ? p : -1;
     };
+    // (a step loads, expands and so on V of tile t and everything else of tile t + 1)
     auto load = [&](PromptCodes<D, kMbs>& c, int32_t tile, const int32_t (&page)[P::turns], int32_t word_page) __attribute__((always_inline)) {
         const int32_t mask = (1 << shift) - 1;
 #pragma unroll
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
             const bool key = part_of(i) < D / 32;
             const int64_t p = max(page[i], 0);
             if (key) {
-                const int32_t place = (tile * kKvTile + lane) & mask;
+                const int32_t place = ((tile + 1) * kKvTile + lane) & mask;
                 c.codes[i] = *reinterpret_cast<const u32x4*>(a.cache.k_codes + at.k_block(p, head, part_of(i), place));
                 c.scales[i] = a.cache.k_scales[at.scale(p, head, part_of(i), place)];
             } else {
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
         }
         if constexpr (kMbs) {
             if (wave == P::waves - 1) {
-                const int32_t place = (tile * kKvTile + lane) & mask;
+                const int32_t place = ((tile + 1) * kKvTile + lane) & mask;
                 const int64_t p = max(word_page, 0);
 #pragma unroll
                 for (int w = 0; w < P::words; ++w) {
@@ -161,8 +164,9 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
             }
         }
     };
-    auto spread = [&](PromptLds<D, kMbs>& to, PromptCodes<D, kMbs>& c, int32_t tile, const int32_t (&page)[P::turns], int32_t word_page) __attribute__((always_inline)) {
-        const int32_t key0 = tile * kKvTile;
+    auto spread = [&](int step, PromptCodes<D, kMbs>& c, int32_t tile, const int32_t (&page)[P::turns], int32_t word_page) __attribute__((always_inline)) {
+        const int32_t key0 = tile * kKvTile;  // (step: tile - tile0, at least -1)
+        u32x4(*to_k)[kWave] = lds.k[(step + 1) & 1], (*to_v)[kWave] = lds.v[step & 1];
 #pragma unroll
         for (int i = 0; i < P::turns; ++i) {
             if (part_of(i) >= P::parts) continue;
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
                 const int b = part_of(i);
                 const float scale = scale_of(c.scales[i]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) to.k[(lane >> 5) * P::steps + 2 * b + (j >> 1)][32 * (j & 1) + n] = expand8(c.codes[i][j], scale);
+                for (int j = 0; j < 4; ++j) to_k[(lane >> 5) * P::steps + 2 * b + (j >> 1)][32 * (j & 1) + n] = expand8(c.codes[i][j], scale);
             } else {
                 const int32_t group = v_index(i) / P::units, unit = v_index(i) % P::units;
                 float scale[4];
@@ -182,8 +186,8 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
                     // keys that nobody sees hold anything; NaN blocks go into the rows that see them, not through the product
                     const bool used = key >= lo_all && key < hi_all && page[i] >= 0;
                     if (used && E == 255u) {
-                        atomicOr(&to.bad[4 * group + t], 1u << (unit >> 2));
-                        to.any_bad = 1;
+                        atomicOr(&lds.bad[step & 1][4 * group + t], 1u << (unit >> 2));
+                        lds.any_bad[step & 1] = 1;
                     }
                     if (!used || E == 255u) {
                         E = 127u;
@@ -203,7 +207,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
                         const uint32_t which = e ? 0x07060302u : 0x05040100u;
                         const int column = 8 * unit + 2 * kByte + e, c0 = column >> 7 << 2, f = min(D / 32 - c0, 4), d = column & 127;
                         const int operand = c0 + d % f, row = d / f;
-                        reinterpret_cast<u32x2*>(&to.v[operand * 4 + u][32 * h + row])[w] =
+                        reinterpret_cast<u32x2*>(&to_v[operand * 4 + u][32 * h + row])[w] =
                             u32x2{__builtin_amdgcn_perm(x[1], x[0], which), __builtin_amdgcn_perm(x[3], x[2], which)};
                     }
                 };
@@ -215,6 +219,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
         }
         if (wave == P::waves - 1) {
             const uint64_t have = __builtin_amdgcn_ballot_w64(word_page >= 0);
+            auto& to = lds.of[(step + 1) % 3];
             if (lane == 0) to.there = (uint32_t)(have & 1) | (uint32_t)(have >> 16 & 1) << 1 | (uint32_t)(have >> 32 & 1) << 2 | (uint32_t)(have >> 48 & 1) << 3;
             if constexpr (kMbs) {
 #pragma unroll
@@ -227,34 +232,36 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
     };
 
     // ---- a tile from LDS ------------------------------------------------------------------------------------------------
-    auto take = [&](const PromptLds<D, kMbs>& from, int32_t tile) __attribute__((always_inline)) {
-        const int32_t key0 = tile * kKvTile;
-        if (key0 >= hi_some || key0 + kKvTile <= lo_some) return;
-        float x[32];
+    f32x16 sum[2][P::words];               // K Q^T of 32 keys each, by windows
+    u32x4 weight[kMbs ? P::words : 1][4];  // P^T of 16 keys each, as the second operand
+    auto scores = [&](const u32x4 (*k)[kWave]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            f32x16 sum[P::words];
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int w = 0; w < P::words; ++w) {
-                sum[w] = f32x16{};
+                sum[kb][w] = f32x16{};
 #pragma unroll
                 for (int e = 8 * w; e < 8 * w + 8; ++e)
-                    if (e < P::steps) sum[w] = mfma32(from.k[kb * P::steps + e][lane], q[e], sum[w]);
+                    if (e < P::steps) sum[kb][w] = mfma32(k[kb * P::steps + e][lane], q[e], sum[kb][w]);
             }
+    };
+    // the weights of `tile`, whose scores are in `sum`
+    auto weigh = [&](int step, int32_t tile) __attribute__((always_inline)) {
+        const auto& from = lds.of[step % 3];
+        const int32_t key0 = tile * kKvTile;
+        float x[32];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int key = 32 * kb + 8 * (i >> 2) + (i & 3);  // + 4 half
-                if constexpr (kMbs) {
-                    float y = sum[0][i] * from.ks[0][key + 4 * half];
+        for (int i = 0; i < 32; ++i) {
+            const int kb = i >> 4, key = 32 * kb + 8 * ((i & 15) >> 2) + (i & 3);  // + 4 half
+            if constexpr (kMbs) {
+                x[i] = sum[kb][0][i & 15] * from.ks[0][key + 4 * half];
 #pragma unroll
-                    for (int w = 1; w < P::words; ++w) y += sum[w][i] * from.ks[w][key + 4 * half];
-                    x[16 * kb + i] = y;
-                } else {
-                    float y = sum[0][i];
+                for (int w = 1; w < P::words; ++w) x[i] += sum[kb][w][i & 15] * from.ks[w][key + 4 * half];
+            } else {
+                x[i] = sum[kb][0][i & 15];
 #pragma unroll
-                    for (int w = 1; w < P::words; ++w) y += sum[w][i];
-                    x[16 * kb + i] = y * a.scale2;
-                }
+                for (int w = 1; w < P::words; ++w) x[i] += sum[kb][w][i & 15];
+                x[i] *= a.scale2;
             }
         }
         const uint32_t there = __builtin_amdgcn_readfirstlane(from.there);
@@ -264,18 +271,6 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
                 const int in_tile = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3), key = key0 + in_tile + 4 * half;
                 x[i] = key >= lo && key < hi && (there >> (in_tile >> 4) & 1) ? x[i] : -__builtin_inff();
             }
-        }
-        if (__builtin_amdgcn_readfirstlane(from.any_bad)) {
-            uint32_t bad = 0;
-            for (int j = 0; j < kKvTile; ++j)
-                if (key0 + j >= lo && key0 + j < hi) bad |= from.bad[j];
-#pragma unroll
-            for (int t = 0; t < P::columns; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int column = 128 * (t / 4) + P::run(t) * (8 * (i >> 2) + 4 * half + (i & 3)) + t % 4;
-                    if (bad >> (column >> 5) & 1) o[t][i] = __builtin_nanf("");
-                }
         }
         float top = fmaxf(x[0], x[1]);
 #pragma unroll
@@ -289,68 +284,103 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
             for (int t = 0; t < P::columns; ++t) o[t] *= shrink;
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            x[i] = __builtin_amdgcn_exp2f(x[i] - m);
-            l += x[i];
-        }
+        for (int u = 0; u < 4; ++u) {
 #pragma unroll
-        for (int w = 0; w < (kMbs ? P::words : 1); ++w) {
-            u32x4 weight[4];  // of 16 keys each, as the second operand
+            for (int j = 0; j < 4; ++j) {
+                const float y0 = __builtin_amdgcn_exp2f(x[8 * u + 2 * j] - m), y1 = __builtin_amdgcn_exp2f(x[8 * u + 2 * j + 1] - m);
+                l += y0 + y1;
+                if constexpr (kMbs) {
+                    const int key = 16 * u + 8 * (j >> 1) + 2 * (j & 1) + 4 * half;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float y0 = x[8 * u + 2 * j], y1 = x[8 * u + 2 * j + 1];
-                    if constexpr (kMbs) {
-                        const int key = 16 * u + 8 * (j >> 1) + 2 * (j & 1) + 4 * half;
-                        y0 *= from.vs[w][key];
-                        y1 *= from.vs[w][key + 1];
-                    }
-                    weight[u][j] = pack_bf16(y0, y1);
+                    for (int w = 0; w < P::words; ++w) weight[w][u][j] = pack_bf16(y0 * from.vs[w][key], y1 * from.vs[w][key + 1]);
+                } else {
+                    weight[0][u][j] = pack_bf16(y0, y1);
                 }
-            }
-#pragma unroll
-            for (int t = (kMbs ? 4 * w : 0); t < (kMbs ? 4 * w + 4 : P::columns); ++t) {
-                if (t >= P::columns) break;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) o[t] = mfma32(from.v[t * 4 + u][lane], weight[u], o[t]);
             }
         }
     };
+    // the tile's V by its weights, and the next one's scores (past the last tile of whatever is in LDS, and nobody reads them)
+    auto multiply = [&](int step, int32_t tile) __attribute__((always_inline)) {
+        if (__builtin_amdgcn_readfirstlane(lds.any_bad[step & 1])) {
+            const int32_t key0 = tile * kKvTile;
+            uint32_t bad = 0;
+            for (int j = 0; j < kKvTile; ++j)
+                if (key0 + j >= lo && key0 + j < hi) bad |= lds.bad[step & 1][j];
+#pragma unroll
+            for (int t = 0; t < P::columns; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int column = 128 * (t / 4) + P::run(t) * (8 * (i >> 2) + 4 * half + (i & 3)) + t % 4;
+                    if (bad >> (column >> 5) & 1) o[t][i] = __builtin_nanf("");
+                }
+        }
+        const u32x4(*v)[kWave] = lds.v[step & 1];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int t = 0; t < P::columns; ++t) o[t] = mfma32(v[t * 4 + u][lane], weight[kMbs ? t / 4 : 0][u], o[t]);
+        scores(lds.k[(step + 1) & 1]);
+        // operands are asked of LDS several products ahead: left to itself the compiler reads each right before its product and waits for it
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * P::columns + 2 * P::steps; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+    };
 
-    // ---- the loop: tile t multiplied, t + 1 expanded, t + 2 loaded, page ids of t + 3 ------------------------------------
+    // ---- the loop: tile t is taken, V of t + 1 and the rest of t + 2 expanded from codes loaded a tile earlier, page ids a tile before that.  Of
+    // the two wavefronts of a SIMD one weighs a tile and then multiplies, the other multiplies and then weighs the next tile: while one keeps
+    // the matrix pipeline the other has the vector ALU.
     if (tile0 < tile_end) {
+        const bool late = wave < 4;
         int32_t page[P::turns], page_next[P::turns], word_page, word_page_next;
         PromptCodes<D, kMbs> codes;
         auto ids = [&](int32_t tile, int32_t (&p)[P::turns], int32_t& w) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < P::turns; ++i) p[i] = page_of(tile, subtile(i));
-            w = page_of(tile, lane >> 4);
+            for (int i = 0; i < P::turns; ++i) p[i] = page_of(part_of(i) < D / 32 ? tile + 1 : tile, subtile(i));
+            w = page_of(tile + 1, lane >> 4);
         };
-        for (int b = 0; b < 2; ++b) {
-            if (threadIdx.x < kKvTile) lds[b].bad[threadIdx.x] = 0;
-            if (threadIdx.x == 0) lds[b].any_bad = 0;
-        }
-        ids(tile0, page, word_page);
-        load(codes, tile0, page, word_page);
-        ids(tile0 + 1, page_next, word_page_next);
-        meet();
-        spread(lds[0], codes, tile0, page, word_page);
-        for (int32_t tile = tile0; tile < tile_end; ++tile) {
-            PromptLds<D, kMbs>&now = lds[(tile - tile0) & 1], &next = lds[(tile - tile0 + 1) & 1];
+        auto turn = [&](int32_t tile) __attribute__((always_inline)) {  // loads step `tile`, page ids of the next
 #pragma unroll
             for (int i = 0; i < P::turns; ++i) page[i] = page_next[i];
             word_page = word_page_next;
-            if (tile + 1 < tile_end) load(codes, tile + 1, page, word_page);
-            ids(tile + 2, page_next, word_page_next);
-            meet();  // `now` is written, and nobody reads `next` any more
-            take(now, tile);
-            const bool was_bad = __builtin_amdgcn_readfirstlane(now.any_bad);
-            if (tile + 1 < tile_end) spread(next, codes, tile + 1, page, word_page);
+            load(codes, tile, page, word_page);
+            ids(tile + 1, page_next, word_page_next);
+        };
+        if (threadIdx.x < 2 * kKvTile) (&lds.bad[0][0])[threadIdx.x] = 0;
+        if (threadIdx.x < 2) lds.any_bad[threadIdx.x] = 0;
+        const int32_t first_seen = max(tile0, lo_some / kKvTile), behind_seen = (hi_some + kKvTile - 1) / kKvTile;
+        // K of tile0 (V of this step is nobody's: no codes), then V of tile0 and K of tile0 + 1
+        ids(tile0 - 1, page_next, word_page_next);
+        turn(tile0 - 1);
+        meet();
+        spread(-1, codes, tile0 - 1, page, word_page);
+        turn(tile0);
+        meet();
+        if (first_seen == tile0 && tile0 < behind_seen) {
+            scores(lds.k[0]);
+            if (!late) weigh(0, tile0);
+        }
+        spread(0, codes, tile0, page, word_page);
+        for (int32_t tile = tile0; tile < tile_end; ++tile) {
+            const int step = tile - tile0;
+            turn(tile + 1);
+            meet();  // V of t and the rest of t + 1 are written; nobody reads V of t - 1 or K of t any more
+            const bool seen = tile >= first_seen && tile < behind_seen, seen_next = tile + 1 >= first_seen && tile + 1 < behind_seen;
+            if (seen) {
+                if (late) weigh(step, tile);
+                multiply(step, tile);
+            } else if (seen_next) {
+                scores(lds.k[(step + 1) & 1]);
+            }
+            if (!late && seen_next) weigh(step + 1, tile + 1);
+            const bool was_bad = __builtin_amdgcn_readfirstlane(lds.any_bad[step & 1]);
+            spread(step + 1, codes, tile + 1, page, word_page);
             if (was_bad) {  // (rare) cleared once everybody has read it
                 meet();
-                if (threadIdx.x < kKvTile) now.bad[threadIdx.x] = 0;
-                if (threadIdx.x == 0) now.any_bad = 0;
+                if (threadIdx.x < kKvTile) lds.bad[step & 1][threadIdx.x] = 0;
+                if (threadIdx.x == 0) lds.any_bad[step & 1] = 0;
             }
         }
     }
@@ -383,7 +413,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
 template <int D, bool kMbs>
 int launch_prompt(const AttentionArgs& a, hipStream_t s) {
     using P = PromptShape<D>;
-    constexpr int kBytes = 2 * sizeof(PromptLds<D, kMbs>);
+    constexpr int kBytes = sizeof(PromptLds<D>);
     static LdsOptIn opt_in;
     if (int st = opt_in.ensure(reinterpret_cast<const void*>(&attention_prompt_kernel<D, kMbs>), kBytes)) return st;
     const int64_t groups = prompt_row_tiles(a.S, a.T, a.group, D) * a.cache.at.heads;
