@@ -43,7 +43,7 @@ struct PromptShape {
 template <int D>
 struct PromptLds {
     u32x4 k[2][D / 8][kWave], v[2][D / 8][kWave];  // by tile mod 2
-    struct {                                       // by tile mod 3
+    struct alignas(16) {                           // by tile mod 3
         float ks[(D + 127) / 128][kKvTile], vs[(D + 127) / 128][kKvTile];  // scale2 / F of a key, 1 / F of a value
         uint32_t there;                                                    // subtiles whose page exists
     } of[3];
@@ -134,32 +134,52 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
         if (tile >= tile0 && tile < tile_end && key < r.keys) p = table[key >> shift];
         return p < a.num_pages ? p : -1;
     };
+    // addresses: the lane's part of each array in page 0, place 0; a page and a place in it come on top
+    const uint32_t code_page = (uint32_t)at.k_block(1, 0, 0, 0), scale_page = (uint32_t)at.scale(1, 0, 0, 0), word_page_bytes = (uint32_t)at.word(1, 0, 0, 0);
+    const int32_t mask = (1 << shift) - 1;
+    const uint8_t *code_at[P::turns], *scale_at[P::turns];
+    int32_t first_key[P::turns];     // of the lane's unit, in the tile
+    uint32_t v_base[P::turns];       // where its V goes in LDS: bytes
+#pragma unroll
+    for (int i = 0; i < P::turns; ++i) {
+        if (part_of(i) < D / 32) {
+            code_at[i] = a.cache.k_codes + at.k_block(0, head, part_of(i), 0);
+            scale_at[i] = a.cache.k_scales + at.scale(0, head, part_of(i), 0);
+            first_key[i] = lane;
+            v_base[i] = 0;
+        } else {
+            const int32_t group = v_index(i) / P::units, unit = v_index(i) % P::units;
+            code_at[i] = a.cache.v_codes + at.v_unit(0, head, unit, 0);
+            scale_at[i] = a.cache.v_scales + at.scale(0, head, unit >> 2, 0);
+            first_key[i] = 4 * group;
+            // group = 4 u + 2 w + h: keys of step u, half h, and of its eight the first or second four (w)
+            v_base[i] = (group >> 2) * 1024 + 512 * (group & 1) + 8 * (group >> 1 & 1);
+        }
+    }
     // (a step loads, expands and so on V of tile t and everything else of tile t + 1)
     auto load = [&](PromptCodes<D, kMbs>& c, int32_t tile, const int32_t (&page)[P::turns], int32_t word_page) __attribute__((always_inline)) {
-        const int32_t mask = (1 << shift) - 1;
 #pragma unroll
         for (int i = 0; i < P::turns; ++i) {
             if (part_of(i) >= P::parts) continue;  // wave-uniform
-            const bool key = part_of(i) < D / 32;
-            const int64_t p = max(page[i], 0);
-            if (key) {
-                const int32_t place = ((tile + 1) * kKvTile + lane) & mask;
-                c.codes[i] = *reinterpret_cast<const u32x4*>(a.cache.k_codes + at.k_block(p, head, part_of(i), place));
-                c.scales[i] = a.cache.k_scales[at.scale(p, head, part_of(i), place)];
+            const uint32_t p = (uint32_t)max(page[i], 0);
+            if (part_of(i) < D / 32) {
+                const uint32_t place = ((tile + 1) * kKvTile + first_key[i]) & mask;
+                c.codes[i] = *reinterpret_cast<const u32x4*>(code_at[i] + ((uint64_t)p * code_page + place * 16));
+                c.scales[i] = *(scale_at[i] + ((uint64_t)p * scale_page + place));
             } else {
-                const int32_t group = v_index(i) / P::units, unit = v_index(i) % P::units, place = (tile * kKvTile + 4 * group) & mask;
-                c.codes[i] = *reinterpret_cast<const u32x4*>(a.cache.v_codes + at.v_unit(p, head, unit, place));
-                c.scales[i] = *reinterpret_cast<const uint32_t*>(a.cache.v_scales + at.scale(p, head, unit >> 2, place));
+                const uint32_t place = (tile * kKvTile + first_key[i]) & mask;  // a multiple of 4
+                c.codes[i] = *reinterpret_cast<const u32x4*>(code_at[i] + ((uint64_t)p * code_page + place * (D / 2)));
+                c.scales[i] = *reinterpret_cast<const uint32_t*>(scale_at[i] + ((uint64_t)p * scale_page + place));
             }
         }
         if constexpr (kMbs) {
             if (wave == P::waves - 1) {
-                const int32_t place = ((tile + 1) * kKvTile + lane) & mask;
-                const int64_t p = max(word_page, 0);
+                const uint32_t place = ((tile + 1) * kKvTile + lane) & mask;
+                const uint64_t p = (uint64_t)(uint32_t)max(word_page, 0) * word_page_bytes + place;
 #pragma unroll
                 for (int w = 0; w < P::words; ++w) {
-                    c.kw[w] = a.cache.k_mbs[at.word(p, head, w, place)];
-                    c.vw[w] = a.cache.v_mbs[at.word(p, head, w, place)];
+                    c.kw[w] = a.cache.k_mbs[at.word(0, head, w, 0) + p];
+                    c.vw[w] = a.cache.v_mbs[at.word(0, head, w, 0) + p];
                 }
             }
         }
@@ -177,26 +197,28 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
 #pragma unroll
                 for (int j = 0; j < 4; ++j) to_k[(lane >> 5) * P::steps + 2 * b + (j >> 1)][32 * (j & 1) + n] = expand8(c.codes[i][j], scale);
             } else {
-                const int32_t group = v_index(i) / P::units, unit = v_index(i) % P::units;
+                const uint32_t unit = v_index(i) % P::units;
+                // keys that nobody sees hold anything; NaN blocks go into the rows that see them, not through the product
+                const bool inside = key0 >= lo_all && key0 + kKvTile <= hi_all;
+                if (!inside || __builtin_amdgcn_ballot_w64(page[i] < 0 || ((~c.scales[i] - 0x01010101u) & c.scales[i] & 0x80808080u))) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const int32_t key = key0 + first_key[i] + t;
+                        const bool used = key >= lo_all && key < hi_all && page[i] >= 0, nan = (c.scales[i] >> (8 * t) & 0xFFu) == 255u;
+                        if (used && nan) {
+                            atomicOr(&lds.bad[step & 1][first_key[i] + t], 1u << (unit >> 2));
+                            lds.any_bad[step & 1] = 1;
+                        }
+                        if (!used || nan) {
+                            c.scales[i] = (c.scales[i] & ~(0xFFu << (8 * t))) | 127u << (8 * t);
+                            c.codes[i][t] = 0;
+                        }
+                    }
+                }
                 float scale[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int32_t key = key0 + 4 * group + t;
-                    uint32_t E = c.scales[i] >> (8 * t) & 0xFFu;
-                    // keys that nobody sees hold anything; NaN blocks go into the rows that see them, not through the product
-                    const bool used = key >= lo_all && key < hi_all && page[i] >= 0;
-                    if (used && E == 255u) {
-                        atomicOr(&lds.bad[step & 1][4 * group + t], 1u << (unit >> 2));
-                        lds.any_bad[step & 1] = 1;
-                    }
-                    if (!used || E == 255u) {
-                        E = 127u;
-                        c.codes[i][t] = 0;
-                    }
-                    scale[t] = scale_of(E);
-                }
-                // group = 4 u + 2 w + h: keys of step u, half h, and of its eight the first or second four (w)
-                const int u = group >> 2, h = group & 1, w = group >> 1 & 1;
+                for (int t = 0; t < 4; ++t) scale[t] = scale_of(c.scales[i] >> (8 * t) & 0xFFu);
+                uint8_t* to = reinterpret_cast<uint8_t*>(to_v) + v_base[i];
                 auto pair = [&](auto byte) __attribute__((always_inline)) {
                     constexpr int kByte = decltype(byte)::value;
                     uint32_t x[4];
@@ -205,10 +227,17 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t which = e ? 0x07060302u : 0x05040100u;
-                        const int column = 8 * unit + 2 * kByte + e, c0 = column >> 7 << 2, f = min(D / 32 - c0, 4), d = column & 127;
-                        const int operand = c0 + d % f, row = d / f;
-                        reinterpret_cast<u32x2*>(&to_v[operand * 4 + u][32 * h + row])[w] =
-                            u32x2{__builtin_amdgcn_perm(x[1], x[0], which), __builtin_amdgcn_perm(x[3], x[2], which)};
+                        // column 8 unit + j -> operand c0 + d mod f, row d / f  (a constant from lane to lane but for heads of 96 and 192)
+                        constexpr int kRun = D % 128 == 0 ? 4 : D == 64 ? 2 : 0;
+                        const int j = 2 * kByte + e;
+                        uint32_t place;
+                        if constexpr (kRun != 0) {
+                            place = (unit >> 4) * (D % 128 == 0 ? 16384 : 0) + (unit & 15) * (8 / kRun * 16) + (j % kRun) * 4096 + j / kRun * 16;
+                        } else {
+                            const uint32_t column = 8 * unit + j, c0 = column >> 7 << 2, f = min(D / 32 - c0, 4u), d = column & 127;
+                            place = (c0 + d % f) * 4096 + d / f * 16;
+                        }
+                        *reinterpret_cast<u32x2*>(to + place) = u32x2{__builtin_amdgcn_perm(x[1], x[0], which), __builtin_amdgcn_perm(x[3], x[2], which)};
                     }
                 };
                 pair(std::integral_constant<int, 0>{});
@@ -249,35 +278,46 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
     auto weigh = [&](int step, int32_t tile) __attribute__((always_inline)) {
         const auto& from = lds.of[step % 3];
         const int32_t key0 = tile * kKvTile;
-        float x[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const int kb = i >> 4, key = 32 * kb + 8 * ((i & 15) >> 2) + (i & 3);  // + 4 half
-            if constexpr (kMbs) {
-                x[i] = sum[kb][0][i & 15] * from.ks[0][key + 4 * half];
-#pragma unroll
-                for (int w = 1; w < P::words; ++w) x[i] += sum[kb][w][i & 15] * from.ks[w][key + 4 * half];
-            } else {
-                x[i] = sum[kb][0][i & 15];
-#pragma unroll
-                for (int w = 1; w < P::words; ++w) x[i] += sum[kb][w][i & 15];
-                x[i] *= a.scale2;
-            }
-        }
         const uint32_t there = __builtin_amdgcn_readfirstlane(from.there);
-        if (!(key0 >= lo_each && key0 + kKvTile <= hi_each && there == 15u)) {
+        const bool whole = key0 >= lo_each && key0 + kKvTile <= hi_each && there == 15u;
+        float x[32];  // scores less `base`
+        auto relative = [&](float base) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                const int in_tile = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3), key = key0 + in_tile + 4 * half;
-                x[i] = key >= lo && key < hi && (there >> (in_tile >> 4) & 1) ? x[i] : -__builtin_inff();
-            }
-        }
-        float top = fmaxf(x[0], x[1]);
+                const int kb = i >> 4, key = 32 * kb + 8 * ((i & 15) >> 2) + (i & 3);  // + 4 half
+                if constexpr (kMbs) {
+                    x[i] = -base;
 #pragma unroll
-        for (int i = 2; i < 32; ++i) top = fmaxf(top, x[i]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__builtin_amdgcn_ballot_w64(top > m + 8.0f)) {
-            const float higher = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - higher);
+                    for (int w = 0; w < P::words; ++w)
+                        x[i] = __builtin_fmaf(sum[kb][w][i & 15], (*reinterpret_cast<const f32x4*>(&from.ks[w][(key & ~3) + 4 * half]))[i & 3], x[i]);
+                } else {
+                    float y = sum[kb][0][i & 15];
+#pragma unroll
+                    for (int w = 1; w < P::words; ++w) y += sum[kb][w][i & 15];
+                    x[i] = __builtin_fmaf(y, a.scale2, -base);
+                }
+            }
+            if (!whole) {
+                // (opaque: the comparisons would be made in front of the branch, for every tile)
+                int32_t from_key = lo - key0 - 4 * half, to_key = hi - key0 - 4 * half, pages = there;
+                asm volatile("" : "+v"(from_key), "+v"(to_key), "+v"(pages));
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int key = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3);
+                    x[i] = key >= from_key && key < to_key && (pages >> (key >> 4) & 1) ? x[i] : -__builtin_inff();
+                }
+            }
+            float top = fmaxf(x[0], x[1]);
+#pragma unroll
+            for (int i = 2; i < 32; ++i) top = fmaxf(top, x[i]);
+            return fmaxf(top, __shfl_xor(top, 32));
+        };
+        // the maximum moves only when a score is 8 (a factor 256) above it, or when it is the row's first
+        const float base = m == kLowest ? 0.0f : m, top = relative(base);
+        const bool moves = top > 8.0f || (m == kLowest && top > kLowest);
+        if (__builtin_amdgcn_ballot_w64(moves)) {
+            const float higher = moves ? base + top : m, shrink = __builtin_amdgcn_exp2f(m - higher);
+            relative(moves ? higher : base);
             m = higher;
             l *= shrink;
 #pragma unroll
@@ -286,15 +326,19 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float y0 = __builtin_amdgcn_exp2f(x[8 * u + 2 * j] - m), y1 = __builtin_amdgcn_exp2f(x[8 * u + 2 * j + 1] - m);
-                l += y0 + y1;
-                if constexpr (kMbs) {
-                    const int key = 16 * u + 8 * (j >> 1) + 2 * (j & 1) + 4 * half;
+            for (int c = 0; c < 2; ++c) {  // keys 16 u + 8 c + 4 half ..
+                f32x4 y;
 #pragma unroll
-                    for (int w = 0; w < P::words; ++w) weight[w][u][j] = pack_bf16(y0 * from.vs[w][key], y1 * from.vs[w][key + 1]);
-                } else {
-                    weight[0][u][j] = pack_bf16(y0, y1);
+                for (int j = 0; j < 4; ++j) {
+                    y[j] = __builtin_amdgcn_exp2f(x[8 * u + 4 * c + j]);
+                    l += y[j];
+                }
+#pragma unroll
+                for (int w = 0; w < (kMbs ? P::words : 1); ++w) {
+                    f32x4 z = y;
+                    if constexpr (kMbs) z *= *reinterpret_cast<const f32x4*>(&from.vs[w][16 * u + 8 * c + 4 * half]);
+                    weight[w][u][2 * c] = pack_bf16(z[0], z[1]);
+                    weight[w][u][2 * c + 1] = pack_bf16(z[2], z[3]);
                 }
             }
         }
