@@ -279,8 +279,8 @@ int mx_gemm_mbs_elem_grouped(mx_elem_t a_elem, const uint8_t* a_codes, const uin
  *   v_codes  [num_pages, Hkv, page_size/4, D/8, 4, 4] 4 neighbouring tokens of 8 codes (4 bytes) each
  *   k_scales, v_scales  [num_pages, Hkv, D/32, page_size]
  *   k_mbs, v_mbs        [num_pages, Hkv, ceil(D/128), page_size], or both NULL: no MBS words
- * Alignment: codes 16 bytes, scales 4 bytes, rows of q, k, v and outputs 16 bytes with leading dimensions (elements from
- * one token's heads to the next one's; a token's heads lie next to each other) a multiple of 8.
+ * Alignment: codes 16 bytes, scales 4 bytes, norm weights and cos_sin 16 bytes, rows of q, k, v and outputs 16 bytes with leading
+ * dimensions (elements from one token's heads to the next one's; a token's heads lie next to each other) a multiple of 8.
  *
  * Indexes that are on the GPU are not trusted with memory: slots outside the cache are not written or read, pages outside
  * it hold no keys, rows outside the query tensor are not touched. */

@@ -20,6 +20,7 @@ namespace mx {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAbreast = 2;  // heads that a wavefront works on at a time: their chains of dependent fp64 operations overlap
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct RowsArgs {
@@ -30,7 +31,7 @@ struct RowsArgs {
     uint16_t *q_out, *k_out;
     KvArrays cache;
     int64_t ldq, ldk, ldv, ldq_out, ldk_out, max_position, places;
-    double eps;
+    double eps, inverse_D;
     int32_t T, Hq, R, rule, per_wave, q_chunks, kv_chunks;
     uint32_t carry, token_groups, waves;
 };
@@ -38,11 +39,34 @@ struct RowsArgs {
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+template <int kControl>
+__device__ __forceinline__ double dpp_lane(double x) {
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)u, kControl, 0xF, 0xF, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(u >> 32), kControl, 0xF, 0xF, true);
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+// Sum over the lanes of a row, the same in all of them (exchanges as for the quantizer's maxima, mx_common.h).
 template <int kLanes>
 __device__ __forceinline__ double row_sum(double x) {
-#pragma unroll
-    for (int m = 1; m < kLanes; m <<= 1) x += __shfl_xor(x, m);
+    x += dpp_lane<0xB1>(x);
+    x += dpp_lane<0x4E>(x);
+    if constexpr (kLanes == 8) return x + dpp_lane<0x141>(x);
+    x += dpp_lane<0x124>(x);
+    x += dpp_lane<0x128>(x);
+    if constexpr (kLanes == 32) x += __shfl_xor(x, 16);
     return x;
+}
+// 1 / sqrt(x) to within a few units of 2^-52: the instruction's estimate (28 bits) and two Newton steps.
+__device__ __forceinline__ double inverse_root(double x) {
+    const double first = __builtin_amdgcn_rsq(x);
+    double r = first;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const double half = 0.5 * r, e = __builtin_fma(-x * r, half, 0.5);  // 1/2 - x r^2 / 2
+        r = __builtin_fma(r, e, r);
+    }
+    return first == 0.0 || __builtin_isinf(first) ? first : r;
 }
 
 // kLanes: of a row.  kTurn: norm, rotation or both are asked for.  kPairs: neighbours are rotated, else halves.  kCache: keys and
@@ -79,99 +103,118 @@ __global__ __launch_bounds__(kThreads) void kv_rows_kernel(RowsArgs a) {
     const int32_t in_page = (int32_t)(place & ((1 << shift) - 1));
 
     const uint16_t* row = x + (int64_t)token * ldx + (int64_t)first * D + j * 8;
-    u32x4 next = {0, 0, 0, 0};
-    if (live) next = *reinterpret_cast<const u32x4*>(row);
+    u32x4 next[kAbreast];
+#pragma unroll
+    for (int c = 0; c < kAbreast; ++c) next[c] = live && c < heads ? *reinterpret_cast<const u32x4*>(row + (int64_t)c * D) : u32x4{0, 0, 0, 0};
 
     // coefficients of the lane's elements and of their partners
     double own[8], other[8];
     int partner = lane;
-    bool normed = false;
+    bool normed = false, rotated = false;
     if constexpr (kTurn) {
         const uint16_t* weight = role == 0 ? a.q_weight : a.k_weight;
         normed = weight != nullptr && role != 2;
         const int half = a.R >> 1, e = j * 8;
         const bool turned = a.cos_sin && e < a.R && live;
+        rotated = turned;
         const bool upper = !kPairs && e >= half;
         if (turned && !kPairs) partner = upper ? lane - half / 8 : lane + half / 8;
         const int pe = e + (partner - (int)lane) * 8;
         const bool known = position < a.max_position;
-        const float* angle = a.cos_sin + (int64_t)(known && turned ? position : 0) * a.R + (kPairs ? e >> 1 : upper ? e - half : e);
+        u32x4 w = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, wp = w;
+        if (normed && live) {
+            w = *reinterpret_cast<const u32x4*>(weight + e);
+            wp = *reinterpret_cast<const u32x4*>(weight + pe);
+        }
+        float c[8] = {1, 1, 1, 1, 1, 1, 1, 1}, s[8] = {};
+        if (turned && known) {
+            const float* angle = a.cos_sin + (int64_t)position * a.R + (kPairs ? e >> 1 : upper ? e - half : e);
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                if (kPairs && i) break;
+                const f32x4 x = *reinterpret_cast<const f32x4*>(angle + i), y = *reinterpret_cast<const f32x4*>(angle + half + i);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) { c[i + t] = x[t]; s[i + t] = y[t]; }
+            }
+        } else if (turned) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = __builtin_nanf("");
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            double c = 1.0, s = 0.0;
-            if (turned) {
-                if (known) {
-                    c = angle[kPairs ? i >> 1 : i];
-                    s = angle[half + (kPairs ? i >> 1 : i)];
-                } else {
-                    c = __builtin_nan("");
-                }
-                if (kPairs ? (i & 1) == 0 : !upper) s = -s;
-            }
-            double w = 1.0, wp = 1.0;
-            if (normed && live) {
-                w = bf16_low(weight[e + i]);
-                wp = bf16_low(weight[kPairs ? e + (i ^ 1) : pe + i]);
-            }
-            own[i] = c * w;
-            other[i] = s * wp;
+            const float own_w = i & 1 ? bf16_high(w[i >> 1]) : bf16_low(w[i >> 1]);
+            const int mate = kPairs ? i ^ 1 : i;
+            const uint32_t mate_w = kPairs ? w[mate >> 1] : wp[mate >> 1];
+            const float other_w = mate & 1 ? bf16_high(mate_w) : bf16_low(mate_w);
+            const double sine = s[kPairs ? i >> 1 : i];
+            own[i] = (double)c[kPairs ? i >> 1 : i] * (double)own_w;
+            other[i] = ((kPairs ? (i & 1) == 0 : !upper) ? -sine : sine) * (double)other_w;
         }
     }
 
-    for (int h = 0; h < heads; ++h) {
-        u32x4 raw = next;
-        if (h + 1 < heads && live) next = *reinterpret_cast<const u32x4*>(row + (int64_t)(h + 1) * D);
+    auto turn = [&](u32x4 raw) __attribute__((always_inline)) -> u32x4 {
+        double r = 1.0;
+        if (normed) {
+            double sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const double lo = bf16_low(raw[i]), hi = bf16_high(raw[i]);
+                sum = __builtin_fma(lo, lo, sum);
+                sum = __builtin_fma(hi, hi, sum);
+            }
+            r = inverse_root(__builtin_fma(row_sum<kLanes>(sum), a.inverse_D, a.eps));
+        }
+        u32x4 mate = raw;
+        if (!kPairs && a.cos_sin) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mate[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(partner * 4, (int)raw[i]);
+        }
+        u32x4 turned;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const double lo = bf16_low(raw[i]), hi = bf16_high(raw[i]);
+            double y0 = lo * own[2 * i], y1 = hi * own[2 * i + 1];
+            if (rotated) {  // (else 0 times an infinity would not be 0)
+                const double mlo = bf16_low(mate[i]), mhi = bf16_high(mate[i]);
+                y0 = __builtin_fma(kPairs ? mhi : mlo, other[2 * i], y0);
+                y1 = __builtin_fma(kPairs ? mlo : mhi, other[2 * i + 1], y1);
+            }
+            turned[i] = pack_bf16((float)(y0 * r), (float)(y1 * r));
+        }
+        return turned;
+    };
+    for (int h0 = 0; h0 < heads; h0 += kAbreast) {
+        u32x4 raw[kAbreast];
+#pragma unroll
+        for (int c = 0; c < kAbreast; ++c) {
+            raw[c] = next[c];
+            if (h0 + kAbreast + c < heads && live) next[c] = *reinterpret_cast<const u32x4*>(row + (int64_t)(h0 + kAbreast + c) * D);
+        }
         if constexpr (kTurn) {
             if (role != 2) {
-                double r = 1.0;
-                if (normed) {
-                    double sum = 0.0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const double lo = bf16_low(raw[i]), hi = bf16_high(raw[i]);
-                        sum = __builtin_fma(lo, lo, sum);
-                        sum = __builtin_fma(hi, hi, sum);
-                    }
-                    r = 1.0 / __builtin_sqrt(row_sum<kLanes>(sum) / D + a.eps);
-                }
-                u32x4 mate = raw;
-                if (!kPairs && a.cos_sin) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mate[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(partner * 4, (int)raw[i]);
-                }
-                u32x4 turned;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const double lo = bf16_low(raw[i]), hi = bf16_high(raw[i]);
-                    double y0 = lo * own[2 * i], y1 = hi * own[2 * i + 1];
-                    // (no partner: 0 times an infinity would not be 0)
-                    if (kPairs || partner != (int)lane) {
-                        const double mlo = bf16_low(mate[i]), mhi = bf16_high(mate[i]);
-                        if (!kPairs || (a.cos_sin && j * 8 < a.R)) {
-                            y0 = __builtin_fma(kPairs ? mhi : mlo, other[2 * i], y0);
-                            y1 = __builtin_fma(kPairs ? mlo : mhi, other[2 * i + 1], y1);
-                        }
-                    }
-                    turned[i] = pack_bf16((float)(y0 * r), (float)(y1 * r));
-                }
-                raw = turned;
+                for (int c = 0; c < kAbreast; ++c) raw[c] = turn(raw[c]);
             }
         }
-        if (out && live) *reinterpret_cast<u32x4*>(out + (int64_t)token * ldo + (int64_t)(first + h) * D + j * 8) = raw;
-        if constexpr (kCache) {
-            if (role != 0) {
-                if (!live) raw = u32x4{0, 0, 0, 0};  // (inactive lanes of a window)
-                const ChunkResult res = quantize_chunk<true, kMbs, kLanes == 8 ? 8 : 16>(raw, a.rule, a.carry);
-                if (cached) {
-                    const int head = first + h;
-                    const KvLayout& at = a.cache.at;
-                    if (role == 1) {
-                        *reinterpret_cast<uint32_t*>(a.cache.k_codes + at.k_block(page, head, j >> 2, in_page) + (j & 3) * 4) = res.codes;
-                    } else {
-                        *reinterpret_cast<uint32_t*>(a.cache.v_codes + at.v_unit(page, head, j, in_page)) = res.codes;
+#pragma unroll
+        for (int c = 0; c < kAbreast; ++c) {
+            const int head = first + h0 + c;
+            if (h0 + c >= heads) continue;  // wave-uniform
+            if (out && live) *reinterpret_cast<u32x4*>(out + (int64_t)token * ldo + (int64_t)head * D + j * 8) = raw[c];
+            if constexpr (kCache) {
+                if (role != 0) {
+                    if (!live) raw[c] = u32x4{0, 0, 0, 0};  // (inactive lanes of a window)
+                    const ChunkResult res = quantize_chunk<true, kMbs, kLanes == 8 ? 8 : 16>(raw[c], a.rule, a.carry);
+                    if (cached) {
+                        const KvLayout& at = a.cache.at;
+                        if (role == 1) {
+                            *reinterpret_cast<uint32_t*>(a.cache.k_codes + at.k_block(page, head, j >> 2, in_page) + (j & 3) * 4) = res.codes;
+                        } else {
+                            *reinterpret_cast<uint32_t*>(a.cache.v_codes + at.v_unit(page, head, j, in_page)) = res.codes;
+                        }
+                        if ((j & 3) == 0) (role == 1 ? a.cache.k_scales : a.cache.v_scales)[at.scale(page, head, j >> 2, in_page)] = (uint8_t)res.E;
+                        if (kMbs && (j & 15) == 0) (role == 1 ? a.cache.k_mbs : a.cache.v_mbs)[at.word(page, head, j >> 4, in_page)] = (uint8_t)res.m8;
                     }
-                    if ((j & 3) == 0) (role == 1 ? a.cache.k_scales : a.cache.v_scales)[at.scale(page, head, j >> 2, in_page)] = (uint8_t)res.E;
-                    if (kMbs && (j & 15) == 0) (role == 1 ? a.cache.k_mbs : a.cache.v_mbs)[at.word(page, head, j >> 4, in_page)] = (uint8_t)res.m8;
                 }
             }
         }
@@ -229,9 +272,9 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
 
 inline int lanes_of(int D) { return D <= 64 ? 8 : D <= 128 ? 16 : 32; }
 
-// Heads that a wavefront takes one after the other: one where the launch is small (its latency is what counts), four where it
+// Heads that a wavefront takes one after the other: one where the launch is small (its latency is what counts), eight where it
 // fills the device several times.
-inline int heads_per_wave(int64_t rows_of_waves) { return rows_of_waves > 16384 ? 4 : 1; }
+inline int heads_per_wave(int64_t rows_of_waves) { return rows_of_waves > 32768 ? 8 : rows_of_waves > 8192 ? 4 : 1; }
 
 template <int kLanes, bool kTurn, bool kPairs>
 void launch_rows(const RowsArgs& a, bool cache, bool mbs, dim3 grid, hipStream_t s) {
@@ -251,6 +294,7 @@ int run_rows(RowsArgs a, bool turn, bool pairs, bool cache, hipStream_t stream) 
     const int lanes = lanes_of(a.cache.at.D), tokens = kWave / lanes;
     a.token_groups = (uint32_t)((a.T + (int64_t)tokens - 1) / tokens);
     a.carry = rule_carry(a.rule);
+    a.inverse_D = 1.0 / a.cache.at.D;
     a.per_wave = heads_per_wave((int64_t)a.token_groups * (a.Hq + 2 * (int64_t)a.cache.at.heads));
     a.q_chunks = (a.Hq + a.per_wave - 1) / a.per_wave;
     a.kv_chunks = (a.cache.at.heads + a.per_wave - 1) / a.per_wave;
@@ -281,7 +325,7 @@ int check_turn(const RowsArgs& a, mx_rope_t style, int64_t T, int64_t Hq, int64_
     if ((a.cos_sin != nullptr) != (R != 0)) return MX_EINVAL;
     if (a.cos_sin && !a.positions) return MX_ENULL;
     if ((Hq && (!good_rows(a.q, a.ldq) || !good_rows(a.q_out, a.ldq_out))) || (Hkv && !good_rows(a.k, a.ldk))) return MX_EALIGN;
-    if (!aligned(a.cos_sin, 4) || !aligned(a.q_weight, 2) || !aligned(a.k_weight, 2) || !aligned(a.positions, 4)) return MX_EALIGN;
+    if (!aligned(a.cos_sin, 16) || !aligned(a.q_weight, 16) || !aligned(a.k_weight, 16) || !aligned(a.positions, 4)) return MX_EALIGN;
     return MX_OK;
 }
 

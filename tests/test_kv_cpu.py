@@ -73,7 +73,7 @@ BAD_CACHE = [(dict(kc=None), ENULL), (dict(vs=None), ENULL), (dict(km=None), EIN
 BAD_TURN = [(dict(T=-1), EINVAL), (dict(T=1 << 31), EINVAL), (dict(Hq=-1), EINVAL), (dict(ldq=1016), EINVAL), (dict(ldk=248), EINVAL), (dict(ldqo=8), EINVAL),
             (dict(q=None), ENULL), (dict(k=None), ENULL), (dict(q_out=None), ENULL), (dict(positions=None), ENULL), (dict(table=None), EINVAL), (dict(R=0), EINVAL),
             (dict(R=144), EINVAL), (dict(R=24), EUNSUPPORTED), (dict(style=2), EINVAL), (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL),
-            (dict(q=A + 8), EALIGN), (dict(ldk=260), EALIGN), (dict(most=-1), EINVAL), (dict(D=144), EUNSUPPORTED)]
+            (dict(q=A + 8), EALIGN), (dict(ldk=260), EALIGN), (dict(table=A + 8), EALIGN), (dict(kw=A + 2), EALIGN), (dict(most=-1), EINVAL), (dict(D=144), EUNSUPPORTED)]
 
 
 @pytest.mark.parametrize("name, base, bad", [
