@@ -74,15 +74,20 @@ __device__ __forceinline__ u32x4 expand8(uint32_t codes, float scale) {
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-// Largest (sum) over the four lanes with the same lane mod 16.
-__device__ __forceinline__ float column_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+// Both values that lanes l and l ^ 32 (l ^ 16) hold, in both: the swaps of the vector ALU, without the LDS crossbar's latency.
+__device__ __forceinline__ f32x2 both32(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
-__device__ __forceinline__ float column_sum(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+__device__ __forceinline__ f32x2 both16(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
+// Largest (sum) over the two lanes with the same lane mod 32, and over the four with the same lane mod 16.
+__device__ __forceinline__ float pair_max(float x) { const f32x2 y = both32(x); return fmaxf(y[0], y[1]); }
+__device__ __forceinline__ float pair_sum(float x) { const f32x2 y = both32(x); return y[0] + y[1]; }
+__device__ __forceinline__ float column_max(float x) { const f32x2 y = both16(x); return pair_max(fmaxf(y[0], y[1])); }
+__device__ __forceinline__ float column_sum(float x) { const f32x2 y = both16(x); return pair_sum(y[0] + y[1]); }
 __device__ __forceinline__ float scale_of(uint32_t E) { return __uint_as_float(E << 23); }
 __device__ __forceinline__ float sigma_of(uint32_t m8) { return __builtin_amdgcn_rcpf(__uint_as_float(0x3F800000u | (m8 << 15))); }
 

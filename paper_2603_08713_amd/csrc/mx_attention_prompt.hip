@@ -310,7 +310,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
             float top = fmaxf(x[0], x[1]);
 #pragma unroll
             for (int i = 2; i < 32; ++i) top = fmaxf(top, x[i]);
-            return fmaxf(top, __shfl_xor(top, 32));
+            return pair_max(top);
         };
         // the maximum moves only when a score is 8 (a factor 256) above it, or when it is the row's first
         const float base = m == kLowest ? 0.0f : m, top = relative(base);
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
         }
     }
 
-    l += __shfl_xor(l, 32);
+    l = pair_sum(l);
     if (!real) return;
     const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
     const int64_t t = r.first + token;
