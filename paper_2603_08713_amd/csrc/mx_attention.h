@@ -39,13 +39,17 @@ struct AttentionArgs {
     int32_t num_pages, max_pages, room;
     int32_t S, T, Hq, group;  // group: query heads of a key head
     int32_t window, causal;
-    int32_t workers_log2;     // wavefronts that the batch is cut for
+    int32_t workers_log2;     // wavefronts that the batch is cut for (few rows)
+    int32_t splits;           // most pieces of a row tile's keys (many rows)
+    int64_t row_tiles;        // of a key head, at most (many rows)
     float scale2;             // scale * log2(e)
 };
 
-// kernel of mx_attention_prompt.hip, and row tiles that its launch makes of a key head
+// kernels of mx_attention_prompt.hip, and row tiles that they make of a key head
 int launch_attention_prompt(const AttentionArgs& a, hipStream_t stream);
+int64_t attention_prompt_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
 int64_t prompt_row_tiles(int64_t S, int64_t T, int64_t group, int64_t D);
+int64_t prompt_height(int64_t D);  // rows of a tile
 
 // kernels of mx_attention_rows.hip
 int launch_attention_rows(const AttentionArgs& a, hipStream_t stream);
@@ -133,6 +137,58 @@ struct HeadShape {
     static constexpr int start(int p) { return p < full ? 128 * p : p == full && half ? 128 * full : 128 * full + 64 * half; }
     static constexpr int width(int p) { return p < full ? 128 : p == full && half ? 64 : 32; }
 };
+
+// A row from its parts, row `at` of each: part(i) has the maxima of kHeight rows, their sums, their O.  kWaves wavefronts (of a workgroup
+// of that many, or one of four) do it: lanes have 4 columns each, and the parts are dealt to the groups of lanes.
+template <int D, int kHeight, int kWaves, typename F>
+__device__ __forceinline__ void join_parts(const AttentionArgs& a, int32_t t, int h, int32_t at, int32_t count, F&& part) {
+    constexpr int kQuads = D / 4, kSides = 64 / kQuads, kDeal = kSides * kWaves;
+    __shared__ f32x4 sums[kWaves > 1 ? kWaves : 1][kQuads];
+    __shared__ float weights[kWaves > 1 ? kWaves : 1];
+    const int lane = threadIdx.x & 63, wave = kWaves > 1 ? uniform(threadIdx.x >> 6) : 0;
+    float m = kLowest;
+    for (int i = lane; i < count; i += 64) m = fmaxf(m, part(i)[at]);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+    float l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    const int side = lane / kQuads, quad = lane - side * kQuads;
+    if (side < kSides) {
+#pragma unroll 8
+        for (int i = wave * kSides + side; i < count; i += kDeal) {
+            const float* s = part(i);
+            const float w = __builtin_amdgcn_exp2f(s[at] - m);
+            l += w * s[kHeight + at];
+            o += w * *reinterpret_cast<const f32x4*>(s + 2 * kHeight + at * D + 4 * quad);
+        }
+    }
+    const float own_l = l;
+    const f32x4 own = o;
+#pragma unroll
+    for (int x = 1; x < kSides; ++x) {  // (only the first side's sums are used)
+        const int from = (lane + x * kQuads) & 63;
+        l += __shfl(own_l, from);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] += __shfl(own[c], from);
+    }
+    if constexpr (kWaves > 1) {
+        if (side == 0) sums[wave][quad] = o;
+        if (lane == 0) weights[wave] = l;
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+            if (side == 0) o += sums[w][quad];
+            l += weights[w];
+        }
+    }
+    if (side == 0) {
+        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+        *reinterpret_cast<u32x2*>(a.out + (int64_t)t * a.ldo + (int64_t)h * D + 4 * quad) =
+            u32x2{pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse)};
+        if (a.lse && lane == 0) a.lse[(int64_t)t * a.Hq + h] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
+    }
+}
 
 }  // namespace
 }  // namespace mx

@@ -9,17 +9,19 @@ bool good_shape(int64_t S, int64_t T, int64_t Hq, int64_t Hkv) {
     return S >= 0 && T >= 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && S <= kKvMost && T <= kKvMost && Hq <= kKvMostHeads;
 }
 
-// Many rows a key head: tiles of 256 rows that share a tile of expanded keys, as far as they fill the device.
+// Whether the kernel for many rows takes a call.  It expands a key once for 256 rows (heads above 128: 128) where the one for few rows
+// does for 16 to 64, but pays for a whole tile of rows and needs tiles enough for the compute units.  Few against many, us, at 8 key
+// heads of 128: one request behind 8192 keys, 256 rows a head 42 / 41, 512 rows 54 / 49, 4096 rows 292 / 206; 16 requests behind 2000
+// keys, 64 rows 44 / 64, 128 rows 57 / 57, 256 rows 88 / 85; 8 behind 4000, 256 rows 88 / 98; 64 behind 2000, 128 rows 177 / 141.
 bool is_prompt(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
-    const int64_t group = Hq / Hkv;
-    return T * group > 64 * S && prompt_row_tiles(0, T, group, D) * Hkv >= 128;
+    const int64_t rows = T * (Hq / Hkv), tiles = rows / prompt_height(D) * Hkv;
+    return (rows >= 512 * S && tiles >= 16) || (rows > 64 * S && tiles >= 128);
 }
 
-}  // namespace
-}  // namespace mx
-
-namespace mx {
-namespace {
+int64_t workspace_of(bool prompt, int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    if (!S || !T) return 0;
+    return prompt ? attention_prompt_workspace(S, T, Hq, Hkv, D) : attention_rows_workspace(S, T, Hq, Hkv, D);
+}
 
 // force: 0 = the kernel that is_prompt picks, 1 = the one for few rows, 2 = the one for many
 int attention(int force, const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,
@@ -36,7 +38,7 @@ int attention(int force, const void* q_bf16, int64_t ldq, const int64_t* row_off
         !aligned(block_table, 4) || !aligned(lse_or_null, 4) || !aligned(workspace, 16))
         return MX_EALIGN;
     const bool prompt = force ? force == 2 : is_prompt(num_seqs, T, Hq, Hkv, D);
-    const int64_t need = prompt ? 0 : attention_rows_workspace(num_seqs, T, Hq, Hkv, D);
+    const int64_t need = workspace_of(prompt, num_seqs, T, Hq, Hkv, D);
     if (workspace_bytes < need) return MX_EINVAL;
     if (need && !workspace) return MX_ENULL;
     if (int st = check_device()) return st;
@@ -77,7 +79,7 @@ extern "C" int64_t mx_attention_kv_workspace(int64_t num_seqs, int64_t T, int64_
     using namespace mx;
     if (!good_shape(num_seqs, T, Hq, Hkv)) return MX_EINVAL;
     if (!kv_head_dim(D)) return MX_EUNSUPPORTED;
-    return num_seqs && T && !is_prompt(num_seqs, T, Hq, Hkv, D) ? attention_rows_workspace(num_seqs, T, Hq, Hkv, D) : 0;
+    return workspace_of(is_prompt(num_seqs, T, Hq, Hkv, D), num_seqs, T, Hq, Hkv, D);
 }
 
 extern "C" int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,
@@ -105,5 +107,5 @@ extern "C" int mx_internal_attention_kv(int force, const void* q_bf16, int64_t l
 extern "C" int64_t mx_internal_attention_kv_workspace(int force, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
     using namespace mx;
     const int64_t size = mx_attention_kv_workspace(num_seqs, T, Hq, Hkv, D);
-    return size < 0 || !num_seqs || !T || force == 0 ? size : force == 1 ? attention_rows_workspace(num_seqs, T, Hq, Hkv, D) : 0;
+    return size < 0 || force == 0 ? size : workspace_of(force == 2, num_seqs, T, Hq, Hkv, D);
 }

@@ -50,6 +50,48 @@ struct PromptLds {
     uint32_t bad[2][kKvTile], any_bad[2];  // blocks of a value that are NaN, and whether any is
 };
 
+// A row tile of the batch: whose it is, and its pieces of keys.
+struct RowTile {
+    KvRequest r;
+    int32_t s, row_tile;
+    int64_t index;  // among all
+    __device__ __forceinline__ int32_t tiles(const AttentionArgs& a, int height) const {
+        const int32_t row0 = row_tile * height, row_last = min(row0 + height, r.rows * a.group) - 1;
+        const int32_t begin = r.lo(row0 / a.group, a.window) / kKvTile, end = (r.hi(row_last / a.group, a.causal) + kKvTile - 1) / kKvTile;
+        return max(end - begin, 0);
+    }
+    __device__ __forceinline__ int32_t pieces(const AttentionArgs& a, int height) const { return kv_pieces(tiles(a, height), a.splits); }
+};
+// The row tile that stands `from_end` from the batch's last, or (row >= 0) the one with the first query head of the key head of query row `row`.
+template <int kHeight>
+__device__ __forceinline__ RowTile find_row_tile(const AttentionArgs& a, int64_t from_end, int32_t row) {
+    const int lane = threadIdx.x & 63;
+    int64_t total = 0;
+    if (row < 0)
+        for (int s0 = (a.S - 1) / 64 * 64; s0 >= 0; s0 -= 64) total += read_lane(wave_scan((int64_t)request_of(a, s0 + lane).row_tiles(a.group, kHeight)), 63);
+    const int64_t tile = total - 1 - from_end;
+    RowTile found = {};
+    found.s = -1;
+    if (row < 0 && tile < 0) return found;
+    int64_t before = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        const KvRequest x = request_of(a, s0 + lane);
+        const int64_t mine = x.row_tiles(a.group, kHeight), end = before + wave_scan(mine);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(row < 0 ? end > tile : row >= x.first && row < x.first + x.rows);
+        if (hit) {
+            const int at = __builtin_ctzll(hit);
+            found.s = s0 + at;
+            found.r = KvRequest{read_lane(x.first, at), read_lane(x.rows, at), read_lane(x.pos0, at), read_lane(x.keys, at)};
+            found.index = read_lane(end, at) - read_lane(mine, at);  // of the request's first
+            found.row_tile = row < 0 ? (int32_t)(tile - found.index) : 0;
+            found.index += found.row_tile;
+            return found;
+        }
+        before = read_lane(end, 63);
+    }
+    return found;
+}
+
 // One wavefront's share of a tile's codes, in flight.
 template <int D, bool kMbs>
 struct PromptCodes {
@@ -67,38 +109,20 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
     const int heads = a.cache.at.heads, shift = a.cache.at.page_shift;
     const int head = blockIdx.x % heads;  // (the row tiles of one key head on one XCD, as far as the heads are 8 or so)
-
-    // the request and row tile: the last of the batch first, for under the causal rule a request's last rows see most
-    KvRequest r;
-    int32_t s = -1, row_tile = 0;
-    {
-        int64_t total = 0;
-        for (int s0 = (a.S - 1) / 64 * 64; s0 >= 0; s0 -= 64) {
-            const KvRequest x = request_of(a, s0 + lane);
-            total += read_lane(wave_scan(x.row_tiles(a.group, P::rows)), 63);
-        }
-        const int64_t tile = total - 1 - blockIdx.x / heads;
-        if (tile < 0) return;
-        int64_t before = 0;
-        for (int s0 = 0; s0 < a.S; s0 += 64) {
-            const KvRequest x = request_of(a, s0 + lane);
-            const int64_t mine = x.row_tiles(a.group, P::rows), end = before + wave_scan(mine);
-            const uint64_t hit = __builtin_amdgcn_ballot_w64(end > tile);
-            if (hit) {
-                const int at = __builtin_ctzll(hit);
-                s = s0 + at;
-                row_tile = (int32_t)(tile - (read_lane(end, at) - read_lane(mine, at)));
-                r = KvRequest{read_lane(x.first, at), read_lane(x.rows, at), read_lane(x.pos0, at), read_lane(x.keys, at)};
-                break;
-            }
-            before = read_lane(end, 63);
-        }
-        if (s < 0) return;
-    }
+    const int32_t number = blockIdx.x / heads, split = number % a.splits;
+    // the last row tile of the batch first: under the causal rule a request's last rows see most
+    const RowTile which = find_row_tile<P::rows>(a, number / a.splits, -1);
+    if (which.s < 0) return;
+    const int32_t s = which.s, row_tile = which.row_tile;
+    const KvRequest& r = which.r;
     const int32_t rows = r.rows * a.group;
     const int32_t row0 = row_tile * P::rows, row_last = min(row0 + P::rows, rows) - 1;
     const int32_t lo_all = r.lo(row0 / a.group, a.window), hi_all = r.hi(row_last / a.group, a.causal);
-    const int32_t tile0 = lo_all / kKvTile, tile_end = (hi_all + kKvTile - 1) / kKvTile;
+    // this piece of the tiles that the rows see
+    const int32_t pieces = which.pieces(a, P::rows);
+    if (split >= pieces || which.index >= a.row_tiles) return;  // (offsets that overlap make more row tiles than there is room for)
+    const int32_t all_begin = lo_all / kKvTile, all = which.tiles(a, P::rows);
+    const int32_t tile0 = all_begin + kv_piece_begin(all, pieces, split), tile_end = all_begin + kv_piece_begin(all, pieces, split + 1);
     // the wavefront's rows: keys that some of them sees, and that all of them see
     const int32_t my_row = row0 + 32 * wave + n;
     const bool real = my_row < rows;
@@ -431,46 +455,100 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
 
     l = pair_sum(l);
     if (!real) return;
-    const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
     const int64_t t = r.first + token;
-    if (a.lse && half == 0) a.lse[t * a.Hq + q_head] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
-    uint16_t* out = a.out + t * a.ldo + (int64_t)q_head * D;
+    // the lane's runs of neighbouring columns: f(first column, values), 4 at a time
+    auto each_run = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < P::columns; c += 4) {
-        constexpr int kMost = 16;
-        const int f = P::run(c);
+        for (int c = 0; c < P::columns; c += 4) {
+            const int run = P::run(c);
 #pragma unroll
-        for (int i0 = 0; i0 < 16; i0 += 4) {
-            float y[kMost];
+            for (int i0 = 0; i0 < 16; i0 += 4) {
+                float y[16];
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+                for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e < f) y[f * b + e] = o[c + e < P::columns ? c + e : 0][i0 + b] * inverse;
-            uint16_t* to = out + 32 * c + f * (2 * i0 + 4 * half);
+                    for (int e = 0; e < 4; ++e)
+                        if (e < run) y[run * b + e] = o[c + e < P::columns ? c + e : 0][i0 + b];
 #pragma unroll
-            for (int e = 0; e < 4 * f; e += 4) *reinterpret_cast<u32x2*>(to + e) = u32x2{pack_bf16(y[e], y[e + 1]), pack_bf16(y[e + 2], y[e + 3])};
+                for (int e = 0; e < 4 * run; e += 4) f(32 * c + run * (2 * i0 + 4 * half) + e, f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]});
+            }
         }
+    };
+    if (pieces == 1) {
+        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+        if (a.lse && half == 0) a.lse[t * a.Hq + q_head] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
+        uint16_t* out = a.out + t * a.ldo + (int64_t)q_head * D;
+        each_run([&](int d, f32x4 y) __attribute__((always_inline)) {
+            *reinterpret_cast<u32x2*>(out + d) = u32x2{pack_bf16(y[0] * inverse, y[1] * inverse), pack_bf16(y[2] * inverse, y[3] * inverse)};
+        });
+    } else {
+        float* slot = a.partial + ((which.index * heads + head) * a.splits + split) * (int64_t)(P::rows * (D + 2));
+        const int32_t in_tile = my_row - row0;
+        if (half == 0) {
+            slot[in_tile] = m;
+            slot[P::rows + in_tile] = l;
+        }
+        float* to = slot + 2 * P::rows + in_tile * D;
+        each_run([&](int d, f32x4 y) __attribute__((always_inline)) { *reinterpret_cast<f32x4*>(to + d) = y; });
     }
 }
 
+// Rows whose keys were cut into pieces: a wavefront a row.
+template <int D>
+__global__ __launch_bounds__(256) void attention_prompt_join_kernel(AttentionArgs a) {
+    constexpr int kHeight = PromptShape<D>::rows;
+    const int64_t id = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
+    const int32_t t = uniform((int32_t)((uint32_t)id / (uint32_t)a.Hq));
+    const int h = (int)(id - (int64_t)t * a.Hq), heads = a.cache.at.heads, head = h / a.group;
+    if (t >= a.T) return;
+    RowTile which = find_row_tile<kHeight>(a, 0, t);
+    if (which.s < 0) return;
+    const int32_t row = (t - which.r.first) * a.group + (h - head * a.group);
+    which.row_tile = row / kHeight;
+    which.index += which.row_tile;
+    const int32_t pieces = which.pieces(a, kHeight);
+    if (pieces == 1 || which.index >= a.row_tiles) return;
+    const float* first = a.partial + ((which.index * heads + head) * a.splits) * (int64_t)(kHeight * (D + 2));
+    join_parts<D, kHeight, 1>(a, t, h, row - which.row_tile * kHeight, pieces,
+                              [&](int32_t i) __attribute__((always_inline)) { return first + (int64_t)i * (kHeight * (D + 2)); });
+}
+
+// Pieces of the keys, where the row tiles alone leave compute units without one: what fits one round of workgroups, with half a
+// partial tile for each of several requests.  (One request of 4096 rows a
+// key head behind 8192 keys, 128 row tiles: 321 us whole, 206 in two pieces.)
+int splits_of(int64_t S, int64_t T, int64_t group, int64_t heads, int64_t D) {
+    const int64_t height = prompt_height(D), groups = ((T * group + height - 1) / height + S / 2) * heads;
+    return groups <= 128 ? (int)(256 / groups) : 1;
+}
+
 template <int D, bool kMbs>
-int launch_prompt(const AttentionArgs& a, hipStream_t s) {
+int launch_prompt(const AttentionArgs& args, hipStream_t s) {
     using P = PromptShape<D>;
     constexpr int kBytes = sizeof(PromptLds<D>);
     static LdsOptIn opt_in;
     if (int st = opt_in.ensure(reinterpret_cast<const void*>(&attention_prompt_kernel<D, kMbs>), kBytes)) return st;
-    const int64_t groups = prompt_row_tiles(a.S, a.T, a.group, D) * a.cache.at.heads;
-    if (groups >= (int64_t)1 << 23) return MX_EINVAL;  // (a launch of fewer than 2^32 work-items)
+    AttentionArgs a = args;
+    a.splits = splits_of(a.S, a.T, a.group, a.cache.at.heads, D);
+    a.row_tiles = prompt_row_tiles(a.S, a.T, a.group, D);
+    const int64_t groups = a.row_tiles * a.cache.at.heads * a.splits, rows = (int64_t)a.T * a.Hq;
+    if (groups >= (int64_t)1 << 23 || rows >= (int64_t)1 << 26) return MX_EINVAL;  // (launches of fewer than 2^32 work-items)
     hipLaunchKernelGGL((attention_prompt_kernel<D, kMbs>), dim3((unsigned)groups), dim3(P::threads), kBytes, s, a);
+    if (int st = launch_status()) return st;
+    if (a.splits > 1) hipLaunchKernelGGL((attention_prompt_join_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
     return launch_status();
 }
 
 }  // namespace
 
+int64_t prompt_height(int64_t D) { return D <= 128 ? PromptShape<128>::rows : PromptShape<256>::rows; }
+
 int64_t prompt_row_tiles(int64_t S, int64_t T, int64_t group, int64_t D) {
-    const int64_t rows = D <= 128 ? PromptShape<128>::rows : PromptShape<256>::rows;
-    return S + (T * group + rows - 1) / rows;  // one partial tile a request at most
+    return S + (T * group + prompt_height(D) - 1) / prompt_height(D);  // one partial tile a request at most
+}
+
+int64_t attention_prompt_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    const int64_t splits = splits_of(S, T, Hq / Hkv, Hkv, D);
+    return splits > 1 ? prompt_row_tiles(S, T, Hq / Hkv, D) * Hkv * splits * prompt_height(D) * (D + 2) * 4 : 0;
 }
 
 int launch_attention_prompt(const AttentionArgs& a, hipStream_t stream) {

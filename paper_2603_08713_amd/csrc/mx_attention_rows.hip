@@ -554,13 +554,11 @@ __global__ __launch_bounds__(kThreads, (kWorkersLog2<D, kTiles> - 9)) void atten
     }
 }
 
-// Rows that were cut into pieces, kWaves wavefronts a row: lanes have 4 columns each and the parts are dealt to the groups of lanes.
+// Rows that were cut into pieces, kWaves wavefronts a row.
 template <int D, int kTiles, int kWaves>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionArgs a) {
-    constexpr int kHeight = 16 * kTiles, kQuads = D / 4, kSides = 64 / kQuads, kDeal = kSides * kWaves;
-    __shared__ f32x4 sums[kWaves > 1 ? kWaves : 1][kQuads];
-    __shared__ float weights[kWaves > 1 ? kWaves : 1];
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), part_of_row = kWaves > 1 ? wave : 0;
+    constexpr int kHeight = 16 * kTiles;
+    const int wave = uniform(threadIdx.x >> 6);
     const int64_t id = kWaves > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kWavesInGroup + wave;
     const int32_t t = uniform((int32_t)((uint32_t)id / (uint32_t)a.Hq));
     const int h = (int)(id - (int64_t)t * a.Hq);
@@ -573,53 +571,10 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionArgs 
     const int32_t row = (t - r.first) * a.group + (h - head * a.group), row_tile = row / kHeight, at = row - row_tile * kHeight;
     const int64_t item_at = read_lane(batch.end, who) - read_lane(batch.size, who) + (int64_t)(head * row_tiles + row_tile) * item;
     const KvLine::Parts parts = KvLine::parts(item_at, item, batch.share);
-    const int32_t count = parts.count;
-    if (count == 1) return;
-    auto part = [&](int32_t i) __attribute__((always_inline)) {
+    if (parts.count == 1) return;
+    join_parts<D, kHeight, kWaves>(a, t, h, at, parts.count, [&](int32_t i) __attribute__((always_inline)) {
         return a.partial + (int64_t)(2 * (parts.first + i) + (i == 0 ? parts.late : 0)) * kPartFloats<D, kTiles>;
-    };
-    float m = kLowest;
-    for (int i = lane; i < count; i += 64) m = fmaxf(m, part(i)[at]);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-    float l = 0.0f;
-    f32x4 o = {0, 0, 0, 0};
-    const int side = lane / kQuads, quad = lane - side * kQuads;
-    if (side < kSides) {
-#pragma unroll 8
-        for (int i = part_of_row * kSides + side; i < count; i += kDeal) {
-            const float* s = part(i);
-            const float w = __builtin_amdgcn_exp2f(s[at] - m);
-            l += w * s[kHeight + at];
-            o += w * *reinterpret_cast<const f32x4*>(s + 2 * kHeight + at * D + 4 * quad);
-        }
-    }
-    const float own_l = l;
-    const f32x4 own = o;
-#pragma unroll
-    for (int x = 1; x < kSides; ++x) {  // (only the first side's sums are used)
-        const int from = (lane + x * kQuads) & 63;
-        l += __shfl(own_l, from);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] += __shfl(own[c], from);
-    }
-    if constexpr (kWaves > 1) {
-        if (side == 0) sums[wave][quad] = o;
-        if (lane == 0) weights[wave] = l;
-        __syncthreads();
-        if (wave) return;
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) {
-            if (side == 0) o += sums[w][quad];
-            l += weights[w];
-        }
-    }
-    if (side == 0) {
-        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
-        *reinterpret_cast<u32x2*>(a.out + (int64_t)t * a.ldo + (int64_t)h * D + 4 * quad) =
-            u32x2{pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse)};
-        if (a.lse && lane == 0) a.lse[(int64_t)t * a.Hq + h] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
-    }
+    });
 }
 
 // Two row tiles where most requests bring more than one tile's rows.  (Heads above 128 keep to one: two do not fit the registers.)

@@ -117,4 +117,9 @@ struct KvLine {
     }
 };
 
+// Pieces that the keys of a row tile (of many rows) are cut into, `tiles` of them: at most `most`, of four tiles at least; and where piece i
+// begins.
+MX_HD int32_t kv_pieces(int32_t tiles, int32_t most) { return kv_max(1, kv_min(most, tiles / 4)); }
+MX_HD int32_t kv_piece_begin(int32_t tiles, int32_t pieces, int32_t i) { return (int32_t)((int64_t)tiles * i / pieces); }
+
 }  // namespace mx

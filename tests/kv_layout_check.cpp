@@ -134,6 +134,12 @@ int main() {
                     for (int32_t room : {0, 16, 1 << 30})
                         for (int32_t window : {0, 1, 100, 1 << 30}) request(begin, end, len < INT32_MIN || len > INT32_MAX ? 5 : len, T, room, window, window || (begin & 1), false);
     for (int i = 0; i < 2000; ++i) batch(rng);
+    for (int tiles = 0; tiles < 300; ++tiles)
+        for (int most = 1; most <= 64; ++most) {
+            const int pieces = kv_pieces(tiles, most);
+            CHECK(pieces >= 1 && pieces <= most && kv_piece_begin(tiles, pieces, 0) == 0 && kv_piece_begin(tiles, pieces, pieces) == tiles, "pieces");
+            for (int i = 0; i < pieces && pieces > 1; ++i) CHECK(kv_piece_begin(tiles, pieces, i + 1) - kv_piece_begin(tiles, pieces, i) >= 4, "a short piece");
+        }
     printf(failures ? "%d failures\n" : "layout, requests and pieces hold\n", failures);
     return failures != 0;
 }
