@@ -1,17 +1,21 @@
 // Attention over the paged MXFP4 cache for many query rows per key head: prompts and chunks of prompts.
 //
-// A workgroup takes 32 rows for each of its wavefronts - (token, query head of the key head) - and goes through the keys that any of
-// them sees, 64 at a time.  The codes of a tile are expanded once for the workgroup: each wavefront turns its part of K or V into operands of
-// the matrix instruction (32 x 32 x 16, transposed as in mx_attention.h) and writes them to LDS in the order in which a lane reads
-// them, 16 bytes a lane, so that reads meet no conflicts and K and V need no further shuffling.  Two tiles in LDS: while one is multiplied the
-// next is expanded from codes that were loaded a tile earlier; one barrier a tile.
+// A workgroup takes 32 rows for each of its wavefronts - (token, query head of the key head) - and goes through the keys that any
+// of them sees, 64 at a time.  The codes of a tile are expanded once for the workgroup: each wavefront turns its part of K or V into
+// operands of the matrix instruction (32 x 32 x 16, transposed as in mx_attention.h) and writes them to LDS in the order in which a
+// lane reads them, 16 bytes a lane, so that reads meet no conflicts and K and V need no further shuffling.  Two tiles of K and of V
+// in LDS: while one is multiplied the next is expanded from codes that were loaded a tile earlier; one barrier a tile.
 //
-// Per tile a wavefront issues D/4 matrix instructions (32 clocks each), reads the tile from LDS (D/4 KiB; a compute unit's wavefronts
-// together as long as their matrix instructions take) and does 9 vector operations for each of 32 scores a lane: the three run beside each
-// other in the two wavefronts of a SIMD.
+// Lane l has query row l mod 32 and, of 32 keys, those with bit 2 = l / 32: a row's maximum and sum need one exchange.  V's columns
+// are dealt to the 32 rows of an operand so that a lane ends with runs of neighbouring columns of its row.
 //
-// Lane l has query row l mod 32 and, of 32 keys, those with bit 2 = l / 32: a row's maximum and sum need one exchange.  V's columns are dealt to
-// the 32 rows of an operand so that a lane ends with runs of neighbouring columns of its row.
+// What bounds it, at four prompts of 4096 tokens or fewer, 32 heads on 8 of 128 (276 GFLOP counted under the mask, 343 us = 805 TFLOP/s,
+// a bf16 library product of 8192^3 on the same card: 1375): the issue of vector instructions.  A wavefront's tile is 32 matrix
+// instructions (32 clocks each) and some 260 vector instructions.  With parts of the kernel left out: everything but loads, barriers and what a
+// workgroup begins and ends with 157 us (70 of it the beginnings and ends alone, 1344 workgroups), the weights by themselves 113 more, the products
+// 114, the expansion 48.  The two wavefronts of a SIMD work in opposite phases, one in its products while the other weighs
+// (403 -> 361 us); the weights of a single wavefront, 6 clocks an instruction, are then the longer of the two.  Neither half the reads of LDS (363
+// for 368) nor wavefront priorities (351 to 355 for 350) change it; 128 rows a workgroup, two of them on a compute unit, take 403.
 #include "mx_attention.h"
 #include "mx_gemm_shared.h"
 
@@ -298,50 +302,59 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
                     if (e < P::steps) sum[kb][w] = mfma32(k[kb * P::steps + e][lane], q[e], sum[kb][w]);
             }
     };
+    // which pages a step's tile has, asked of LDS while the last products of the tile before run
+    uint32_t there_of;
+    auto ask_pages = [&](int step) __attribute__((always_inline)) { there_of = lds.of[step % 3].there; };
     // the weights of `tile`, whose scores are in `sum`
     auto weigh = [&](int step, int32_t tile) __attribute__((always_inline)) {
         const auto& from = lds.of[step % 3];
+        f32x4 ks[kMbs ? P::words : 1][8];
+        if constexpr (kMbs) {
+#pragma unroll
+            for (int w = 0; w < P::words; ++w)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ks[w][i] = *reinterpret_cast<const f32x4*>(&from.ks[w][8 * i + 4 * half]);
+        }
         const int32_t key0 = tile * kKvTile;
-        const uint32_t there = __builtin_amdgcn_readfirstlane(from.there);
+        const uint32_t there = __builtin_amdgcn_readfirstlane(there_of);
         const bool whole = key0 >= lo_each && key0 + kKvTile <= hi_each && there == 15u;
-        float x[32];  // scores less `base`
-        auto relative = [&](float base) __attribute__((always_inline)) {
+        const float base = m == kLowest ? 0.0f : m;
+        float x[32];  // scores less `base`: of keys 32 (i / 16) + 8 (i / 4 mod 4) + 4 half + i mod 4
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const int kb = i >> 4;
+            if constexpr (kMbs) {
+                x[i] = -base;
+#pragma unroll
+                for (int w = 0; w < P::words; ++w) x[i] = __builtin_fmaf(sum[kb][w][i & 15], ks[w][i >> 2][i & 3], x[i]);
+            } else {
+                float y = sum[kb][0][i & 15];
+#pragma unroll
+                for (int w = 1; w < P::words; ++w) y += sum[kb][w][i & 15];
+                x[i] = __builtin_fmaf(y, a.scale2, -base);
+            }
+        }
+        if (!whole) {
+            // (opaque: the comparisons would be made in front of the branch, for every tile)
+            int32_t from_key = lo - key0 - 4 * half, to_key = hi - key0 - 4 * half, pages = there;
+            asm volatile("" : "+v"(from_key), "+v"(to_key), "+v"(pages));
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                const int kb = i >> 4, key = 32 * kb + 8 * ((i & 15) >> 2) + (i & 3);  // + 4 half
-                if constexpr (kMbs) {
-                    x[i] = -base;
-#pragma unroll
-                    for (int w = 0; w < P::words; ++w)
-                        x[i] = __builtin_fmaf(sum[kb][w][i & 15], (*reinterpret_cast<const f32x4*>(&from.ks[w][(key & ~3) + 4 * half]))[i & 3], x[i]);
-                } else {
-                    float y = sum[kb][0][i & 15];
-#pragma unroll
-                    for (int w = 1; w < P::words; ++w) y += sum[kb][w][i & 15];
-                    x[i] = __builtin_fmaf(y, a.scale2, -base);
-                }
+                const int key = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3);
+                x[i] = key >= from_key && key < to_key && (pages >> (key >> 4) & 1) ? x[i] : -__builtin_inff();
             }
-            if (!whole) {
-                // (opaque: the comparisons would be made in front of the branch, for every tile)
-                int32_t from_key = lo - key0 - 4 * half, to_key = hi - key0 - 4 * half, pages = there;
-                asm volatile("" : "+v"(from_key), "+v"(to_key), "+v"(pages));
+        }
+        float top = fmaxf(x[0], x[1]);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int key = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3);
-                    x[i] = key >= from_key && key < to_key && (pages >> (key >> 4) & 1) ? x[i] : -__builtin_inff();
-                }
-            }
-            float top = fmaxf(x[0], x[1]);
-#pragma unroll
-            for (int i = 2; i < 32; ++i) top = fmaxf(top, x[i]);
-            return pair_max(top);
-        };
+        for (int i = 2; i < 32; ++i) top = fmaxf(top, x[i]);
+        top = pair_max(top);
         // the maximum moves only when a score is 8 (a factor 256) above it, or when it is the row's first
-        const float base = m == kLowest ? 0.0f : m, top = relative(base);
         const bool moves = top > 8.0f || (m == kLowest && top > kLowest);
         if (__builtin_amdgcn_ballot_w64(moves)) {
             const float higher = moves ? base + top : m, shrink = __builtin_amdgcn_exp2f(m - higher);
-            relative(moves ? higher : base);
+            const float change = moves ? higher - base : 0.0f;  // (what it loses is of the size of the scores' own rounding)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] -= change;
             m = higher;
             l *= shrink;
 #pragma unroll
@@ -368,26 +381,14 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
         }
     };
     // the tile's V by its weights, and the next one's scores (past the last tile of whatever is in LDS, and nobody reads them)
-    auto multiply = [&](int step, int32_t tile) __attribute__((always_inline)) {
-        if (__builtin_amdgcn_readfirstlane(lds.any_bad[step & 1])) {
-            const int32_t key0 = tile * kKvTile;
-            uint32_t bad = 0;
-            for (int j = 0; j < kKvTile; ++j)
-                if (key0 + j >= lo && key0 + j < hi) bad |= lds.bad[step & 1][j];
-#pragma unroll
-            for (int t = 0; t < P::columns; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int column = 128 * (t / 4) + P::run(t) * (8 * (i >> 2) + 4 * half + (i & 3)) + t % 4;
-                    if (bad >> (column >> 5) & 1) o[t][i] = __builtin_nanf("");
-                }
-        }
+    auto multiply = [&](int step) __attribute__((always_inline)) {
         const u32x4(*v)[kWave] = lds.v[step & 1];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int t = 0; t < P::columns; ++t) o[t] = mfma32(v[t * 4 + u][lane], weight[kMbs ? t / 4 : 0][u], o[t]);
         scores(lds.k[(step + 1) & 1]);
+        ask_pages(step + 1);
         // operands are asked of LDS several products ahead: left to itself the compiler reads each right before its product and waits for it
         __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
@@ -395,6 +396,21 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+    };
+
+    // NaN blocks of values go into the rows that see them
+    auto spoil = [&](int step, int32_t tile) __attribute__((always_inline)) {
+        const int32_t key0 = tile * kKvTile;
+        uint32_t bad = 0;
+        for (int j = 0; j < kKvTile; ++j)
+            if (key0 + j >= lo && key0 + j < hi) bad |= lds.bad[step & 1][j];
+#pragma unroll
+        for (int t = 0; t < P::columns; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int column = 128 * (t / 4) + P::run(t) * (8 * (i >> 2) + 4 * half + (i & 3)) + t % 4;
+                if (bad >> (column >> 5) & 1) o[t][i] = __builtin_nanf("");
+            }
     };
 
     // ---- the loop: tile t is taken, V of t + 1 and the rest of t + 2 expanded from codes loaded a tile earlier, page ids a tile before that.  Of
@@ -419,15 +435,18 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
         if (threadIdx.x < 2 * kKvTile) (&lds.bad[0][0])[threadIdx.x] = 0;
         if (threadIdx.x < 2) lds.any_bad[threadIdx.x] = 0;
         const int32_t first_seen = max(tile0, lo_some / kKvTile), behind_seen = (hi_some + kKvTile - 1) / kKvTile;
-        // K of tile0 (V of this step is nobody's: no codes), then V of tile0 and K of tile0 + 1
-        ids(tile0 - 1, page_next, word_page_next);
-        turn(tile0 - 1);
-        meet();
-        spread(-1, codes, tile0 - 1, page, word_page);
+        // K of tile0 (V of this step is nobody's: no codes), then V of tile0 and K of tile0 + 1; both asked for at once
+        int32_t page_before[P::turns], word_page_before;
+        PromptCodes<D, kMbs> codes_before;
+        ids(tile0 - 1, page_before, word_page_before);
+        ids(tile0, page_next, word_page_next);
+        load(codes_before, tile0 - 1, page_before, word_page_before);
         turn(tile0);
+        spread(-1, codes_before, tile0 - 1, page_before, word_page_before);
         meet();
         if (first_seen == tile0 && tile0 < behind_seen) {
             scores(lds.k[0]);
+            ask_pages(0);
             if (!late) weigh(0, tile0);
         }
         spread(0, codes, tile0, page, word_page);
@@ -435,15 +454,18 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
             const int step = tile - tile0;
             turn(tile + 1);
             meet();  // V of t and the rest of t + 1 are written; nobody reads V of t - 1 or K of t any more
+            const uint32_t any_bad = lds.any_bad[step & 1];
             const bool seen = tile >= first_seen && tile < behind_seen, seen_next = tile + 1 >= first_seen && tile + 1 < behind_seen;
             if (seen) {
                 if (late) weigh(step, tile);
-                multiply(step, tile);
+                multiply(step);
             } else if (seen_next) {
                 scores(lds.k[(step + 1) & 1]);
+                ask_pages(step + 1);
             }
+            const bool was_bad = __builtin_amdgcn_readfirstlane(any_bad);
+            if (was_bad && seen) spoil(step, tile);
             if (!late && seen_next) weigh(step + 1, tile + 1);
-            const bool was_bad = __builtin_amdgcn_readfirstlane(lds.any_bad[step & 1]);
             spread(step + 1, codes, tile + 1, page, word_page);
             if (was_bad) {  // (rare) cleared once everybody has read it
                 meet();
@@ -514,8 +536,8 @@ __global__ __launch_bounds__(256) void attention_prompt_join_kernel(AttentionArg
 }
 
 // Pieces of the keys, where the row tiles alone leave compute units without one: what fits one round of workgroups, with half a
-// partial tile for each of several requests.  (One request of 4096 rows a
-// key head behind 8192 keys, 128 row tiles: 321 us whole, 206 in two pieces.)
+// partial tile for each of several requests.  (One request of 4096 rows a key head behind 8192 keys, 128 row tiles: 321 us whole,
+// 206 in two pieces.)
 int splits_of(int64_t S, int64_t T, int64_t group, int64_t heads, int64_t D) {
     const int64_t height = prompt_height(D), groups = ((T * group + height - 1) / height + S / 2) * heads;
     return groups <= 128 ? (int)(256 / groups) : 1;
