@@ -556,7 +556,7 @@ __global__ __launch_bounds__(kThreads, (kWorkersLog2<D, kTiles> - 9)) void atten
 
 // Rows that were cut into pieces, kWaves wavefronts a row.
 template <int D, int kTiles, int kWaves>
-__global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionArgs a) {
+__global__ __launch_bounds__((kWaves > 1 ? kWaves * kWave : kThreads)) void attention_join_kernel(AttentionArgs a) {
     constexpr int kHeight = 16 * kTiles;
     const int wave = uniform(threadIdx.x >> 6);
     const int64_t id = kWaves > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kWavesInGroup + wave;
@@ -591,9 +591,11 @@ int launch_tiles(const AttentionArgs& args, hipStream_t s) {
     if (a.cache.k_mbs) hipLaunchKernelGGL((attention_rows_kernel<D, kTiles, true>), grid, dim3(kThreads), 0, s, a);
     else hipLaunchKernelGGL((attention_rows_kernel<D, kTiles, false>), grid, dim3(kThreads), 0, s, a);
     if (int st = launch_status()) return st;
-    // few rows are cut into many parts (of 2048 workers' shares), many rows into few
+    // few rows are cut into many parts of the 2048 shares, many rows into few.  Calls with 1, 4, 16 wavefronts a row in the join: 128 rows behind
+    // 131072 keys - / 73.1 / 71.0 us, 512 rows behind 8192 - / 27.4 / 28.6, 1024 rows 45.5 / 43.7 / 48.5
     const int64_t rows = (int64_t)a.T * a.Hq;
-    if (rows <= 1024) hipLaunchKernelGGL((attention_join_kernel<D, kTiles, kWavesInGroup>), dim3((unsigned)rows), dim3(kThreads), 0, s, a);
+    if (rows <= 256) hipLaunchKernelGGL((attention_join_kernel<D, kTiles, 16>), dim3((unsigned)rows), dim3(16 * kWave), 0, s, a);
+    else if (rows <= 1024) hipLaunchKernelGGL((attention_join_kernel<D, kTiles, 4>), dim3((unsigned)rows), dim3(4 * kWave), 0, s, a);
     else hipLaunchKernelGGL((attention_join_kernel<D, kTiles, 1>), dim3((unsigned)((rows + kWavesInGroup - 1) / kWavesInGroup)), dim3(kThreads), 0, s, a);
     return launch_status();
 }
