@@ -15,7 +15,7 @@
 // codes of each of 4 tokens; pairs of converted tokens are interleaved by v_perm into the operands of 8 products, one for each of the
 // 8 columns, which then lie next to each other in a lane's results.  The MBS factors multiply a key's score and its weight (1 / F
 // by the hardware reciprocal, within an ulp), once per window of 128 of D.
-// Rounding: q, K, V are exact operands; scores, statistics and sums are fp32; P is rounded to bf16 (2^-9 relative to each weight,
+// Rounding: q, K, V are exact operands; scores, statistics and sums are fp32; P is rounded to bf16 (at most 2^-8 relative to each weight,
 // independent from key to key), the sum l takes the weights before that rounding.
 //
 // Masked places.  Tiles that some row does not see whole take the masked form: scores are replaced, not added to; V and its scales

@@ -11,10 +11,10 @@
 //
 // What bounds it, at four prompts of 4096 tokens or fewer, 32 heads on 8 of 128 (276 GFLOP counted under the mask, 343 us = 805 TFLOP/s,
 // a bf16 library product of 8192^3 on the same card: 1375): the issue of vector instructions.  A wavefront's tile is 32 matrix
-// instructions (32 clocks each) and some 260 vector instructions.  With parts of the kernel left out: everything but loads, barriers and what a
+// instructions (32 clocks each) and 284 vector instructions.  With parts of the kernel left out: everything but loads, barriers and what a
 // workgroup begins and ends with 157 us (70 of it the beginnings and ends alone, 1344 workgroups), the weights by themselves 113 more, the products
 // 114, the expansion 48.  The two wavefronts of a SIMD work in opposite phases, one in its products while the other weighs
-// (403 -> 361 us); the weights of a single wavefront, 6 clocks an instruction, are then the longer of the two.  Neither half the reads of LDS (363
+// (505 -> 436 us when it was done); the weights of a single wavefront, 6 clocks an instruction, are then the longer of the two.  Neither half the reads of LDS (363
 // for 368) nor wavefront priorities (351 to 355 for 350) change it; 128 rows a workgroup, two of them on a compute unit, take 403.
 #include "mx_attention.h"
 #include "mx_gemm_shared.h"

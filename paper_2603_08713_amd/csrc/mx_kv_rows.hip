@@ -10,7 +10,9 @@
 // x^2 + eps): the partner's raw bits come through the LDS crossbar (4 dwords for 8 elements).  It is evaluated in fp64 and
 // rounded to fp32 and then bf16: w c and w s are exact, the sum carries one rounding, so that the result does not depend on how
 // anyone orders the operations - a neighbouring bf16 value would change MBS words and codes of its whole window.
-// Bound: HBM, 2 bytes in and 2 (0.55 for a cached row) out per element.
+// Bound: HBM, 2 bytes in and 2 (0.55 for a cached row) out per element.  8192 tokens of 32 + 8 heads of 128: 34 us, 5.1 TB/s (a copy's
+// rate); 4097 tokens with the write of keys and values 26 us, 3.4 TB/s, the quantizer's chain behind the norm's; 16384 x 8 heads of 64
+// written 10.4 us, 4.1 TB/s, read 9.8 us, 4.3 TB/s.
 #include "mx_dequantize_math.h"
 #include "mx_internal.h"
 #include "mx_kv.h"
@@ -272,8 +274,8 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
 
 inline int lanes_of(int D) { return D <= 64 ? 8 : D <= 128 ? 16 : 32; }
 
-// Heads that a wavefront takes one after the other: one where the launch is small (its latency is what counts), eight where it
-// fills the device several times.
+// Heads that a wavefront takes one after the other: one where the launch is small (its latency is what counts: 64 tokens of 80 heads, written
+// and read, 8.4 us; 2 heads 10.3, 4 heads 11.2), eight where it fills the device several times.
 inline int heads_per_wave(int64_t rows_of_waves) { return rows_of_waves > 32768 ? 8 : rows_of_waves > 8192 ? 4 : 1; }
 
 template <int kLanes, bool kTurn, bool kPairs>

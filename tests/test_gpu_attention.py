@@ -275,3 +275,41 @@ def test_a_serving_loop(mx, oracle):
         want, _, tol, _, written = ref.attention(rotated, offsets, lens, table, k_cache, v_cache, D ** -0.5, True, 0)
         assert written[:live].all() and not written[live:].any()
         assert (np.abs(out.cpu().double().numpy() - want) <= tol)[written].all()
+
+
+@pytest.mark.parametrize("n, keys, many", [([128], [128], True), ([128], [700], True), ([512, 30, 600], [512, 900, 1000], True), ([100], [100], False),
+                                           ([1] * 40, list(range(1, 400, 10)), False), ([3, 200], [4000, 300], False)])
+def test_the_kernel_that_a_call_takes(n, keys, many):
+    """Without a choice by the caller: the same bits as from the kernel that the sizes ask for, within the tolerance."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2603_08713_amd as mx
+
+    b = Batch(mx, 11, n, keys, 32, 8, 128, 32, True, wide=1)
+    out, lse = b.check()
+    with mx.forced(attention=2 if many else 1):
+        again, lse_again = b.run()
+    assert torch.equal(out, again) and torch.equal(lse, lse_again)
+
+
+def test_a_cache_beyond_4_gib(mx):
+    """Codes of more than 2^32 bytes an array: the same rows in the first and in the last pages give the same bits."""
+    Hq, Hkv, D, page = 16, 4, 128, 64
+    pages = (5 << 30) // (Hkv * page * D // 2)
+    caches = mx.mx_kv_cache(pages, Hkv, D, page)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(12)
+    keys, n = 333, 70
+    used = -(-keys // page)
+    rows = torch.randn((keys, 2 * Hkv, D), generator=g, device="cuda").to(torch.bfloat16)
+    q = torch.randn((n, Hq, D), generator=g, device="cuda").to(torch.bfloat16)
+    offsets, lens = torch.tensor([0, n], device="cuda"), torch.tensor([keys], dtype=torch.int32, device="cuda")
+    j = torch.arange(keys, device="cuda")
+    results = []
+    for first in (0, pages - used):
+        table = torch.arange(first, first + used, dtype=torch.int32, device="cuda")[None, :].contiguous()
+        slots = first * page + j
+        mx.mx_kv_write(rows[:, :Hkv], rows[:, Hkv:], slots, *caches)
+        results.append((mx.mx_attention_kv(q, offsets, lens, table, *caches),) + tuple(mx.mx_kv_read(slots, *caches)))
+    for low, high in zip(*results):
+        assert torch.equal(low, high)
