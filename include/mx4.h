@@ -310,7 +310,8 @@ int mx_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int64_t num_seq
  *   (y_i, y_j) -> (y_i cos - y_j sin, y_j cos + y_i sin)   on the first R elements, R a multiple of 16 (else MX_EUNSUPPORTED)
  * cos_sin: fp32 [max_position, R], a position's R/2 cosines and then its R/2 sines; NULL with R = 0: no rotation.  Evaluated in
  * fp64 and rounded to fp32 and then to bf16.  A token of negative position (padding) keeps its outputs as they are; the rotated
- * elements of one at or beyond max_position are NaN.  Outputs may be the inputs themselves.  Hq or Hkv may be 0. */
+ * elements of one at or beyond max_position are NaN.  Without a table positions are not read (they may be NULL), and every row is
+ * written.  Outputs may be the inputs themselves.  Hq or Hkv may be 0. */
 int mx_qk_norm_rope(const void* q_bf16, int64_t ldq, const void* k_bf16, int64_t ldk, const int32_t* positions,
                     const float* cos_sin_or_null, int64_t max_position, const void* q_weight_or_null, const void* k_weight_or_null,
                     double eps, mx_rope_t style, int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t R,

@@ -847,7 +847,7 @@ def mx_attention_kv(q, row_offsets, kv_lens, block_table, k_cache, v_cache, scal
     pointers, pages, heads, page, D = _cache_arrays(k_cache, v_cache)
     ldq = _rows_of_heads(q, torch.bfloat16, "q")
     T, Hq, _ = q.shape
-    if q.shape[2] != D or Hq % heads:
+    if q.shape[2] != D or not heads or Hq % heads:
         raise ValueError("q and the cache disagree on the head size, or the key heads do not divide the query heads")
     S = _here(kv_lens, torch.int32, "kv_lens", 1).shape[0]
     _flat(kv_lens, torch.int32, (S,), "kv_lens")
@@ -862,6 +862,7 @@ def mx_attention_kv(q, row_offsets, kv_lens, block_table, k_cache, v_cache, scal
         workspace = torch.empty(mx_attention_kv_workspace(S, T, Hq, heads, D), dtype=torch.uint8, device=q.device)
     else:
         _here(workspace, torch.uint8, "workspace", 1)
+        _flat(workspace, torch.uint8, workspace.shape, "workspace")
     arguments = (_ptr(q), ldq, _ptr(row_offsets), _ptr(kv_lens), _ptr(block_table), block_table.shape[1], *pointers, pages, page, S, T, Hq, heads, D,
                  D ** -0.5 if scale is None else scale, int(bool(causal)), int(window), _ptr(out), ldo, _ptr(lse), _ptr(workspace), workspace.numel(), _stream())
     force = _forced("attention")

@@ -313,3 +313,18 @@ def test_a_cache_beyond_4_gib(mx):
         results.append((mx.mx_attention_kv(q, offsets, lens, table, *caches),) + tuple(mx.mx_kv_read(slots, *caches)))
     for low, high in zip(*results):
         assert torch.equal(low, high)
+
+
+def test_refused_before_a_launch(mx):
+    """A workspace of one byte that says it has many, queries that the key heads do not divide, a cache without heads."""
+    b = Batch(mx, 13, [1, 2], [70, 20], 4, 2, 128, 16, True)
+    size = mx.mx_attention_kv_workspace(2, 3, 4, 2, 128)
+    one = torch.zeros(1, dtype=torch.uint8, device="cuda")
+    for workspace in (one.expand(size + 1), torch.zeros((size + 1, 2), dtype=torch.uint8, device="cuda")[:, 0], one.cpu()):
+        with pytest.raises(TypeError):
+            b.run(workspace=workspace)
+    b.q = b.q[:, :3]
+    with pytest.raises(ValueError):
+        b.run()
+    with pytest.raises(ValueError):
+        mx.mx_attention_kv(b.q, b.offsets, b.lens, b.table, *mx.mx_kv_cache(2, 0, 128, 16))
