@@ -139,54 +139,58 @@ struct HeadShape {
 };
 
 // A row from its parts, row `at` of each: part(i) has the maxima of kHeight rows, their sums, their O.  kWaves wavefronts (of a workgroup
-// of that many, or one of four) do it: lanes have 4 columns each, and the parts are dealt to the groups of lanes.
+// of that many, or one of four) do it: lanes have 4 columns each, the parts are dealt to the groups of lanes, and every group goes through
+// its own with a running maximum, so that a part is one round trip to memory.
+struct Joined {
+    float m, l;
+    f32x4 o;
+    __device__ __forceinline__ void take(float m2, float l2, f32x4 o2) {
+        const float top = fmaxf(m, m2), mine = __builtin_amdgcn_exp2f(m - top), other = __builtin_amdgcn_exp2f(m2 - top);
+        m = top;
+        l = mine * l + other * l2;
+        o = mine * o + other * o2;
+    }
+};
 template <int D, int kHeight, int kWaves, typename F>
 __device__ __forceinline__ void join_parts(const AttentionArgs& a, int32_t t, int h, int32_t at, int32_t count, F&& part) {
     constexpr int kQuads = D / 4, kSides = 64 / kQuads, kDeal = kSides * kWaves;
     __shared__ f32x4 sums[kWaves > 1 ? kWaves : 1][kQuads];
-    __shared__ float weights[kWaves > 1 ? kWaves : 1];
+    __shared__ float tops[kWaves > 1 ? kWaves : 1], weights[kWaves > 1 ? kWaves : 1];
     const int lane = threadIdx.x & 63, wave = kWaves > 1 ? uniform(threadIdx.x >> 6) : 0;
-    float m = kLowest;
-    for (int i = lane; i < count; i += 64) m = fmaxf(m, part(i)[at]);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-    float l = 0.0f;
-    f32x4 o = {0, 0, 0, 0};
+    Joined row = {kLowest, 0.0f, f32x4{0, 0, 0, 0}};
     const int side = lane / kQuads, quad = lane - side * kQuads;
     if (side < kSides) {
 #pragma unroll 8
         for (int i = wave * kSides + side; i < count; i += kDeal) {
             const float* s = part(i);
-            const float w = __builtin_amdgcn_exp2f(s[at] - m);
-            l += w * s[kHeight + at];
-            o += w * *reinterpret_cast<const f32x4*>(s + 2 * kHeight + at * D + 4 * quad);
+            row.take(s[at], s[kHeight + at], *reinterpret_cast<const f32x4*>(s + 2 * kHeight + at * D + 4 * quad));
         }
     }
-    const float own_l = l;
-    const f32x4 own = o;
+    const Joined own = row;
 #pragma unroll
     for (int x = 1; x < kSides; ++x) {  // (only the first side's sums are used)
         const int from = (lane + x * kQuads) & 63;
-        l += __shfl(own_l, from);
+        f32x4 o;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] += __shfl(own[c], from);
+        for (int c = 0; c < 4; ++c) o[c] = __shfl(own.o[c], from);
+        row.take(__shfl(own.m, from), __shfl(own.l, from), o);
     }
     if constexpr (kWaves > 1) {
-        if (side == 0) sums[wave][quad] = o;
-        if (lane == 0) weights[wave] = l;
+        if (side == 0) sums[wave][quad] = row.o;
+        if (lane == 0) {
+            tops[wave] = row.m;
+            weights[wave] = row.l;
+        }
         __syncthreads();
         if (wave) return;
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) {
-            if (side == 0) o += sums[w][quad];
-            l += weights[w];
-        }
+        for (int w = 1; w < kWaves; ++w) row.take(tops[w], weights[w], sums[w][quad]);
     }
     if (side == 0) {
-        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+        const float inverse = row.l == 0.0f ? 0.0f : 1.0f / row.l;
         *reinterpret_cast<u32x2*>(a.out + (int64_t)t * a.ldo + (int64_t)h * D + 4 * quad) =
-            u32x2{pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse)};
-        if (a.lse && lane == 0) a.lse[(int64_t)t * a.Hq + h] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
+            u32x2{pack_bf16(row.o[0] * inverse, row.o[1] * inverse), pack_bf16(row.o[2] * inverse, row.o[3] * inverse)};
+        if (a.lse && lane == 0) a.lse[(int64_t)t * a.Hq + h] = row.l == 0.0f ? -__builtin_inff() : (row.m + __builtin_log2f(row.l)) * kLn2;
     }
 }
 
