@@ -28,7 +28,7 @@ int check_device() {
 extern "C" const char* mx_status_string(int status) {
     switch (status) {
         case MX_OK: return "ok";
-        case MX_EINVAL: return "invalid argument (negative size, K not a multiple of 32, leading dimension too small, or bad enum)";
+        case MX_EINVAL: return "invalid argument (negative size, K not a multiple of 32, leading dimension or workspace too small, or bad enum)";
         case MX_ENULL: return "required pointer is NULL";
         case MX_EALIGN: return "pointer or leading dimension is misaligned";
         case MX_EUNSUPPORTED: return "no HIP device, the current device is not gfx950, or a shape or element format this entry point does not cover";
@@ -37,4 +37,4 @@ extern "C" const char* mx_status_string(int status) {
     }
 }
 
-extern "C" int mx_version(void) { return 200; }
+extern "C" int mx_version(void) { return 300; }
