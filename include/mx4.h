@@ -349,6 +349,8 @@ int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const uint8_t* k_sc
  * exponentials, fp32 [T, Hq]) if not NULL; out does not overlap q.  A row that sees no key: zeros, -inf.  Rows at or beyond row_offsets[num_seqs] are not
  * written.  Requests' rows do not overlap.  NaN in a key or value reaches the rows that see it and no others.
  * Scores, softmax and sums in fp32, weights rounded to bf16 for the product with the values.
+ * A call with more rows than one launch holds returns MX_EINVAL: T Hq of 2^26 and more where requests bring few rows, and of about
+ * 2^31 (heads above 128: 2^30) where they bring many.
  * |x_hat F| of the cache's rows has to be below 2^127 (what mx_kv_write stores of |x| < 2^125 is).
  * workspace: DEVICE memory, 16-byte aligned, of at least mx_attention_kv_workspace(...) bytes, which the call overwrites; calls
  * that can run at the same time need one each. */

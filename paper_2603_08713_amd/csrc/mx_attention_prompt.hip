@@ -553,7 +553,8 @@ int launch_prompt(const AttentionArgs& args, hipStream_t s) {
     a.splits = splits_of(a.S, a.T, a.group, a.cache.at.heads, D);
     a.row_tiles = prompt_row_tiles(a.S, a.T, a.group, D);
     const int64_t groups = a.row_tiles * a.cache.at.heads * a.splits, rows = (int64_t)a.T * a.Hq;
-    if (groups >= (int64_t)1 << 23 || rows >= (int64_t)1 << 26) return MX_EINVAL;  // (launches of fewer than 2^32 work-items)
+    // launches of fewer than 2^32 work-items (pieces are only made of calls with few rows), rows of a key head that 32 bits count
+    if (groups >= (int64_t)1 << 23 || (int64_t)a.T * a.group >= (int64_t)1 << 30) return MX_EINVAL;
     hipLaunchKernelGGL((attention_prompt_kernel<D, kMbs>), dim3((unsigned)groups), dim3(P::threads), kBytes, s, a);
     if (int st = launch_status()) return st;
     if (a.splits > 1) hipLaunchKernelGGL((attention_prompt_join_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);

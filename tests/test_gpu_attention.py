@@ -328,3 +328,26 @@ def test_refused_before_a_launch(mx):
         b.run()
     with pytest.raises(ValueError):
         mx.mx_attention_kv(b.q, b.offsets, b.lens, b.table, *mx.mx_kv_cache(2, 0, 128, 16))
+
+
+def test_a_million_tokens_at_once(mx):
+    """2^26 rows: the last of them against the same rows in a call of their own size; the kernel for few rows refuses them."""
+    T, Hq, Hkv, D, page, window, last = 1 << 20, 64, 8, 64, 16, 16, 300
+    g = torch.Generator(device="cuda")
+    g.manual_seed(14)
+    caches = mx.mx_kv_cache(T // page, Hkv, D, page)
+    table = torch.randperm(T // page, generator=g, device="cuda").int()[None, :].contiguous()
+    used = -(-(last + window) // page)  # pages that the last rows see
+    slots = (table[0, -used:].long()[:, None] * page + torch.arange(page, device="cuda")).flatten()
+    rows = torch.randn((used * page, 2 * Hkv, D), generator=g, device="cuda").to(torch.bfloat16)
+    mx.mx_kv_write(rows[:, :Hkv], rows[:, Hkv:], slots, *caches)
+    q = torch.empty((T, Hq, D), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    offsets = torch.tensor([0, T], device="cuda")
+    if mx.binding._forced("attention") == 1:
+        with pytest.raises(mx.binding.MxError):
+            mx.mx_attention_kv(q, offsets, i32(T), table, *caches, window=window)
+        return
+    out = mx.mx_attention_kv(q, offsets, i32(T), table, *caches, window=window)[T - last:]
+    want, _, tol, _, _ = ref.attention(q[T - last:], torch.tensor([0, last], device="cuda"), i32(used * page), table[:, -used:], *caches, D ** -0.5, True, window)
+    assert (np.abs(out.cpu().double().numpy() - want) <= tol).all()
