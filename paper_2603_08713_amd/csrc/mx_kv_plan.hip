@@ -4,8 +4,9 @@
 // One launch.  Every workgroup sums up the requests by itself (new tokens and new pages before each, an inclusive scan through the
 // lanes and then the wavefronts) into LDS, then takes tokens: the request of a token by a binary search in the offsets, its page
 // either from the request's table or, past the pages that the request holds, from the list of free ones.  A page that a step adds
-// begins with one of its tokens, so the token that stands first in a page also writes the table's entry.  Nothing is passed
-// between workgroups; what depends on the totals alone is written by the first.
+// begins with one of its tokens, so the token that stands first in a page also writes the table's entry; the entries of pages whose first
+// token is at or beyond T, which no thread takes, are written request by request.  Nothing is passed between workgroups; what depends on the
+// totals alone is written by the first.
 // Bound: latency (a launch, the lengths' round trip, the scan, the search, the table's round trip); 12 bytes written a token.  64 requests
 // with a token each 4.2 us, 512 requests with 65 000 tokens 6.0 (an empty launch 2.2).
 #include "mx_kv.h"
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(PlanArgs a) {
     const int64_t t0 = (int64_t)blockIdx.x * kThreads * a.per_thread;
     for (int i = 0; i < a.per_thread; ++i) {
         const int64_t t = t0 + (int64_t)i * kThreads + tid;
-        if (t >= a.T) return;
+        if (t >= a.T) break;
         int64_t slot = -1;
         int32_t position = -1;
         if (t < row_at[a.S]) {
@@ -110,6 +111,19 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(PlanArgs a) {
         }
         a.slots[t] = slot;
         a.positions[t] = position;
+    }
+
+    // More tokens than places: kv_lens and free_next count them all, so the pages that begin with one of the others stand in the table too (an entry
+    // left from before would be another request's page to whoever reads it).
+    if (rows0 <= a.T) return;
+    for (int s = blockIdx.x * kWaves + wave; s < a.S; s += gridDim.x * kWaves) {
+        const int64_t part = (1 << a.page_shift) - 1, c = max(a.ctx_lens[s], 0), n = max(a.new_lens[s], 0);
+        const int64_t held = (c + part) >> a.page_shift, need = min((c + n + part) >> a.page_shift, (int64_t)a.max_pages);
+        const int64_t beyond = (c + (a.T - row_at[s]) + part) >> a.page_shift;  // the first page that begins with token T or a later one
+        for (int64_t index = max(held, beyond) + lane; index < need; index += kWave) {
+            const int64_t at = max(start, (int64_t)0) + page_at[s] + (index - held);
+            a.block_table[(int64_t)s * a.max_pages + index] = at < a.free_count ? a.free_pages[at] : -1;
+        }
     }
 }
 

@@ -98,6 +98,37 @@ def test_plan_of_many(mx, S, most, new, page):
     assert got[4].item() == want[4] and np.array_equal(t.cpu().numpy(), want[5])
 
 
+@pytest.mark.parametrize("ctx, new, page, width, free, start, T", [
+    ([7, 7], [5, 40], 16, 4, 6, 0, 6),                  # pages that begin beyond the places, one of a request that has some
+    ([0, 0, 40], [20, 50, 33], 16, 5, 20, 1, 10),       # and those of requests that have none
+    ([16, 3], [16, 1], 16, 3, 4, 0, 16),                # the last place ends a page
+    ([16, 3], [17, 13], 16, 3, 4, 0, 16),               # the first token beyond begins one
+    ([0, 30], [3, 5], 16, 4, 9, 0, 0),                  # no places at all
+    ([0, 0], [100, 100], 16, 4, 9, 0, 40),              # the free list and the table's rows are at their ends
+])
+def test_plan_takes_the_pages_of_tokens_without_a_place(mx, ctx, new, page, width, free, start, T):
+    """Fewer places than tokens: the pages of the others are counted in free_next, so they stand in the table too, and no entry is left from
+    before - attention would read another request's page there."""
+    test_plan(mx, ctx, new, page, width, free, start, T)
+
+
+@pytest.mark.parametrize("S, most, new, page, part", [(1, 100, 70000, 16, 3), (1100, 300, 90, 16, 2), (4096, 90, 40, 32, 50), (70, 0, 5000, 64, 9)])
+def test_plan_of_many_with_few_places(mx, S, most, new, page, part):
+    rng = np.random.default_rng(S)
+    ctx, n = rng.integers(0, most + 1, S), rng.integers(0, new + 1, S)
+    width = (most + new) // page + 2
+    table = rng.integers(0, 1 << 20, (S, width)).astype(np.int32)
+    free = rng.permutation(int(n.sum()) // page + 2 * S + 5).astype(np.int32)
+    T = int(n.sum()) // part
+    want = ref.plan(ctx, n, page, table, free, 4, T)
+    t = torch.from_numpy(table).cuda()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    got = mx.mx_kv_plan(i32(ctx), i32(n), page, t, torch.from_numpy(free).cuda(), i32([4]), T)
+    for name, g, w in zip(("row_offsets", "kv_lens", "slots", "positions"), got, want):
+        assert np.array_equal(g.cpu().numpy(), w), name
+    assert got[4].item() == want[4] and np.array_equal(t.cpu().numpy(), want[5])
+
+
 # ---- norm and rotation ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
 @pytest.mark.parametrize("style", ["half", "pairs"])
