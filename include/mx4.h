@@ -347,7 +347,8 @@ int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const uint8_t* k_sc
  *   causal:      keys 0 .. p, p = kv_lens[s] - n + i;  with window > 0 only the last `window` of them
  *   not causal:  all keys (window must be 0)
  * of those whose page exists.  out = softmax(scale q . k_hat) v_hat, bf16 [T, Hq, D]; lse (natural logarithm of the sum of
- * exponentials, fp32 [T, Hq]) if not NULL; out does not overlap q.  A row that sees no key: zeros, -inf.  Rows at or beyond row_offsets[num_seqs] are not
+ * exponentials, fp32 [T, Hq]) if not NULL; out does not overlap q.  A row that sees no key: zeros, -inf.  A row
+ * that sees keys whose scores are all -inf (an infinity in its query, or 2e38 passed): NaN.  Rows at or beyond row_offsets[num_seqs] are not
  * written.  Requests' rows do not overlap.  NaN in a key or value reaches the rows that see it and no others.
  * Scores, softmax and sums in fp32, weights rounded to bf16 for the product with the values.
  * A call with more rows than one launch holds returns MX_EINVAL: T Hq of 2^26 and more where requests bring few rows, and of about

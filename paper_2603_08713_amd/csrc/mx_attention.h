@@ -3,7 +3,8 @@
 // Query row i of a request sees keys [lo, hi) (KvRequest); with s_j = scale q . k_j,
 //     m = max s_j,  l = sum exp(s_j - m),  o = sum exp(s_j - m) v_j / l,  lse = m + ln l,
 // in one pass over the keys: m is a running maximum, and l and the accumulated o are rescaled when it grows.  A row that sees
-// nothing is written as zeros, its lse as -inf.
+// nothing is written as zeros, its lse as -inf.  m starts at a finite number, so a row that sees keys but has no score above -inf ends with
+// l = 0 as well, where the formula has exp(-inf - -inf): NaN.  Which of the two it is, its range of keys and the pages say (sees_a_key).
 //
 // Both products go to the bf16 matrix instruction 16 x 16 x 32 in transposed form, S^T = K Q^T and O^T = V^T P^T.  Its result has
 // one query row per lane column (lane mod 16) and four keys (or four of D) per lane, so that
@@ -97,6 +98,7 @@ __device__ __forceinline__ float sigma_of(uint32_t m8) { return __builtin_amdgcn
 
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int32_t read_lane(int32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ float read_lane(float x, int lane) { return __uint_as_float((uint32_t)read_lane((int32_t)__float_as_uint(x), lane)); }
 __device__ __forceinline__ int64_t read_lane(int64_t x, int lane) {
     return (int64_t)((uint64_t)(uint32_t)read_lane((int32_t)x, lane) | (uint64_t)(uint32_t)read_lane((int32_t)(x >> 32), lane) << 32);
 }
@@ -138,6 +140,25 @@ struct HeadShape {
     static constexpr int width(int p) { return p < full ? 128 : p == full && half ? 64 : 32; }
 };
 
+// Whether the row of a lane that asks sees a key: whether a page with one of its keys lo .. hi - 1 is there.  All lanes of the wavefront call it;
+// [begin, end) holds the ranges of all that ask and stays inside the table.  64 pages a round, in the rare case that l is 0.
+__device__ __forceinline__ bool sees_a_key(const AttentionArgs& a, int32_t s, bool asks, int32_t lo, int32_t hi, int32_t begin, int32_t end) {
+    asks = asks && lo < hi;
+    bool found = false;
+    if (!__builtin_amdgcn_ballot_w64(asks)) return found;
+    const int32_t* table = a.block_table + (int64_t)s * a.max_pages;
+    const int shift = a.cache.at.page_shift, lane = threadIdx.x & 63;
+    const int32_t first = lo >> shift, last = (hi - 1) >> shift, end_page = (end - 1) >> shift;
+    for (int32_t j = begin >> shift; j <= end_page; j += 64) {
+        const int32_t id = j + lane <= end_page ? table[j + lane] : -1;
+        const uint64_t there = __builtin_amdgcn_ballot_w64(id >= 0 && id < a.num_pages);
+        const int32_t from = kv_max(first - j, 0), to = kv_min(last - j, 63);
+        if (asks && from <= to) found = found || (there & (~(uint64_t)0 << from) & (~(uint64_t)0 >> (63 - to))) != 0;
+        if (!__builtin_amdgcn_ballot_w64(asks && !found)) break;
+    }
+    return found;
+}
+
 // A row from its parts, row `at` of each: part(i) has the maxima of kHeight rows, their sums, their O.  kWaves wavefronts (of a workgroup
 // of that many, or one of four) do it: lanes have 4 columns each, the parts are dealt to the groups of lanes, and every group goes through
 // its own with a running maximum, so that a part is one round trip to memory.
@@ -152,7 +173,7 @@ struct Joined {
     }
 };
 template <int D, int kHeight, int kWaves, typename F>
-__device__ __forceinline__ void join_parts(const AttentionArgs& a, int32_t t, int h, int32_t at, int32_t count, F&& part) {
+__device__ __forceinline__ void join_parts(const AttentionArgs& a, int32_t t, int h, int32_t s, const KvRequest& r, int32_t at, int32_t count, F&& part) {
     constexpr int kQuads = D / 4, kSides = 64 / kQuads, kDeal = kSides * kWaves;
     __shared__ f32x4 sums[kWaves > 1 ? kWaves : 1][kQuads];
     __shared__ float tops[kWaves > 1 ? kWaves : 1], weights[kWaves > 1 ? kWaves : 1];
@@ -191,6 +212,13 @@ __device__ __forceinline__ void join_parts(const AttentionArgs& a, int32_t t, in
         *reinterpret_cast<u32x2*>(a.out + (int64_t)t * a.ldo + (int64_t)h * D + 4 * quad) =
             u32x2{pack_bf16(row.o[0] * inverse, row.o[1] * inverse), pack_bf16(row.o[2] * inverse, row.o[3] * inverse)};
         if (a.lse && lane == 0) a.lse[(int64_t)t * a.Hq + h] = row.l == 0.0f ? -__builtin_inff() : (row.m + __builtin_log2f(row.l)) * kLn2;
+    }
+    if (read_lane(row.l, 0) == 0.0f) {  // (written over where it is NaN)
+        const int32_t lo = r.lo(t - r.first, a.window), hi = r.hi(t - r.first, a.causal);
+        if (sees_a_key(a, s, true, lo, hi, lo, hi) && side == 0) {
+            *reinterpret_cast<u32x2*>(a.out + (int64_t)t * a.ldo + (int64_t)h * D + 4 * quad) = u32x2{0x7FC07FC0u, 0x7FC07FC0u};
+            if (a.lse && lane == 0) a.lse[(int64_t)t * a.Hq + h] = __builtin_nanf("");
+        }
     }
 }
 

@@ -476,6 +476,7 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
     }
 
     l = pair_sum(l);
+    const bool sees = pieces == 1 && sees_a_key(a, s, real && l == 0.0f, lo, hi, lo_some, hi_some);
     if (!real) return;
     const int64_t t = r.first + token;
     // the lane's runs of neighbouring columns: f(first column, values), 4 at a time
@@ -497,8 +498,8 @@ __global__ __launch_bounds__(PromptShape<D>::threads, (PromptShape<D>::waves / 4
         }
     };
     if (pieces == 1) {
-        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
-        if (a.lse && half == 0) a.lse[t * a.Hq + q_head] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
+        const float none = sees ? __builtin_nanf("") : 0.0f, inverse = l == 0.0f ? none : 1.0f / l;
+        if (a.lse && half == 0) a.lse[t * a.Hq + q_head] = l == 0.0f ? none - __builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
         uint16_t* out = a.out + t * a.ldo + (int64_t)q_head * D;
         each_run([&](int d, f32x4 y) __attribute__((always_inline)) {
             *reinterpret_cast<u32x2*>(out + d) = u32x2{pack_bf16(y[0] * inverse, y[1] * inverse), pack_bf16(y[2] * inverse, y[3] * inverse)};
@@ -531,7 +532,7 @@ __global__ __launch_bounds__(256) void attention_prompt_join_kernel(AttentionArg
     const int32_t pieces = which.pieces(a, kHeight);
     if (pieces == 1 || which.index >= a.row_tiles) return;
     const float* first = a.partial + ((which.index * heads + head) * a.splits) * (int64_t)(kHeight * (D + 2));
-    join_parts<D, kHeight, 1>(a, t, h, row - which.row_tile * kHeight, pieces,
+    join_parts<D, kHeight, 1>(a, t, h, which.s, which.r, row - which.row_tile * kHeight, pieces,
                               [&](int32_t i) __attribute__((always_inline)) { return first + (int64_t)i * (kHeight * (D + 2)); });
 }
 

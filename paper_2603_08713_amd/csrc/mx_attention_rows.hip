@@ -525,13 +525,14 @@ __global__ __launch_bounds__(kThreads, (kWorkersLog2<D, kTiles> - 9)) void atten
     for (int b = 0; b < kTiles; ++b) {
         const float l = column_sum(st.l[b]);
         const int32_t row = row0 + 16 * b + n;
+        const bool sees = direct && sees_a_key(a, s, row < rows && l == 0.0f, lo[b], hi[b], lo_all, hi_all);
         if (row >= rows) continue;
         if (direct) {
             const int32_t i = row / a.group;
             const int64_t t = r.first + i;
             const int h = head * a.group + (row - i * a.group);
-            const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
-            if (a.lse && g == 0) a.lse[t * a.Hq + h] = l == 0.0f ? -__builtin_inff() : (st.m[b] + __builtin_log2f(l)) * kLn2;
+            const float none = sees ? __builtin_nanf("") : 0.0f, inverse = l == 0.0f ? none : 1.0f / l;
+            if (a.lse && g == 0) a.lse[t * a.Hq + h] = l == 0.0f ? none - __builtin_inff() : (st.m[b] + __builtin_log2f(l)) * kLn2;
             uint16_t* o = a.out + t * a.ldo + (int64_t)h * D;
             each_run<D>(st.o[b], g, [&](int d, auto wide, const float* x) __attribute__((always_inline)) {
                 uint32_t w[4];
@@ -577,7 +578,7 @@ __global__ __launch_bounds__((kWaves > 1 ? kWaves * kWave : kThreads)) void atte
     const int64_t item_at = read_lane(batch.end, who) - read_lane(batch.size, who) + (int64_t)(head * row_tiles + row_tile) * item;
     const KvLine::Parts parts = KvLine::parts(item_at, item, batch.share);
     if (parts.count == 1) return;
-    join_parts<D, kHeight, kWaves>(a, t, h, at, parts.count, [&](int32_t i) __attribute__((always_inline)) {
+    join_parts<D, kHeight, kWaves>(a, t, h, batch.block + who, r, at, parts.count, [&](int32_t i) __attribute__((always_inline)) {
         return a.partial + (int64_t)(2 * (parts.first + i) + (i == 0 ? parts.late : 0)) * kPartFloats<D, kTiles>;
     });
 }

@@ -184,6 +184,50 @@ def test_nan_and_infinity_in_queries(mx):
     assert int(torch.isnan(out.float()).sum()) == 2 * 128
 
 
+def _all_minus(b, dtype=torch.bfloat16):
+    """Rewrites every key of the cache's requests as -1 in each element."""
+    H, D = b.caches[0][1].shape[1], b.q.shape[2]
+    rows = torch.full((len(b.slots), H, D), -1.0, dtype=dtype, device="cuda")
+    v = torch.randn((len(b.slots), H, D), device="cuda").to(dtype)
+    b.mx.mx_kv_write(rows, v, torch.from_numpy(b.slots).cuda(), *b.caches)
+
+
+@pytest.mark.parametrize("D, mbs", [(64, True), (96, False), (128, True), (192, True), (256, False)])
+@pytest.mark.parametrize("n, keys", [([1], [1]), ([1, 3, 2], [5000, 70, 0]), ([70, 5, 40], [70, 900, 12])])
+def test_rows_whose_scores_are_all_minus_infinity(mx, D, mbs, n, keys):
+    """exp(-inf - -inf): such a row is NaN, as its formula says, and not what a row without keys gets - whole rows and rows whose keys are cut,
+    the same queries before their request's first key (zeros, -inf), and rows beside them."""
+    b = Batch(mx, D, n, keys, 4, 2, D, 16, mbs)
+    _all_minus(b)
+    b.q.zero_()
+    b.q[:, 1, 3] = float("inf")
+    b.q[::2, 2, D - 1] = float("inf")
+    out, lse = b.check()
+    sees = ~torch.isneginf(lse[:, 0])
+    assert bool(torch.isnan(out[sees, 1].float()).all()) and bool(torch.isnan(lse[sees, 1]).all()) and not bool(torch.isnan(out[:, 0].float()).any())
+    b.check(window=3)
+    b.check(causal=False)
+    b.check(scale=-0.5)  # (+inf - +inf: NaN as well)
+
+
+def test_minus_infinity_and_missing_pages(mx):
+    """Whether such a row sees a key goes by the pages that exist: some, one in the middle, none."""
+    n, keys = [1, 2, 30, 1], [3000, 200, 40, 500]
+    b = Batch(mx, 21, n, keys, 4, 2, 128, 16, True)
+    _all_minus(b)
+    b.q.zero_()
+    b.q[:, :, 0] = float("inf")
+    pages = b.caches[0][1].shape[0]
+    b.table[0, :] = -1
+    b.table[1, :12] = pages  # (only the page of the last 8 keys is there)
+    b.table[2, 1] = -7
+    b.table[3, :9], b.table[3, 10:] = -1, 1 << 30  # (one page, between two tiles' borders)
+    out, lse = b.check()
+    assert bool((out[0] == 0).all()) and bool(torch.isneginf(lse[0]).all()) and bool(torch.isnan(out[1:].float()).all())
+    b.check(window=5)
+    b.check(causal=False)
+
+
 def test_a_page_used_twice_and_a_shared_prefix(mx):
     """Requests that share pages, and a page that stands in a table twice."""
     b = Batch(mx, 8, [1, 2, 5], [150, 150, 150], 4, 2, 128, 16, True)
