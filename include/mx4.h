@@ -283,6 +283,9 @@ int mx_gemm_mbs_elem_grouped(mx_elem_t a_elem, const uint8_t* a_codes, const uin
  * Alignment: codes 16 bytes, scales 4 bytes, norm weights and cos_sin 16 bytes, rows of q, k, v and outputs 16 bytes with leading
  * dimensions (elements from one token's heads to the next one's; a token's heads lie next to each other) a multiple of 8.
  *
+ * A call whose launch would have 2^32 work-items or more returns MX_EINVAL.  (Of rows, mx_qk_norm_rope to mx_kv_read, 64 work-items take 8, 4
+ * or 2 tokens - D up to 64, 128, 256 - of up to eight heads of queries, keys or values.)
+ *
  * Indexes that are on the GPU are not trusted with memory: slots outside the cache are not written or read, pages outside
  * it hold no keys, rows outside the query tensor are not touched. */
 typedef enum {
@@ -351,7 +354,7 @@ int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const uint8_t* k_sc
  * that sees keys whose scores are all -inf (an infinity in its query, or 2e38 passed): NaN.  Rows at or beyond row_offsets[num_seqs] are not
  * written.  Requests' rows do not overlap.  NaN in a key or value reaches the rows that see it and no others.
  * Scores, softmax and sums in fp32, weights rounded to bf16 for the product with the values.
- * A call with more rows than one launch holds returns MX_EINVAL: T Hq of 2^26 and more where requests bring few rows, and of about
+ * A call with more rows than one launch holds returns MX_EINVAL: T Hq above 2^26 - 4 where requests bring few rows, and of about
  * 2^31 (heads above 128: 2^30) where they bring many.
  * |x_hat F| of the cache's rows has to be below 2^127 (what mx_kv_write stores of |x| < 2^125 is).
  * workspace: DEVICE memory, 16-byte aligned, of at least mx_attention_kv_workspace(...) bytes, which the call overwrites; calls

@@ -38,6 +38,7 @@ int attention(int force, const void* q_bf16, int64_t ldq, const int64_t* row_off
         !aligned(block_table, 4) || !aligned(lse_or_null, 4) || !aligned(workspace, 16))
         return MX_EALIGN;
     const bool prompt = force ? force == 2 : is_prompt(num_seqs, T, Hq, Hkv, D);
+    if (!(prompt ? attention_prompt_fits(num_seqs, T, Hq, Hkv, D) : attention_rows_fit(T, Hq))) return MX_EINVAL;
     const int64_t need = workspace_of(prompt, num_seqs, T, Hq, Hkv, D);
     if (workspace_bytes < need) return MX_EINVAL;
     if (need && !workspace) return MX_ENULL;

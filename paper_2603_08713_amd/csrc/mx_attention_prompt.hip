@@ -554,8 +554,6 @@ int launch_prompt(const AttentionArgs& args, hipStream_t s) {
     a.splits = splits_of(a.S, a.T, a.group, a.cache.at.heads, D);
     a.row_tiles = prompt_row_tiles(a.S, a.T, a.group, D);
     const int64_t groups = a.row_tiles * a.cache.at.heads * a.splits, rows = (int64_t)a.T * a.Hq;
-    // launches of fewer than 2^32 work-items (pieces are only made of calls with few rows), rows of a key head that 32 bits count
-    if (groups >= (int64_t)1 << 23 || (int64_t)a.T * a.group >= (int64_t)1 << 30) return MX_EINVAL;
     hipLaunchKernelGGL((attention_prompt_kernel<D, kMbs>), dim3((unsigned)groups), dim3(P::threads), kBytes, s, a);
     if (int st = launch_status()) return st;
     if (a.splits > 1) hipLaunchKernelGGL((attention_prompt_join_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
@@ -568,6 +566,12 @@ int64_t prompt_height(int64_t D) { return D <= 128 ? PromptShape<128>::rows : Pr
 
 int64_t prompt_row_tiles(int64_t S, int64_t T, int64_t group, int64_t D) {
     return S + (T * group + prompt_height(D) - 1) / prompt_height(D);  // one partial tile a request at most
+}
+
+// launches of fewer than 2^32 work-items (512 threads a workgroup; pieces are only made of calls with few rows), rows of a key head that 32 bits
+// count
+bool attention_prompt_fits(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    return prompt_row_tiles(S, T, Hq / Hkv, D) * Hkv * splits_of(S, T, Hq / Hkv, Hkv, D) < (int64_t)1 << 23 && T * (Hq / Hkv) < (int64_t)1 << 30;
 }
 
 int64_t attention_prompt_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {

@@ -628,8 +628,9 @@ int64_t attention_rows_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, 
     return with_shape(S, T, Hq / Hkv, D, [](auto d, auto tiles) { return workspace_of<decltype(d)::value, decltype(tiles)::value>(); });
 }
 
+bool attention_rows_fit(int64_t T, int64_t Hq) { return T * Hq <= kKvMostWaves; }  // (a wavefront a row in the join)
+
 int launch_attention_rows(const AttentionArgs& a, hipStream_t stream) {
-    if ((int64_t)a.T * a.Hq >= (int64_t)1 << 26) return MX_EINVAL;  // (a launch of fewer than 2^32 work-items)
     return with_shape(a.S, a.T, a.group, a.cache.at.D,
                       [&](auto d, auto tiles) { return launch_tiles<decltype(d)::value, decltype(tiles)::value>(a, stream); });
 }

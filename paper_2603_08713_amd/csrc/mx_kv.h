@@ -8,6 +8,7 @@ namespace mx {
 
 constexpr int64_t kKvMost = (int64_t)1 << 30;       // tokens of a call
 constexpr int64_t kKvMostHeads = (int64_t)1 << 16;
+constexpr int64_t kKvMostWaves = ((int64_t)1 << 26) - 4;  // of a launch in workgroups of four: fewer than 2^32 work-items, the last workgroup whole
 
 inline bool kv_head_dim(int64_t D) { return D == 64 || D == 96 || D == 128 || D == 192 || D == 256; }
 

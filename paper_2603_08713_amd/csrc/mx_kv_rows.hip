@@ -291,7 +291,7 @@ void launch_rows(const RowsArgs& a, bool turn, bool pairs, bool cache, bool mbs,
     else launch_rows<kLanes, true, false>(a, cache, mbs, grid, s);
 }
 
-// Everything but what tells the calls apart has been checked.
+// Everything but what tells the calls apart has been checked, the size of the launch and the device excepted.
 int run_rows(RowsArgs a, bool turn, bool pairs, bool cache, hipStream_t stream) {
     const int lanes = lanes_of(a.cache.at.D), tokens = kWave / lanes;
     a.token_groups = (uint32_t)((a.T + (int64_t)tokens - 1) / tokens);
@@ -301,9 +301,10 @@ int run_rows(RowsArgs a, bool turn, bool pairs, bool cache, hipStream_t stream) 
     a.q_chunks = (a.Hq + a.per_wave - 1) / a.per_wave;
     a.kv_chunks = (a.cache.at.heads + a.per_wave - 1) / a.per_wave;
     const int64_t waves = (int64_t)a.token_groups * (a.q_chunks + (int64_t)a.kv_chunks * (cache ? 2 : 1));
-    if (waves >= (int64_t)1 << 26) return MX_EINVAL;  // a launch of fewer than 2^32 work-items
+    if (waves > kKvMostWaves) return MX_EINVAL;
     a.waves = (uint32_t)waves;
     if (waves == 0) return MX_OK;
+    if (int st = check_device()) return st;
     const dim3 grid((unsigned)((waves + kThreads / kWave - 1) / (kThreads / kWave)));
     const bool mbs = a.cache.k_mbs != nullptr;
     if (lanes == 8) launch_rows<8>(a, turn, pairs, cache, mbs, grid, stream);
@@ -375,7 +376,6 @@ extern "C" int mx_qk_norm_rope(const void* q_bf16, int64_t ldq, const void* k_bf
     if (Hkv && ldk_out < Hkv * D) return MX_EINVAL;
     if (Hkv && !k_out) return MX_ENULL;
     if (Hkv && !good_rows(k_out, ldk_out)) return MX_EALIGN;
-    if (int st = check_device()) return st;
     a.T = (int32_t)T; a.Hq = (int32_t)Hq; a.R = (int32_t)R;
     a.cache.shape(16, Hkv, D);
     return run_rows(a, true, style == MX_ROPE_PAIRS, false, static_cast<hipStream_t>(stream));
@@ -394,7 +394,6 @@ extern "C" int mx_kv_write(const void* k_bf16, int64_t ldk, const void* v_bf16, 
     if (!k_bf16 || !v_bf16 || !slots) return MX_ENULL;
     if (!good_rows(k_bf16, ldk) || !good_rows(v_bf16, ldv) || !aligned(slots, 8)) return MX_EALIGN;
     if (num_pages == 0) return MX_OK;  // no slot exists
-    if (int st = check_device()) return st;
     a.k = static_cast<const uint16_t*>(k_bf16);
     a.v = static_cast<const uint16_t*>(v_bf16);
     a.ldk = ldk; a.ldv = ldv;
@@ -433,7 +432,6 @@ extern "C" int mx_qk_norm_rope_kv_write(const void* q_bf16, int64_t ldq, const v
     if (ldv < Hkv * D) return MX_EINVAL;
     if (!v_bf16 || !slots) return MX_ENULL;
     if (!good_rows(v_bf16, ldv) || !aligned(slots, 8)) return MX_EALIGN;
-    if (int st = check_device()) return st;
     a.slots = slots;
     a.rule = rule;
     a.T = (int32_t)T; a.Hq = (int32_t)Hq; a.R = (int32_t)R;
@@ -458,7 +456,6 @@ extern "C" int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const ui
     const int64_t per16 = out_dtype == MX_OUT_F32 ? 4 : 8;
     if (!aligned(k_out, 16) || !aligned(v_out, 16) || (k_out && ldk % per16) || (v_out && ldv % per16) || !aligned(slots, 8)) return MX_EALIGN;
     if (num_pages == 0) return MX_OK;
-    if (int st = check_device()) return st;
     a.slots = slots;
     a.k_out = k_out; a.v_out = v_out;
     a.ldk = ldk; a.ldv = ldv;
@@ -470,7 +467,8 @@ extern "C" int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const ui
     a.per_wave = heads_per_wave(groups * 2 * Hkv);
     a.chunks = (uint32_t)((Hkv + a.per_wave - 1) / a.per_wave);
     const int64_t waves = groups * 2 * a.chunks;
-    if (waves >= (int64_t)1 << 26) return MX_EINVAL;
+    if (waves > kKvMostWaves) return MX_EINVAL;
+    if (int st = check_device()) return st;
     a.waves = (uint32_t)waves;
     const dim3 grid((unsigned)((waves + kThreads / kWave - 1) / (kThreads / kWave)));
     hipStream_t s = static_cast<hipStream_t>(stream);

@@ -395,3 +395,25 @@ def test_a_million_tokens_at_once(mx):
     out = mx.mx_attention_kv(q, offsets, i32(T), table, *caches, window=window)[T - last:]
     want, _, tol, _, _ = ref.attention(q[T - last:], torch.tensor([0, last], device="cuda"), i32(used * page), table[:, -used:], *caches, D ** -0.5, True, window)
     assert (np.abs(out.cpu().double().numpy() - want) <= tol).all()
+
+
+def test_as_many_rows_as_one_launch_holds(mx):
+    """2^26 - 4 rows on pages that stand in the table again and again: rows of the beginning, the middle and the end."""
+    if mx.binding._forced("attention") == 2:
+        pytest.skip("the limit of the kernel for few rows")
+    T, Hq, D, page, window, pages = (1 << 24) - 1, 4, 64, 16, 16, 40
+    g = torch.Generator(device="cuda")
+    g.manual_seed(15)
+    caches = mx.mx_kv_cache(pages, Hq, D, page)
+    rows = torch.randn((pages * page, 2 * Hq, D), generator=g, device="cuda").to(torch.bfloat16)
+    mx.mx_kv_write(rows[:, :Hq], rows[:, Hq:], torch.arange(pages * page, device="cuda"), *caches)
+    table = torch.randint(0, pages, (1, -(-T // page)), generator=g, device="cuda").int()
+    q = torch.empty((T, Hq, D), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    lens = torch.tensor([T], dtype=torch.int32, device="cuda")
+    out = mx.mx_attention_kv(q, torch.tensor([0, T], device="cuda"), lens, table, *caches, window=window)
+    for end in (100, T // 2 // page * page, T):
+        first = max(0, (end - 200) // page * page)
+        n = end - max(first + window, 0) if first else end
+        want, _, tol, _, _ = ref.attention(q[end - n:end], torch.tensor([0, n], device="cuda"), lens.fill_(end - first), table[:, first // page:-(-end // page)], *caches,
+                                           D ** -0.5, True, window)
+        assert (np.abs(out[end - n:end].cpu().double().numpy() - want) <= tol).all()

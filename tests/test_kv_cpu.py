@@ -111,6 +111,28 @@ def test_empty_calls_do_nothing(lib):
     assert lib.mx_attention_kv(*_changed(ATTEND, S=0)) == OK
 
 
+# (a wavefront has 8, 4 or 2 tokens of up to eight heads of queries, keys or values; a workgroup has four wavefronts)
+@pytest.mark.parametrize("name, base, changes, most", [
+    ("mx_qk_norm_rope", TURN, dict(Hq=1, Hkv=0, D=256), 2 * ((1 << 26) - 4)),
+    ("mx_qk_norm_rope", TURN, dict(Hq=0, Hkv=9, ldk=1152, ldko=1152), 4 * ((1 << 25) - 2)),
+    ("mx_kv_write", WRITE, dict(Hkv=1, D=256), 2 * ((1 << 25) - 2)),
+    ("mx_qk_norm_rope_kv_write", BOTH, dict(Hq=1, Hkv=1, D=256), 2 * ((1 << 26) // 3 - 1)),
+    ("mx_kv_read", READ, dict(Hkv=1, D=256), 2 * ((1 << 25) - 2)),
+    ("mx_attention_kv", ATTEND, dict(Hq=1, Hkv=1, S=1 << 26), (1 << 26) - 4),
+    ("mx_attention_kv", ATTEND, dict(Hq=1, Hkv=1, S=1), (1 << 30) - 1),
+    ("mx_attention_kv", ATTEND, dict(Hq=8, Hkv=8, S=1), 256 * ((1 << 20) - 2)),
+])
+def test_the_largest_launches(lib, name, base, changes, most):
+    """A launch holds fewer than 2^32 work-items, its last workgroup whole.  What would not fit is refused with the arguments, before anything runs."""
+    torch = pytest.importorskip("torch")
+    call = getattr(lib, name)
+    for T in (most + 1, most + 4, most + 1000):
+        assert T > 1 << 30 or call(*_changed(base, T=T, **changes)) == EINVAL, T
+    if not torch.cuda.device_count():  # (the addresses are made up)
+        for T in (most - 1000, most):
+            assert call(*_changed(base, T=T, **changes)) == EUNSUPPORTED, T
+
+
 def test_workspace_sizes(lib):
     size = lib.mx_attention_kv_workspace
     assert size(0, 0, 8, 2, 128) == 0 and size(3, 0, 8, 2, 128) == 0
