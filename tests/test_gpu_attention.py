@@ -244,6 +244,49 @@ def test_results_do_not_depend_on_the_batch(mx):
     assert torch.equal(one, again) and torch.equal(lse, lse_again)
 
 
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("mbs", [True, False])
+def test_nan_as_the_cache_write_stores_it(mx, D, mbs):
+    """NaN and infinity in rows that mx_kv_write quantizes (scale byte 255 over codes that are all 0), of keys and of values, in tiles that every
+    row sees whole and in tiles that a mask or a request's end cuts."""
+    n, keys = [1, 40, 3], [300, 300, 333]
+    b = Batch(mx, 22, n, keys, 4, 2, D, 16, mbs)
+    at = np.cumsum([0] + keys)
+    H = 2
+    x = torch.randn((7, 2 * H, D), device="cuda").to(torch.bfloat16)
+    x[0, 0, 5] = float("nan")           # request 0: key 20, head 0, the first block: a whole tile
+    x[1, H + 1, D - 1] = float("-inf")  # request 0: value of key 130, head 1, the last block: a whole tile
+    x[2, H, 33] = float("inf")          # request 0: value of key 299, head 0, the second block: the request's last tile
+    x[3, H, 0] = float("nan")           # request 1: value of key 70, head 0: a whole tile for all of its rows
+    x[4, H + 1, 40] = float("inf")      # request 1: value of key 290, which the last ten rows see
+    x[5, 1, D - 2] = float("inf")       # request 1: key 295, head 1, which the last five rows see
+    x[6, 1, 1] = float("nan")           # request 2: key 64, head 1
+    where = [20, 130, 299, at[1] + 70, at[1] + 290, at[1] + 295, at[2] + 64]
+    places = b.slots[where]
+    b.mx.mx_kv_write(x[:, :H], x[:, H:], torch.from_numpy(places).cuda(), *b.caches)
+    for cache, is_key, row, head, block in ((b.caches[0], True, 0, 0, 0), (b.caches[1], False, 2, 0, 1)):
+        codes, scales, _ = ref.cached_rows(cache, is_key, places)
+        assert scales[row, head, block] == 255 and not codes[row, head, 16 * block:16 * block + 16].any()
+    out, lse = b.check()
+    nan = torch.isnan(out.float())
+    assert bool(nan[0, :2].all()) and bool(nan[0, 2:, D - 32:].all()) and not bool(nan[0, 2:, :D - 32].any())
+    assert bool(nan[1:41, :2, :32].all()) and not bool(nan[1:41, :2, 32:].any()) and not bool(nan[1:31, 2:].any()) and bool(nan[36:41, 2:].all())
+    assert not bool(nan[41:, :2].any()) and bool(nan[41:, 2:].all()) and bool(torch.isnan(lse[41:, 2:]).all())
+    b.check(causal=False)
+    b.check(window=100)
+
+
+@pytest.mark.parametrize("n, keys", [([1] * 9, [5000, 1, 77, 3000, 0, 64, 900, 2, 333]), ([3, 130, 1, 20], [4000, 130, 77, 500])])
+def test_each_request_alone(mx, n, keys):
+    """A request of a batch by itself: its own rows, lengths and row of the table, within the tolerance as it is among others."""
+    b = Batch(mx, 9, n, keys, 8, 2, 128, 64, True)
+    b.check()
+    q, offsets, lens, table = b.q, b.offsets.tolist(), b.lens, b.table
+    for s in range(len(n)):
+        b.q, b.offsets, b.lens, b.table = q[offsets[s]:offsets[s + 1]], torch.tensor([0, n[s]], device="cuda"), lens[s:s + 1], table[s:s + 1]
+        b.check()
+
+
 @pytest.mark.parametrize("n, keys", [([1, 1], [3000, 20]), ([50, 3], [70, 900])])
 def test_workspaces_streams_and_graphs(mx, n, keys):
     """A caller's workspace with anything in it; another stream; captured and replayed over changed lengths and queries."""
