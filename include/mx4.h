@@ -303,7 +303,8 @@ typedef enum {
  *   free_next int32 [1]             free_start[0] and the pages that were wanted; beyond free_count if they were too few
  * A token whose page is missing (free_pages or the table's row is at its end) gets slot -1.  All arrays are DEVICE memory;
  * nothing is allocated on the host, so the call can be captured; the next step takes kv_lens and free_next as its ctx_lens and
- * free_start.  T is at least the sum of new_lens: tokens beyond T get no place, but row_offsets, kv_lens, free_next and block_table
+ * free_start.  (A captured step that is replayed reads its ctx_lens and free_start again: it ends with copies of kv_lens and free_next
+ * into them, or two graphs that write each other's take turns.  Without, every replay plans the first step's places anew.)  T is at least the sum of new_lens: tokens beyond T get no place, but row_offsets, kv_lens, free_next and block_table
  * count them and their pages all the same.  num_seqs <= 4096, else MX_EUNSUPPORTED;
  * max_pages * page_size <= 2^30.  kv_lens may not be ctx_lens or new_lens, free_next not free_start (MX_EINVAL). */
 int mx_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int64_t num_seqs, int64_t page_size, int32_t* block_table,

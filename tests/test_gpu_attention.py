@@ -1,4 +1,6 @@
 """Attention over the paged MXFP4 cache against a plain 64-bit implementation (tests/kv_reference.py derives the tolerances)."""
+import os
+
 import numpy as np
 import pytest
 
@@ -362,6 +364,53 @@ def test_a_serving_loop(mx, oracle):
         want, _, tol, _, written = ref.attention(rotated, offsets, lens, table, k_cache, v_cache, D ** -0.5, True, 0)
         assert written[:live].all() and not written[live:].any()
         assert (np.abs(out.cpu().double().numpy() - want) <= tol)[written].all()
+
+
+def test_a_captured_serving_step(mx):
+    """The serving step that the README shows, captured once and replayed step after step with the program's own eager work between the replays, against
+    the same lines run eagerly on a cache of their own."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    once, step = next(b for b in text.split("```")[1::2] if "mx_kv_plan" in b).removeprefix("python").split("# a step:")
+    once, step = compile(once, "README", "exec"), compile("#" + step, "README", "exec")
+    S, Hq, Hkv, D, page, width, T = 3, 6, 2, 128, 16, 6, 45
+    angle = torch.arange(128, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64) / D)
+    w = torch.linspace(0.6, 1.4, D, device="cuda").to(torch.bfloat16)
+    qkv = torch.zeros((T, Hq + 2 * Hkv, D), dtype=torch.bfloat16, device="cuda")
+    given = dict(torch=torch, mx=mx, num_pages=15, kv_heads=Hkv, head_dim=D, page_size=page, S=S, T=T, q_weight=w, k_weight=w,
+                 cos_sin=torch.cat((angle.cos(), angle.sin()), -1).float().cuda(), free_pages=torch.randperm(15, device="cuda").int(),
+                 new=torch.zeros(S, dtype=torch.int32, device="cuda"))
+
+    def server():
+        names = dict(given, block_table=torch.full((S, width), -1, dtype=torch.int32, device="cuda"))
+        exec(once, names)
+        return names
+
+    def run(names):
+        names.update(q=qkv[:, :Hq], k=qkv[:, Hq:Hq + Hkv], v=qkv[:, Hq + Hkv:])
+        exec(step, names)
+
+    captured, eager = server(), server()
+    run(captured)  # (no tokens yet: what a first call sets up)
+    lens, start = captured["lens"], captured["start"]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(captured)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(31)
+    ctx = np.zeros(S, np.int64)
+    for tokens in ([20, 7, 13], [1, 1, 1], [1, 0, 1], [2, 9, 1], [1, 1, 1], [0, 0, 0], [30, 1, 1]):
+        qkv.copy_(torch.randn(qkv.shape, generator=g, device="cuda"))
+        given["new"].copy_(torch.tensor(tokens, dtype=torch.int32))
+        graph.replay()
+        run(eager)
+        torch.cuda.synchronize()
+        ctx += np.array(tokens)
+        live = sum(tokens)
+        for name in ("lens", "start", "slots", "positions", "block_table"):
+            assert torch.equal(captured[name], eager[name]), (name, tokens)
+        assert np.array_equal(lens.cpu().numpy(), ctx) and start.item() == sum(-(-int(c) // page) for c in ctx)
+        assert torch.equal(captured["out"][:live], eager["out"][:live])
+        assert all(torch.equal(x, y) for name in ("k_cache", "v_cache") for x, y in zip(captured[name], eager[name]))
 
 
 @pytest.mark.parametrize("n, keys, many", [([128], [128], True), ([128], [700], True), ([512, 30, 600], [512, 900, 1000], True), ([100], [100], False),
