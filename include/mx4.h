@@ -357,7 +357,8 @@ int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const uint8_t* k_sc
  * Scores, softmax and sums in fp32, weights rounded to bf16 for the product with the values.
  * A call with more rows than one launch holds returns MX_EINVAL: T Hq above 2^26 - 4 where requests bring few rows, and of about
  * 2^31 (heads above 128: 2^30) where they bring many.
- * |x_hat F| of the cache's rows has to be below 2^127 (what mx_kv_write stores of |x| < 2^125 is).
+ * |x_hat F| of the cache's rows has to be below 2^127 (what mx_kv_write stores of |x| < 2^125 is), and |v_hat| kv_lens[s] below 2^119: the
+ * sums of values are kept in fp32 under weights of up to 2^8, before the division.  Beyond that results are infinite or NaN.
  * workspace: DEVICE memory, 16-byte aligned, of at least mx_attention_kv_workspace(...) bytes, which the call overwrites; calls
  * that can run at the same time need one each. */
 int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,

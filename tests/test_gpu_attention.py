@@ -123,6 +123,25 @@ def test_large_scores_and_scales(mx):
         Batch(mx, 3, [1, 20], [500, 300], 8, 2, 128, 64, True, spread=spread).check(scale=scale)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("mbs", [True, False])
+def test_values_as_large_as_they_may_be(mx, D, mbs):
+    """|v| kv_lens of 2^118.2 of the 2^119 that are allowed, under the largest weights: 64 keys at score 0 and the others 7.9 powers of two above them,
+    which is just too little for the running maximum to follow (300 2^7.9 2^110 = 2^126.1 in the sums)."""
+    b = Batch(mx, 24, [1, 40, 2], [300, 300, 299], 4, 2, D, 16, mbs)
+    H = 2
+    rows = torch.zeros((len(b.slots), 2 * H, D), dtype=torch.bfloat16, device="cuda")
+    j = torch.cat([torch.arange(L, device="cuda") for L in (300, 300, 299)])
+    rows[:, :H, 0] = torch.where(j < 64, 0.0, 4.0)[:, None].to(torch.bfloat16)
+    sign = torch.where(torch.arange(D, device="cuda") % 3 == 0, -1.0, 1.0)
+    rows[:, H:] = (2.0 ** 110 * sign).to(torch.bfloat16)
+    b.mx.mx_kv_write(rows[:, :H], rows[:, H:], torch.from_numpy(b.slots).cuda(), *b.caches)
+    b.q.zero_()
+    b.q[:, :, 0] = 1.0
+    out, _ = b.check(scale=7.9 * np.log(2.0) / 4.0)
+    assert bool((out[:43].float() == 2.0 ** 110 * sign).all())
+
+
 def test_missing_pages(mx):
     """Pages outside the cache hold no keys, and lengths beyond the table end with it."""
     b = Batch(mx, 4, [1, 30, 2, 1], [200, 150, 90, 40], 4, 2, 128, 16, True)
