@@ -50,7 +50,6 @@ struct AttentionArgs {
 int launch_attention_prompt(const AttentionArgs& a, hipStream_t stream);
 int64_t attention_prompt_workspace(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
 int64_t prompt_row_tiles(int64_t S, int64_t T, int64_t group, int64_t D);
-int64_t prompt_height(int64_t D);  // rows of a tile
 bool attention_prompt_fits(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);  // whether a launch holds it
 
 // kernels of mx_attention_rows.hip

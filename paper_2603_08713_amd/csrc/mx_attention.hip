@@ -10,11 +10,25 @@ bool good_shape(int64_t S, int64_t T, int64_t Hq, int64_t Hkv) {
 }
 
 // Whether the kernel for many rows takes a call.  It expands a key once for 256 rows (heads above 128: 128) where the one for few rows
-// does for 16 to 64, but pays for a whole tile of rows and needs tiles enough for the compute units.  Few against many, us, at 8 key
-// heads of 128: one request behind 8192 keys, 256 rows a head 42 / 41, 512 rows 54 / 49, 4096 rows 292 / 206; 16 requests behind 2000
-// keys, 64 rows 44 / 64, 128 rows 57 / 57, 256 rows 88 / 85; 8 behind 4000, 256 rows 88 / 98; 64 behind 2000, 128 rows 177 / 141.
-bool is_prompt(int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
-    const int64_t rows = T * (Hq / Hkv), tiles = rows / prompt_height(D) * Hkv;
+// does for 16 to 64, but pays for a whole tile of rows and needs tiles enough for the compute units.  Few / many, us, at 8 key heads, where the line
+// asks for the kernel in capitals:
+//   heads of                                                   64          96         128         192         256
+//   1 request behind 8192 keys, 256 rows a head, FEW      35 / 31     40 / 39     42 / 41     65 / 67     79 / 75
+//   the same, 512 rows, MANY                              45 / 39     56 / 45     54 / 49    108 / 98    132 / 114
+//   the same, 4096 rows, MANY                           207 / 155   331 / 174   292 / 206   668 / 569   784 / 678
+//   16 requests behind 2000 keys, 64 rows, FEW            36 / 40     39 / 42     44 / 64     62 / 85    73 / 102
+//   the same, 128 rows, FEW                               47 / 49     61 / 53     57 / 57    98 / 144   114 / 169
+//   the same, 256 rows, MANY                              75 / 62     96 / 72     88 / 85   188 / 148   216 / 174
+//   8 requests behind 4000 keys, 256 rows, FEW            68 / 76     97 / 85     88 / 98   178 / 269   209 / 321
+//   64 requests behind 2000 keys, 128 rows, MANY        119 / 111   187 / 125   177 / 141   373 / 298   498 / 352
+//   1 request behind 8192 keys, 2 key heads, 1536 rows, FEW                         45 / 46     81 / 85     95 / 99
+//   the same, 2048 rows, MANY                                                       53 / 51    101 / 99   123 / 117
+//   4 requests behind 4000 keys, 512 rows, MANY                                     89 / 80   178 / 274   212 / 326
+// (Heads of 96 lean to many rows a little sooner; above 128 the last one is lost because 128 to 250 tiles of 128 rows are neither cut nor
+// fill the device.)  Tiles are counted in 256 rows for all head sizes: counted in the 128 that a tile of heads above 128 has, 16 requests of 128
+// rows and 8 of 256 went to the slower kernel there.
+bool is_prompt(int64_t S, int64_t T, int64_t Hq, int64_t Hkv) {
+    const int64_t rows = T * (Hq / Hkv), tiles = rows / 256 * Hkv;
     return (rows >= 512 * S && tiles >= 16) || (rows > 64 * S && tiles >= 128);
 }
 
@@ -37,7 +51,7 @@ int attention(int force, const void* q_bf16, int64_t ldq, const int64_t* row_off
     if (!aligned(q_bf16, 16) || ldq % 8 || !aligned(out_bf16, 16) || ldo % 8 || !aligned(row_offsets, 8) || !aligned(kv_lens, 4) ||
         !aligned(block_table, 4) || !aligned(lse_or_null, 4) || !aligned(workspace, 16))
         return MX_EALIGN;
-    const bool prompt = force ? force == 2 : is_prompt(num_seqs, T, Hq, Hkv, D);
+    const bool prompt = force ? force == 2 : is_prompt(num_seqs, T, Hq, Hkv);
     if (!(prompt ? attention_prompt_fits(num_seqs, T, Hq, Hkv, D) : attention_rows_fit(T, Hq))) return MX_EINVAL;
     const int64_t need = workspace_of(prompt, num_seqs, T, Hq, Hkv, D);
     if (workspace_bytes < need) return MX_EINVAL;
@@ -80,7 +94,7 @@ extern "C" int64_t mx_attention_kv_workspace(int64_t num_seqs, int64_t T, int64_
     using namespace mx;
     if (!good_shape(num_seqs, T, Hq, Hkv)) return MX_EINVAL;
     if (!kv_head_dim(D)) return MX_EUNSUPPORTED;
-    return workspace_of(is_prompt(num_seqs, T, Hq, Hkv, D), num_seqs, T, Hq, Hkv, D);
+    return workspace_of(is_prompt(num_seqs, T, Hq, Hkv), num_seqs, T, Hq, Hkv, D);
 }
 
 extern "C" int mx_attention_kv(const void* q_bf16, int64_t ldq, const int64_t* row_offsets, const int32_t* kv_lens, const int32_t* block_table,

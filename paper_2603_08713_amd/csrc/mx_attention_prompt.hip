@@ -536,6 +536,8 @@ __global__ __launch_bounds__(256) void attention_prompt_join_kernel(AttentionArg
                               [&](int32_t i) __attribute__((always_inline)) { return first + (int64_t)i * (kHeight * (D + 2)); });
 }
 
+int64_t prompt_height(int64_t D) { return D <= 128 ? PromptShape<128>::rows : PromptShape<256>::rows; }  // rows of a tile
+
 // Pieces of the keys, where the row tiles alone leave compute units without one: what fits one round of workgroups, with half a
 // partial tile for each of several requests.  (One request of 4096 rows a key head behind 8192 keys, 128 row tiles: 321 us whole,
 // 206 in two pieces.)
@@ -561,8 +563,6 @@ int launch_prompt(const AttentionArgs& args, hipStream_t s) {
 }
 
 }  // namespace
-
-int64_t prompt_height(int64_t D) { return D <= 128 ? PromptShape<128>::rows : PromptShape<256>::rows; }
 
 int64_t prompt_row_tiles(int64_t S, int64_t T, int64_t group, int64_t D) {
     return S + (T * group + prompt_height(D) - 1) / prompt_height(D);  // one partial tile a request at most

@@ -140,6 +140,15 @@ def test_workspace_sizes(lib):
     assert size(1, 1, 8, 3, 128) == EINVAL and size(-1, 1, 8, 2, 128) == EINVAL and size(1, 1, 8, 2, 100) == EUNSUPPORTED
 
 
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("S, new, many", [(1, 32, False), (1, 64, True), (1, 512, True), (16, 8, False), (16, 16, False), (16, 32, True), (8, 32, False), (64, 16, True)])
+def test_the_kernel_for_a_size_is_the_same_for_all_heads(lib, D, S, new, many):
+    """Which kernel a call takes, seen from the workspace that it asks for: by rows and key heads, at every head size where it was measured."""
+    size = (S, S * new, 64, 8, D)
+    few_rows, many_rows = (lib.mx_internal_attention_kv_workspace(force, *size) for force in (1, 2))
+    assert lib.mx_attention_kv_workspace(*size) == (many_rows if many else few_rows)
+
+
 def test_binding_refuses_what_is_not_on_the_gpu():
     torch = pytest.importorskip("torch")
     import paper_2603_08713_amd as mx
