@@ -274,9 +274,19 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
 
 inline int lanes_of(int D) { return D <= 64 ? 8 : D <= 128 ? 16 : 32; }
 
-// Heads that a wavefront takes one after the other: one where the launch is small (its latency is what counts: 64 tokens of 80 heads, written
-// and read, 8.4 us; 2 heads 10.3, 4 heads 11.2), eight where it fills the device several times.
-inline int heads_per_wave(int64_t rows_of_waves) { return rows_of_waves > 32768 ? 8 : rows_of_waves > 8192 ? 4 : 1; }
+// Heads that a wavefront takes: one where the launch is small (its latency is what counts), two abreast where it fills the device, more where it
+// fills it several times and a token's angles are worth keeping.  us with 1, 2, 4, 8 heads, the line's choice starred:
+//   wavefronts of one head each                      norm, rotation                norm, rotation, write
+//     768  (64 tokens of 32 + 8 heads of 128)    4.1*  4.0   4.8   6.6          4.2*  4.6   5.8   8.4
+//    2400  (200)                                 4.5   4.1*  5.0   6.7          5.3   5.0*  5.9   8.5
+//    7200  (600)                                 8.2   5.7*  6.3   7.4         10.1   7.2*  7.4   9.1
+//    9600  (800)                                10.0   6.7   6.7*  7.6         12.5   9.1   8.7* 10.8
+//   31200  (2600)                               25.0  15.8  14.1* 14.1         31.6  19.5  17.5* 17.1
+//   36000  (3000)                               28.0  17.5  15.5  14.3*        35.4  21.6  19.1  19.6*
+//   98304  (8192)                               68.6  38.1  32.7  29.9*        89.3  50.6  40.8  38.7*
+// The write and the read by themselves: 5600 wavefronts 4.4, 4.2*, 4.9, 6.5 and 4.1, 4.1*, 4.4, 5.6; 16400 7.9, 7.1, 7.0*, 8.2 and 7.0, 6.6, 6.6*, 7.2;
+// 65536 23.6, 19.4, 19.0, 18.3* and 20.4, 17.5, 18.7, 17.0*.  Heads of 64 and 256 turn at the same places.
+inline int heads_per_wave(int64_t rows_of_waves) { return rows_of_waves > 32768 ? 8 : rows_of_waves > 8192 ? 4 : rows_of_waves > 2048 ? 2 : 1; }
 
 template <int kLanes, bool kTurn, bool kPairs>
 void launch_rows(const RowsArgs& a, bool cache, bool mbs, dim3 grid, hipStream_t s) {

@@ -279,6 +279,31 @@ def test_fused_write_is_the_two_calls(mx, D, style, norm, R, mbs, T, Hq, Hkv):
         assert _same(again, one) and bool((q_out[0] == 9.0).all()) and not bool((q_out[1] == 9.0).all())
 
 
+@pytest.mark.parametrize("T, Hq, Hkv, D", [(1500, 5, 3, 128), (3001, 5, 3, 128), (9000, 5, 7, 64), (700, 3, 5, 256), (12001, 5, 9, 128)])
+def test_heads_that_a_wavefront_takes_in_part(mx, oracle, T, Hq, Hkv, D):
+    """Sizes at which wavefronts take two, four and eight heads, none of them a divisor of the heads: norm and rotation, the write with and without them,
+    the read."""
+    page = 64
+    pages = T // page + 2
+    one, two = (_filled_cache(mx, 5, pages, Hkv, D, page, True) for _ in range(2))
+    qkv = _rows(D + T, T, Hq + 2 * Hkv, D)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    w = torch.linspace(0.5, 1.7, D, device="cuda").to(torch.bfloat16)
+    table, positions = _cos_sin(T, D), torch.arange(T, device="cuda").int()
+    slots = torch.randperm(pages * page, generator=_gen(T), device="cuda")[:T]
+    q_two, k_two = mx.mx_qk_norm_rope(q, k, positions, table, w, w)
+    some = torch.cat((torch.arange(70), torch.arange(T - 70, T)))
+    for x, y in ((q, q_two), (k, k_two)):
+        assert np.array_equal(ref.bits(ref.to_bf16(ref.norm_rope(x[some], positions[some], table, w, 1e-6, "half"))), ref.bits(y[some]))
+    mx.mx_kv_write(k_two, v, slots, *two)
+    q_one = mx.mx_qk_norm_rope_kv_write(q, k, v, positions, slots, table, *one, w, w)
+    assert np.array_equal(ref.bits(q_one), ref.bits(q_two)) and _same(one, two)
+    _check_rows(oracle, two, slots.cpu().numpy(), k_two, v, "oas", True)
+    for got, cache, is_key in zip(mx.mx_kv_read(slots, *two), two, (True, False)):
+        want = torch.from_numpy(ref.values(*ref.cached_rows(cache, is_key, slots.cpu().numpy()))).float().to(torch.bfloat16)
+        assert torch.equal(got.cpu(), want)
+
+
 def test_rows_on_another_stream_and_in_a_graph(mx):
     """Captured once and replayed over changed inputs, with eager work between the replays."""
     T, Hq, Hkv, D, page = 19, 4, 2, 128, 16
