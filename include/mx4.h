@@ -357,6 +357,11 @@ int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const uint8_t* k_sc
  * Scores, softmax and sums in fp32, weights rounded to bf16 for the product with the values.
  * A call with more rows than one launch holds returns MX_EINVAL: T Hq above 2^26 - 4 where requests bring few rows, and of about
  * 2^31 (heads above 128: 2^30) where they bring many.
+ * A call runs one of two kernels, for few or for many query rows a request, by the mean T / num_seqs.  Where a step brings single tokens and
+ * prompts together, two calls are faster, with the k single tokens first in the batch: one of k requests and T = k, one of the others by
+ * row_offsets + k, kv_lens + k, block_table + k * max_pages and the whole q and out (rows of other requests are not touched).  MI355X, 32 query
+ * heads on 8 of 128: 63 tokens behind up to 8192 keys and a chunk of 2048, 482 us in one call, 213 in two; 255 tokens and a prompt of 2048, 413 and
+ * 224; 64 on 8, a token behind 131072 keys among 6 others and a prompt of 2048, 3290 and 146.
  * |x_hat F| of the cache's rows has to be below 2^127 (what mx_kv_write stores of |x| < 2^125 is), and |v_hat| kv_lens[s] below 2^119: the
  * sums of values are kept in fp32 under weights of up to 2^8, before the division.  Beyond that results are infinite or NaN.
  * workspace: DEVICE memory, 16-byte aligned, of at least mx_attention_kv_workspace(...) bytes, which the call overwrites; calls

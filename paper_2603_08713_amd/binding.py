@@ -838,7 +838,9 @@ def mx_attention_kv_workspace(num_seqs, total_tokens, q_heads, kv_heads, head_di
 def mx_attention_kv(q, row_offsets, kv_lens, block_table, k_cache, v_cache, scale=None, causal=True, window=0, out=None, lse=None, workspace=None):
     """Attention of q [T, Hq, D] (bf16; request s has the rows row_offsets[s] .. row_offsets[s+1]-1) over the cache: request s has kv_lens[s]
     keys in the pages block_table[s].  scale: 1 / sqrt(D) if None.  lse: fp32 [T, Hq], filled if given.  workspace: uint8, if the caller keeps
-    one (calls that can run at the same time need one each); else it comes from the allocator.  Returns out, bf16 [T, Hq, D]."""
+    one (calls that can run at the same time need one each); else it comes from the allocator.  Returns out, bf16 [T, Hq, D].
+    Single tokens and prompts of one step are faster as two calls, the k single tokens first: q[:k], row_offsets[:k + 1], kv_lens[:k], block_table[:k],
+    out=out[:k], and q, row_offsets[k:], kv_lens[k:], block_table[k:], out=out."""
     if _native is not None and out is not None and not getattr(_dev, "choices", None) and _done(
             _native.attention_kv(q, row_offsets, kv_lens, block_table, *k_cache, *v_cache, q.shape[-1] ** -0.5 if scale is None else scale, causal, window, out,
                                  lse, workspace), "mx_attention_kv"):

@@ -27,6 +27,8 @@ bool good_shape(int64_t S, int64_t T, int64_t Hq, int64_t Hkv) {
 // (Heads of 96 lean to many rows a little sooner; above 128 the last one is lost because 128 to 250 tiles of 128 rows are neither cut nor
 // fill the device.)  Tiles are counted in 256 rows for all head sizes: counted in the 128 that a tile of heads above 128 has, 16 requests of 128
 // rows and 8 of 256 went to the slower kernel there.
+// The rule knows the mean and not the requests: single tokens among prompts are served badly by either kernel, and are better called apart (figures in
+// mx4.h at mx_attention_kv).
 bool is_prompt(int64_t S, int64_t T, int64_t Hq, int64_t Hkv) {
     const int64_t rows = T * (Hq / Hkv), tiles = rows / 256 * Hkv;
     return (rows >= 512 * S && tiles >= 16) || (rows > 64 * S && tiles >= 128);

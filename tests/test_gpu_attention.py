@@ -432,6 +432,24 @@ def test_a_captured_serving_step(mx):
         assert all(torch.equal(x, y) for name in ("k_cache", "v_cache") for x, y in zip(captured[name], eager[name]))
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("ones, prompts", [([300, 1, 4000, 17], [(200, 200), (64, 700)]), ([5000], [(530, 530)])])
+def test_prompts_and_single_tokens_by_two_calls(mx, D, ones, prompts):
+    """A step of both kinds: one call for all, and a call for the requests of each kind into one output; the rows of the other kind stay as they are."""
+    n, keys = [1] * len(ones) + [p[0] for p in prompts], ones + [p[1] for p in prompts]
+    b = Batch(mx, 23 + D, n, keys, 8, 2, D, 32, True, wide=2)
+    b.check()
+    q, offsets, lens, table, k = b.q, b.offsets, b.lens, b.table, len(ones)
+    out = torch.full(q.shape, 5.0, dtype=torch.bfloat16, device="cuda")
+    mx.mx_attention_kv(q[:k], offsets[:k + 1], lens[:k], table[:k], *b.caches, out=out[:k])
+    assert bool((out[k:] == 5.0).all())
+    first = out[:k].clone()
+    mx.mx_attention_kv(q, offsets[k:], lens[k:], table[k:], *b.caches, out=out)
+    assert torch.equal(out[:k], first) and bool((out[-2:] == 5.0).all())
+    want, _, tol, _, written = ref.attention(q, offsets, lens, table, *b.caches, D ** -0.5, True, 0)
+    assert (np.abs(out.cpu().double().numpy() - want) <= tol)[written].all()
+
+
 @pytest.mark.parametrize("n, keys, many", [([128], [128], True), ([128], [700], True), ([512, 30, 600], [512, 900, 1000], True), ([100], [100], False),
                                            ([1] * 40, list(range(1, 400, 10)), False), ([3, 200], [4000, 300], False)])
 def test_the_kernel_that_a_call_takes(n, keys, many):
