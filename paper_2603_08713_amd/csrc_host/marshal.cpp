@@ -525,10 +525,12 @@ MX_CALL(attention_kv) {  // q, row_offsets, kv_lens, block_table, the cache's si
             own = at_.any(a[15], at::kByte);
             need(own.dim() == 1 && own.is_contiguous());
         }
+        // (here, where an exception declines: under a dispatch mode of the caller's the allocator may give a tensor without an address)
+        void* work = own.data_ptr();
         void* st = at_.stream();
         return [=] {
             return calls.attention_kv(q.data, q.ld, off, lens, table, width, c.kc, c.ks, c.km, c.vc, c.vs, c.vm, c.pages, c.page, S, q.T, q.H, c.heads, c.D, scale, causal,
-                                      window, o.data, o.ld, lse, own.data_ptr(), own.numel(), st);
+                                      window, o.data, o.ld, lse, work, own.numel(), st);
         };
     });
 }

@@ -418,3 +418,32 @@ def test_native_marshalling_declines_what_the_binding_refuses(mx):
     assert native.kv_write(x, x[:, :1], slots, *kc, *vc, "oas") is None and native.kv_write(x, x, slots, *vc, *kc, "oas") is None
     assert native.kv_read(slots, *kc, *vc, "bf16", x.clone(), x.clone().float()) is None
     assert native.qk_norm_rope(x, x, None, torch.zeros((4, 128), device="cuda"), None, None, 1e-6, "half", x.clone(), x.clone()) is None
+
+
+def test_attention_under_dispatch_modes(mx):
+    """A mode of the caller's sees the workspace being allocated: one that hands on what it sees changes nothing, one that gives a tensor without memory
+    is an exception."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Passes(TorchDispatchMode):
+        seen = 0
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            Passes.seen += 1
+            return func(*args, **(kwargs or {}))
+
+    caches = mx.mx_kv_cache(2, 2, 128, 16)
+    x = _rows(1, 3, 2, 128)
+    mx.mx_kv_write(x, x, torch.arange(3, device="cuda"), *caches)
+    off, lens = torch.tensor([0, 3], device="cuda"), torch.tensor([3], dtype=torch.int32, device="cuda")
+    table = torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    want, out = mx.mx_attention_kv(x, off, lens, table, *caches), torch.zeros_like(x)
+    with Passes():
+        mx.mx_attention_kv(x, off, lens, table, *caches, out=out)
+    assert Passes.seen and torch.equal(out, want)
+    out.zero_()
+    with pytest.raises((RuntimeError, TypeError, ValueError)):
+        with FakeTensorMode(allow_non_fake_inputs=True):
+            mx.mx_attention_kv(x, off, lens, table, *caches, out=out)
+    assert not bool(out.any())
