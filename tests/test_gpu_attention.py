@@ -117,6 +117,45 @@ def test_rows_without_keys(mx, n, keys):
     b.check(causal=False)
 
 
+def test_more_requests_than_lanes(mx):
+    """Batches that a wavefront looks through 64 requests at a time, some of them without rows or keys, the lengths in no order."""
+    rng = np.random.default_rng(40)
+    for S, most, rows in ((64, 90, 2), (65, 40, 3), (200, 130, 2), (389, 20, 4)):
+        n = [int(x) for x in rng.integers(0, rows + 1, S)]
+        keys = [int(x) if rng.random() > 0.1 else 0 for x in rng.integers(1, most, S)]
+        n[S // 2], keys[S // 2] = 70, 200
+        Batch(mx, S, n, keys, 4, 2, 64, 16, True, wide=1).check()
+
+
+@pytest.mark.parametrize("Hq, Hkv, D, page", [(128, 1, 64, 16), (96, 2, 128, 32), (7, 7, 256, 16), (5, 1, 192, 4096), (4, 2, 96, 4096)])
+def test_many_heads_and_large_pages(mx, Hq, Hkv, D, page):
+    """One key head for all queries, as many as queries, key heads by an odd number of queries; pages of 4096."""
+    Batch(mx, Hq, [1, 9, 3], [150, 40, 70], Hq, Hkv, D, page, True).check()
+    Batch(mx, Hq + 1, [30], [200], Hq, Hkv, D, page, False).check(window=50)
+
+
+@pytest.mark.parametrize("window", [299, 300, 301, (1 << 30) - 1, 1 << 31, 1 << 40, (1 << 62)])
+def test_windows_as_long_as_the_keys(mx, window):
+    b = Batch(mx, 41, [1, 20, 5], [300, 300, 3], 4, 2, 128, 16, True)
+    out, lse = b.check(window=window)
+    if window >= 300:
+        want, want_lse = b.run()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("n, keys", [([1, 1], [2000, 20]), ([50, 3], [70, 900])])
+def test_strided_outputs(mx, D, n, keys):
+    """Rows of the output apart from each other, with and without lse: the same bits, and nothing beside them."""
+    b = Batch(mx, 42, n, keys, 4, 2, D, 16, True)
+    want, _ = b.run()
+    T, Hq, _ = want.shape
+    for wide in (1, 3):
+        out = torch.full((T + 1, Hq + wide, D), 9.0, dtype=torch.bfloat16, device="cuda")
+        mx.mx_attention_kv(b.q, b.offsets, b.lens, b.table, *b.caches, out=out[:T, :Hq])
+        assert torch.equal(out[:T, :Hq], want) and bool((out[:, Hq:] == 9.0).all()) and bool((out[T] == 9.0).all())
+
+
 def test_large_scores_and_scales(mx):
     """Scores far apart: one key takes all of a row, and the running maximum moves often."""
     for spread, scale in ((30.0, None), (1.0, 5.0), (1e-3, None), (2.0, -0.3), (1.0, 0.0)):

@@ -129,6 +129,19 @@ def test_plan_of_many_with_few_places(mx, S, most, new, page, part):
     assert got[4].item() == want[4] and np.array_equal(t.cpu().numpy(), want[5])
 
 
+def test_plan_of_lengths_that_32_bits_cannot_add(mx):
+    """Sums of new tokens and of pages beyond 2^31: the places that there are, every entry of the table, totals that stay at 2^31 - 1."""
+    most = (1 << 31) - 1
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.full((5, 4), 77, dtype=torch.int32, device="cuda")
+    offsets, lens, slots, positions, after = mx.mx_kv_plan(i32([20, 0, most, 0, 3]), i32([most, most, most, 5, -most]), 16, table, i32([9, 8, 7]), i32([1]), 12)
+    assert offsets.tolist() == [0, most, 2 * most, 3 * most, 3 * most + 5, 3 * most + 5] and lens.tolist() == [most, most, most, 5, 3]
+    # request 0 holds pages 0 and 1 of its row and takes entries 1 and 2 of the list (8 and 7); the others find it empty
+    assert table.tolist() == [[77, 77, 8, 7], [-1, -1, -1, -1], [77, 77, 77, 77], [-1, 77, 77, 77], [77, 77, 77, 77]]
+    assert positions.tolist() == list(range(20, 32)) and slots.tolist() == [77 * 16 + p for p in range(4, 16)]
+    assert after.item() == 1 + -(-(20 + most) // 16) - 2 + -(-most // 16) + -(-2 * most // 16) - -(-most // 16) + 1
+
+
 # ---- norm and rotation ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
 @pytest.mark.parametrize("style", ["half", "pairs"])
@@ -233,6 +246,30 @@ def test_write_and_read(mx, oracle, D, mbs, rule, page, T):
             want = torch.from_numpy(ref.values(*ref.cached_rows(cache, is_key, slots[ok]))).float().to(dtype)
             assert torch.equal(torch.nan_to_num(got[ok].cpu().float(), nan=-5.0), torch.nan_to_num(want.float(), nan=-5.0)), (name, is_key)
             assert bool((got[~ok] == 3.0).all())
+
+
+def test_strided_rows_out_and_one_array_only(mx):
+    """Outputs whose rows lie apart, and the C call that reads keys or values by themselves."""
+    T, Hq, H, D, page = 9, 3, 2, 128, 4096
+    caches = mx.mx_kv_cache(2, H, D, page)
+    q, k, v = _rows(1, T, Hq, D), _rows(2, T, H, D), _rows(3, T, H, D)
+    slots = torch.tensor([0, 4095, 4096, 8191, 17, 18, 19, 20, 5000], device="cuda")
+    mx.mx_kv_write(k, v, slots, *caches)
+    want = mx.mx_kv_read(slots, *caches)
+    out = torch.full((T, 2 * H + 1, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    mx.mx_kv_read(slots, *caches, k_out=out[:, :H], v_out=out[:, H:2 * H])
+    assert torch.equal(out[:, :H], want[0]) and torch.equal(out[:, H:2 * H], want[1]) and bool((out[:, 2 * H] == 3.0).all())
+    for is_key in (True, False):
+        one = torch.full((T, H, D), 3.0, dtype=torch.bfloat16, device="cuda")
+        at = [one.data_ptr() if is_key else None, H * D, None if is_key else one.data_ptr(), H * D]
+        arrays = [a.data_ptr() for cache in caches for a in cache]
+        assert mx.load_library().mx_kv_read(slots.data_ptr(), *arrays, 2, page, T, H, D, mx.MX_OUT_BF16, *at, torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(one, want[0 if is_key else 1])
+    table, positions = _cos_sin(16, D), torch.arange(T, device="cuda").int()
+    turned = mx.mx_qk_norm_rope(q, k, positions, table)
+    out = torch.full((T, Hq + H + 1, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    mx.mx_qk_norm_rope(q, k, positions, table, q_out=out[:, :Hq], k_out=out[:, Hq:Hq + H])
+    assert torch.equal(out[:, :Hq], turned[0]) and torch.equal(out[:, Hq:Hq + H], turned[1]) and bool((out[:, Hq + H] == 3.0).all())
 
 
 def test_write_equals_the_quantizer(mx):
