@@ -306,7 +306,7 @@ typedef enum {
  * free_start.  (A captured step that is replayed reads its ctx_lens and free_start again: it ends with copies of kv_lens and free_next
  * into them, or two graphs that write each other's take turns.  Without, every replay plans the first step's places anew.)  T is at least the sum of new_lens: tokens beyond T get no place, but row_offsets, kv_lens, free_next and block_table
  * count them and their pages all the same.  num_seqs <= 4096, else MX_EUNSUPPORTED;
- * max_pages * page_size <= 2^30.  kv_lens may not be ctx_lens or new_lens, free_next not free_start (MX_EINVAL). */
+ * max_pages * page_size <= 2^30.  What is written may not overlap ctx_lens, new_lens, free_pages or free_start (MX_EINVAL). */
 int mx_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int64_t num_seqs, int64_t page_size, int32_t* block_table,
                int64_t max_pages, const int32_t* free_pages, int64_t free_count, const int32_t* free_start, int64_t T,
                int64_t* row_offsets, int32_t* kv_lens, int64_t* slots, int32_t* positions, int32_t* free_next, void* stream);

@@ -129,6 +129,15 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(PlanArgs a) {
 
 constexpr int64_t kMostRequests = 4096;  // two numbers of each in LDS: 32 KiB
 
+struct Bytes {
+    const void* at;
+    int64_t size;
+};
+bool apart(Bytes a, Bytes b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return !a.size || !b.size || x + a.size <= y || y + b.size <= x;
+}
+
 }  // namespace
 }  // namespace mx
 
@@ -142,11 +151,15 @@ extern "C" int mx_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int6
     if (!row_offsets || !free_start || !free_next || (num_seqs && (!ctx_lens || !new_lens || !kv_lens || (max_pages && !block_table))) ||
         (free_count && !free_pages) || (T && (!slots || !positions)))
         return MX_ENULL;
-    // (every workgroup reads what the first one would overwrite)
-    if (free_next == free_start || (num_seqs && (kv_lens == ctx_lens || kv_lens == new_lens))) return MX_EINVAL;
     if (!aligned(ctx_lens, 4) || !aligned(new_lens, 4) || !aligned(free_pages, 4) || !aligned(free_start, 4) || !aligned(block_table, 4) ||
         !aligned(kv_lens, 4) || !aligned(positions, 4) || !aligned(free_next, 4) || !aligned(row_offsets, 8) || !aligned(slots, 8))
         return MX_EALIGN;
+    // every workgroup reads what another one would overwrite
+    const Bytes in[] = {{ctx_lens, 4 * num_seqs}, {new_lens, 4 * num_seqs}, {free_pages, 4 * free_count}, {free_start, 4}};
+    const Bytes out[] = {{block_table, 4 * num_seqs * max_pages}, {row_offsets, 8 * (num_seqs + 1)}, {kv_lens, 4 * num_seqs}, {slots, 8 * T}, {positions, 4 * T}, {free_next, 4}};
+    for (const Bytes& o : out)
+        for (const Bytes& i : in)
+            if (!apart(o, i)) return MX_EINVAL;
     if (int st = check_device()) return st;
     PlanArgs a;
     a.ctx_lens = ctx_lens; a.new_lens = new_lens; a.free_pages = free_pages; a.free_start = free_start;

@@ -99,6 +99,26 @@ def test_refusals(lib, name, base, bad):
         assert call(*_changed(base, **changes)) == status, (name, changes)
 
 
+B = 1 << 20  # bytes between arrays that lie apart
+APART = dict(PLAN, ctx=A, new=A + B, table=A + 2 * B, free=A + 3 * B, start=A + 4 * B, offsets=A + 5 * B, lens=A + 6 * B, slots=A + 7 * B, positions=A + 8 * B,
+             next=A + 9 * B)
+
+
+@pytest.mark.parametrize("out, size", [("table", 128), ("offsets", 40), ("lens", 16), ("slots", 80), ("positions", 40), ("next", 4)])
+@pytest.mark.parametrize("into, length", [("ctx", 16), ("new", 16), ("free", 36), ("start", 4)])
+def test_a_plan_does_not_write_what_it_reads(lib, out, size, into, length):
+    """Workgroups read the lengths and the free list while others write: an output on any byte of theirs is refused, one right beside them is not."""
+    step = 8 if out in ("offsets", "slots") else 4
+    at = APART[into]
+    for address in range(at - size // step * step + step, at + length, step):
+        assert lib.mx_kv_plan(*_changed(APART, **{out: address})) == EINVAL, address - at
+    import torch
+
+    if not torch.cuda.device_count():  # (the addresses are made up)
+        for address in (at - size, at + -(-length // step) * step):
+            assert lib.mx_kv_plan(*_changed(APART, **{out: address})) == EUNSUPPORTED, address - at
+
+
 def test_empty_calls_do_nothing(lib):
     """No tokens, no requests or no pages: nothing is launched, so no device is needed."""
     assert lib.mx_qk_norm_rope(*_changed(TURN, T=0)) == OK
