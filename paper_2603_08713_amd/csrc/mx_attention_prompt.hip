@@ -3,19 +3,23 @@
 // A workgroup takes 32 rows for each of its wavefronts - (token, query head of the key head) - and goes through the keys that any
 // of them sees, 64 at a time.  The codes of a tile are expanded once for the workgroup: each wavefront turns its part of K or V into
 // operands of the matrix instruction (32 x 32 x 16, transposed as in mx_attention.h) and writes them to LDS in the order in which a
-// lane reads them, 16 bytes a lane, so that reads meet no conflicts and K and V need no further shuffling.  Two tiles of K and of V
-// in LDS: while one is multiplied the next is expanded from codes that were loaded a tile earlier; one barrier a tile.
+// lane reads them, 16 bytes a lane one behind the other, so that reads meet no conflicts and K and V need no further shuffling.  V's writes do: 8
+// bytes a lane, 32 from one lane to the next, on half of the banks (the 1.4e7 conflict clocks beside 2.0e7 of LDS instructions that the counters
+// show on the case below).  Two tiles of K and of V in LDS: while one is multiplied the next is expanded from codes that were loaded a tile
+// earlier; one barrier a tile.
 //
 // Lane l has query row l mod 32 and, of 32 keys, those with bit 2 = l / 32: a row's maximum and sum need one exchange.  V's columns
 // are dealt to the 32 rows of an operand so that a lane ends with runs of neighbouring columns of its row.
 //
 // What bounds it, at four prompts of 4096 tokens or fewer, 32 heads on 8 of 128 (276 GFLOP counted under the mask, 343 us = 805 TFLOP/s,
-// a bf16 library product of 8192^3 on the same card: 1375): the issue of vector instructions.  A wavefront's tile is 32 matrix
-// instructions (32 clocks each) and 284 vector instructions.  With parts of the kernel left out: everything but loads, barriers and what a
-// workgroup begins and ends with 157 us (70 of it the beginnings and ends alone, 1344 workgroups), the weights by themselves 113 more, the products
-// 114, the expansion 48.  The two wavefronts of a SIMD work in opposite phases, one in its products while the other weighs
-// (505 -> 436 us when it was done); the weights of a single wavefront, 6 clocks an instruction, are then the longer of the two.  Neither half the reads of LDS (363
-// for 368) nor wavefront priorities (351 to 355 for 350) change it; 128 rows a workgroup, two of them on a compute unit, take 403.
+// a bf16 library product of 8192^3 on the same card: 1375): its schedule.  A wavefront's tile is 32 matrix instructions (32 clocks each) and 284
+// vector instructions; of a SIMD's clocks the former have 33 % and the latter 45 %, so neither unit is full.  The two wavefronts of a SIMD work in
+// opposite phases, one in its products while the other weighs (505 -> 436 us when it was done): the vector ALU is fed by one wavefront at a time, an
+// instruction in 6 clocks where two together reach 4, and a tile takes about twice the longer phase.  With parts of the kernel left out:
+// everything but loads, barriers and what a workgroup begins and ends with 157 us (70 of it the beginnings and ends alone, 1344 workgroups), the
+// weights by themselves 113 more, the products 114, the expansion 48.  Neither half the reads of LDS (363 for 368) nor wavefront priorities (351 to
+// 355 for 350) change it; 128 rows a workgroup, two of them on a compute unit, take 403.  Heads above 128 have one wavefront a SIMD and no opposite
+// phase: one prompt of 4096 tokens, 32 heads on 8, takes 149 us with heads of 96, 586 with 192, 694 with 256 (693, 352 and 396 TFLOP/s).
 #include "mx_attention.h"
 #include "mx_gemm_shared.h"
 
