@@ -304,9 +304,9 @@ typedef enum {
  * A token whose page is missing (free_pages or the table's row is at its end) gets slot -1.  All arrays are DEVICE memory;
  * nothing is allocated on the host, so the call can be captured; the next step takes kv_lens and free_next as its ctx_lens and
  * free_start.  (A captured step that is replayed reads its ctx_lens and free_start again: it ends with copies of kv_lens and free_next
- * into them, or two graphs that write each other's take turns.  Without, every replay plans the first step's places anew.)  T is at least the sum of new_lens: tokens beyond T get no place, but row_offsets, kv_lens, free_next and block_table
- * count them and their pages all the same.  num_seqs <= 4096, else MX_EUNSUPPORTED;
- * max_pages * page_size <= 2^30.  What is written may not overlap ctx_lens, new_lens, free_pages or free_start (MX_EINVAL). */
+ * into them, or two graphs that write each other's take turns.  Without, every replay plans the first step's places anew.)
+ * T is at least the sum of new_lens: tokens beyond T get no place, but row_offsets, kv_lens, free_next and block_table count them and
+ * their pages all the same.  num_seqs <= 4096, else MX_EUNSUPPORTED; max_pages * page_size <= 2^30.  What is written may not overlap ctx_lens, new_lens, free_pages or free_start (MX_EINVAL). */
 int mx_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int64_t num_seqs, int64_t page_size, int32_t* block_table,
                int64_t max_pages, const int32_t* free_pages, int64_t free_count, const int32_t* free_start, int64_t T,
                int64_t* row_offsets, int32_t* kv_lens, int64_t* slots, int32_t* positions, int32_t* free_next, void* stream);
@@ -351,8 +351,8 @@ int mx_kv_read(const int64_t* slots, const uint8_t* k_codes, const uint8_t* k_sc
  *   causal:      keys 0 .. p, p = kv_lens[s] - n + i;  with window > 0 only the last `window` of them
  *   not causal:  all keys (window must be 0)
  * of those whose page exists.  out = softmax(scale q . k_hat) v_hat, bf16 [T, Hq, D]; lse (natural logarithm of the sum of
- * exponentials, fp32 [T, Hq]) if not NULL; out does not overlap q.  A row that sees no key: zeros, -inf.  A row
- * that sees keys whose scores are all -inf (an infinity in its query, or 2e38 passed): NaN.  Rows at or beyond row_offsets[num_seqs] are not
+ * exponentials, fp32 [T, Hq]) if not NULL; out does not overlap q.  A row that sees no key: zeros, -inf.  A row that sees keys
+ * whose scores are all -inf (an infinity in its query) or below -2e38: NaN.  Rows at or beyond row_offsets[num_seqs] are not
  * written.  Requests' rows do not overlap.  NaN in a key or value reaches the rows that see it and no others.
  * Scores, softmax and sums in fp32, weights rounded to bf16 for the product with the values.
  * A call with more rows than one launch holds returns MX_EINVAL: T Hq above 2^26 - 4 where requests bring few rows, and of about
