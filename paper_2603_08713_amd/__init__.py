@@ -11,5 +11,6 @@ from .binding import (  # noqa: F401
     mx_dequantize, mx_dequantize_elem, mx_gemm, mx_gemm_mbs, mx_gemm_mbs_elem, mx_gemm_mbs_elem_grouped, mx_gemm_mbs_grouped, mx_gemm_mbs_quantize_a, mx_quantize,
     mx_quantize_elem, mx_quantize_elem_mbs_dynamic, mx_quantize_mbs,
     mx_attention_kv, mx_attention_kv_workspace, mx_kv_cache, mx_kv_plan, mx_kv_read, mx_kv_write, mx_qk_norm_rope, mx_qk_norm_rope_kv_write,
+    MX_SCORE_SIGMOID, MX_SCORE_SOFTMAX, mx_gemm_block128, mx_gemm_block128_grouped, mx_moe_combine, mx_moe_plan, mx_moe_plan_workspace, mx_quantize_block128,
     mx_mbs_lut_build, mx_quantize_mbs_dynamic, mx_quantize_mbs_dynamic_lut, mx_quantize_mbs_dynamic_lut_static, mx_quantize_mbs_pair, mx_quantize_oas, mx_status_string, mx_version,
 )

@@ -18,6 +18,7 @@ _MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
 
 MX_RULE_OCP, MX_RULE_FLOOR, MX_RULE_OAS = 0, 1, 2
 MX_OUT_F32, MX_OUT_BF16 = 0, 1
+MX_SCORE_SOFTMAX, MX_SCORE_SIGMOID = 0, 1
 MX_ELEM_E2M1, MX_ELEM_E4M3, MX_ELEM_E5M2, MX_ELEM_E2M3, MX_ELEM_E3M2 = 0, 1, 2, 3, 4
 _ELEMS = {"e2m1": MX_ELEM_E2M1, "e4m3": MX_ELEM_E4M3, "e5m2": MX_ELEM_E5M2, "e2m3": MX_ELEM_E2M3, "e3m2": MX_ELEM_E3M2}
 _RULES = {"ocp": MX_RULE_OCP, "floor": MX_RULE_FLOOR, "oas": MX_RULE_OAS}
@@ -115,6 +116,18 @@ def load_library() -> ctypes.CDLL:
     L.mx_internal_attention_kv_workspace.argtypes = [ci, i64, i64, i64, i64, i64]
     L.mx_attention_kv_workspace.restype = i64
     L.mx_attention_kv_workspace.argtypes = [i64, i64, i64, i64, i64]
+    L.mx_quantize_block128.restype = ci
+    L.mx_quantize_block128.argtypes = [ci, vp, i64, i64, i64, i64, i64, vp, vp, vp]
+    L.mx_gemm_block128.restype = ci
+    L.mx_gemm_block128.argtypes = [ci, vp, vp, ci, vp, vp, i64, i64, i64, ci, vp, i64, vp]
+    L.mx_gemm_block128_grouped.restype = ci
+    L.mx_gemm_block128_grouped.argtypes = [ci, vp, vp, i64, vp, ci, vp, vp, i32, vp, i64, i64, i64, ci, vp, i64, vp]
+    L.mx_moe_plan.restype = ci
+    L.mx_moe_plan.argtypes = [ci, vp, i64, i64, vp, i64, i64, ci, vp, ci, f, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.mx_moe_plan_workspace.restype = i64
+    L.mx_moe_plan_workspace.argtypes = [i64, i64, i64]
+    L.mx_moe_combine.restype = ci
+    L.mx_moe_combine.argtypes = [ci, vp, i64, i64, vp, vp, i64, i64, i64, ci, vp, i64, vp, i64, vp]
     _lib = L
     return L
 
@@ -204,7 +217,8 @@ def _torch():
 # (in the order in which csrc_host/marshal.cpp keeps the addresses)
 _NATIVE_CALLS = ("mx_quantize", "mx_quantize_mbs", "mx_quantize_mbs_pair", "mx_quantize_mbs_dynamic", "mx_quantize_elem", "mx_dequantize", "mx_gemm",
                  "mx_gemm_mbs", "mx_gemm_mbs_grouped", "mx_gemm_mbs_quantize_a", "mx_gemm_mbs_elem", "mx_gemm_mbs_elem_grouped", "mx_kv_plan",
-                 "mx_qk_norm_rope", "mx_kv_write", "mx_qk_norm_rope_kv_write", "mx_kv_read", "mx_attention_kv", "mx_attention_kv_workspace")
+                 "mx_qk_norm_rope", "mx_kv_write", "mx_qk_norm_rope_kv_write", "mx_kv_read", "mx_attention_kv", "mx_attention_kv_workspace",
+                 "mx_quantize_block128", "mx_gemm_block128", "mx_gemm_block128_grouped", "mx_moe_plan", "mx_moe_plan_workspace", "mx_moe_combine")
 
 
 def marshal_tag(torch) -> str:
@@ -872,4 +886,158 @@ def mx_attention_kv(q, row_offsets, kv_lens, block_table, k_cache, v_cache, scal
         _check((_lib or load_library()).mx_internal_attention_kv(int(force), *arguments), "mx_attention_kv (mx_internal_attention_kv)")
     else:
         _check((_lib or load_library()).mx_attention_kv(*arguments), "mx_attention_kv")
+    return out
+
+
+# ---- FP8 with an fp32 scale for each block of 128, and routing among experts -------------------------------------
+_SCORES = {"softmax": MX_SCORE_SOFTMAX, "sigmoid": MX_SCORE_SIGMOID}
+
+
+def _blocks(n):
+    return (n + 127) // 128
+
+
+def _operand128(codes, scales, name):
+    """Codes [rows, K] and scales of an operand, on the current device -> rows, K."""
+    torch = _torch_module or _torch()
+    rows, K = _here(codes, torch.uint8, name + " codes", 2).shape
+    _flat(codes, torch.uint8, (rows, K), name + " codes")
+    _here(scales, torch.float32, name + " scales", 2)
+    return rows, K
+
+
+def mx_quantize_block128(x, elem="e4m3", block_rows=1, num_groups=1, codes=None, scales=None):
+    """bf16 [rows, K] -> (codes uint8 [rows, K], scales fp32) in E4M3 or E5M2 with a scale for each block of block_rows x 128: block_rows = 1 (activations;
+    scales [rows, ceil(K/128)]) or 128 (weights; x holds num_groups matrices stacked along rows, each of whose blocks end with it: scales
+    [num_groups * ceil(rows/num_groups/128), ceil(K/128)]).  codes.view(torch.float8_e4m3fn) (or float8_e5m2) times the scales is what they stand for."""
+    if _native is not None and codes is not None and scales is not None and _done(
+            _native.quantize_block128(x, elem, block_rows, num_groups, codes, scales), "mx_quantize_block128"):
+        return codes, scales
+    torch = _torch_module or _torch()
+    rows, K, ldx = _rows_ld(x)
+    _here(x, torch.bfloat16, "x", 2)
+    groups, block_rows = int(num_groups), int(block_rows)
+    if groups < 1 or rows % groups or block_rows not in (1, 128):
+        raise ValueError("num_groups must divide the rows, and block_rows be 1 or 128")
+    each = rows // groups
+    codes = torch.empty((rows, K), dtype=torch.uint8, device=x.device) if codes is None else _flat(codes, torch.uint8, (rows, K), "codes")
+    shape = (rows if block_rows == 1 else groups * _blocks(each), _blocks(K))
+    scales = torch.empty(shape, dtype=torch.float32, device=x.device) if scales is None else _flat(scales, torch.float32, shape, "scales")
+    _check((_lib or load_library()).mx_quantize_block128(_elem(elem), _ptr(x), groups, each, K, ldx, block_rows, _ptr(codes), _ptr(scales), _stream()),
+           "mx_quantize_block128")
+    return codes, scales
+
+
+def mx_gemm_block128(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, out_dtype="f32", out=None):
+    """C = A B^T: A [M, K] with scales for 1 x 128, B [N, K] with scales for 128 x 128, both as mx_quantize_block128 gives them."""
+    if _native is not None and out is not None and _done(
+            _native.gemm_block128(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, out_dtype, out), "mx_gemm_block128"):
+        return out
+    torch = _torch_module or _torch()
+    (M, K), (N, Kb) = _operand128(a_codes, a_scales, "a"), _operand128(b_codes, b_scales, "b")
+    if K != Kb:
+        raise ValueError("A and B disagree on K")
+    _flat(a_scales, torch.float32, (M, _blocks(K)), "a scales")
+    _flat(b_scales, torch.float32, (_blocks(N), _blocks(K)), "b scales")
+    code, out, ldc = _c_tensor(M, N, out_dtype, out, a_codes.device)
+    _here(out, out.dtype, "out")
+    _check((_lib or load_library()).mx_gemm_block128(_elem(a_elem), _ptr(a_codes), _ptr(a_scales), _elem(b_elem), _ptr(b_codes), _ptr(b_scales), M, N, K,
+                                                     code, _ptr(out), ldc, _stream()), "mx_gemm_block128")
+    return out
+
+
+def mx_gemm_block128_grouped(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, row_offsets, N, out_dtype="f32", a_rows=None, out=None):
+    """Grouped form of mx_gemm_block128: rows row_offsets[e]..row_offsets[e+1]-1 of C are rows of A times B_e^T, B stacked [G*N, K] (scales
+    [G*ceil(N/128), ceil(K/128)]).  a_rows (int32, a row of A for each row of C: the tokens of mx_moe_plan): A's rows are taken where they lie."""
+    if _native is not None and out is not None and _done(
+            _native.gemm_block128_grouped(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, row_offsets, N, out_dtype, a_rows, out), "mx_gemm_block128_grouped"):
+        return out
+    torch = _torch_module or _torch()
+    (A, K), (NB, Kb) = _operand128(a_codes, a_scales, "a"), _operand128(b_codes, b_scales, "b")
+    G = _here(row_offsets, torch.int64, "row_offsets", 1).shape[0] - 1
+    _flat(row_offsets, torch.int64, (G + 1,), "row_offsets")
+    N = int(N)
+    if G < 0 or NB != G * N or K != Kb:
+        raise ValueError("B must hold num_groups stacked [N, K] weights")
+    _flat(a_scales, torch.float32, (A, _blocks(K)), "a scales")
+    _flat(b_scales, torch.float32, (G * _blocks(N), _blocks(K)), "b scales")
+    M = A
+    if a_rows is not None:
+        M = _here(a_rows, torch.int32, "a_rows", 1).shape[0]
+        _flat(a_rows, torch.int32, (M,), "a_rows")
+    code, out, ldc = _c_tensor(M, N, out_dtype, out, a_codes.device)
+    _here(out, out.dtype, "out")
+    _check((_lib or load_library()).mx_gemm_block128_grouped(_elem(a_elem), _ptr(a_codes), _ptr(a_scales), A, _ptr(a_rows), _elem(b_elem), _ptr(b_codes),
+                                                             _ptr(b_scales), G, _ptr(row_offsets), M, N, K, code, _ptr(out), ldc, _stream()),
+           "mx_gemm_block128_grouped")
+    return out
+
+
+def mx_moe_plan_workspace(num_tokens, num_experts, top_k) -> int:
+    """Bytes of workspace that mx_moe_plan wants for these sizes."""
+    need = (_lib or load_library()).mx_moe_plan_workspace(num_tokens, num_experts, top_k)
+    _check(min(need, 0), "mx_moe_plan_workspace")
+    return need
+
+
+def mx_moe_plan(logits, top_k, scoring="softmax", bias=None, renormalize=True, scale=1.0, num_tokens=None, experts=None, weights=None, row_offsets=None,
+                rows=None, tokens=None, workspace=None):
+    """The top_k experts of every token from logits [T, E] (fp32 or bf16), and the places of their rows in the experts' order.  scoring: "softmax" or "sigmoid"
+    (with which a bias, fp32 [E], may be added for the choice alone).  num_tokens (int64 [1] on the GPU): tokens behind it are padding.  workspace: uint8, if the
+    caller keeps one (calls that can run at the same time need one each); else it comes from the allocator.  Returns (experts int32, weights fp32 [T, k],
+    row_offsets int64 [E+1], rows int32 [T, k], tokens int32 [T*k]): row_offsets for the grouped products, `tokens` for their a_rows, `rows` and `weights` for
+    mx_moe_combine."""
+    if _native is not None and tokens is not None and _done(
+            _native.moe_plan(logits, top_k, scoring, bias, renormalize, float(scale), num_tokens, experts, weights, row_offsets, rows, tokens, workspace), "mx_moe_plan"):
+        return experts, weights, row_offsets, rows, tokens
+    torch = _torch_module or _torch()
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("logits must be fp32 or bf16")
+    T, E = _here(logits, logits.dtype, "logits", 2).shape
+    ld, inner = logits.stride()
+    if inner != 1 and E > 1:
+        raise ValueError("innermost dimension must be contiguous")
+    ld, k = (ld if T > 1 else max(ld, E)), int(top_k)
+    need = mx_moe_plan_workspace(T, E, k)
+    if bias is not None:
+        _flat(bias, torch.float32, (E,), "bias")
+    if num_tokens is not None:
+        _flat(num_tokens, torch.int64, (1,), "num_tokens")
+
+    def output(t, dtype, shape, name):
+        return torch.empty(shape, dtype=dtype, device=logits.device) if t is None else _flat(t, dtype, shape, name)
+
+    experts, weights = output(experts, torch.int32, (T, k), "experts"), output(weights, torch.float32, (T, k), "weights")
+    row_offsets = output(row_offsets, torch.int64, (E + 1,), "row_offsets")
+    rows, tokens = output(rows, torch.int32, (T, k), "rows"), output(tokens, torch.int32, (T * k,), "tokens")
+    workspace = output(None, torch.uint8, (need,), "workspace") if workspace is None else _here(workspace, torch.uint8, "workspace", 1)
+    _flat(workspace, torch.uint8, workspace.shape, "workspace")
+    _check((_lib or load_library()).mx_moe_plan(MX_OUT_BF16 if logits.dtype is torch.bfloat16 else MX_OUT_F32, _ptr(logits), ld, T, _ptr(num_tokens), E, k,
+                                                _SCORES[scoring] if isinstance(scoring, str) else int(scoring), _ptr(bias), int(bool(renormalize)), scale,
+                                                _ptr(experts), _ptr(weights), _ptr(row_offsets), _ptr(rows), _ptr(tokens), _ptr(workspace) or None,
+                                                workspace.numel(), _stream()), "mx_moe_plan")
+    return experts, weights, row_offsets, rows, tokens
+
+
+def mx_moe_combine(y, rows, weights, add=None, out_dtype="bf16", out=None):
+    """out[t] = add[t] + sum_j weights[t, j] * y[rows[t, j]]: y [R, N] (fp32 or bf16), rows int32 and weights fp32 [T, k] as mx_moe_plan gives them, add (or None)
+    and out [T, N] of out_dtype; out may be add itself."""
+    if _native is not None and out is not None and _done(_native.moe_combine(y, rows, weights, add, out_dtype, out), "mx_moe_combine"):
+        return out
+    torch = _torch_module or _torch()
+    if not isinstance(y, torch.Tensor) or y.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("y must be fp32 or bf16")
+    R, N = _here(y, y.dtype, "y", 2).shape
+    T, k = _here(rows, torch.int32, "rows", 2).shape
+    _flat(rows, torch.int32, (T, k), "rows")
+    _flat(weights, torch.float32, (T, k), "weights")
+    _, y, ldy = _matrix(R, N, y.dtype, y, y.device, "y must have a contiguous last dimension")
+    code, out, ldo = _c_tensor(T, N, out_dtype, out, y.device)
+    _here(out, out.dtype, "out")
+    lda = 0
+    if add is not None:
+        _here(add, out.dtype, "add", 2)
+        _, add, lda = _matrix(T, N, out.dtype, add, y.device, "add must be [T, N] of the requested dtype with a contiguous last dimension")
+    _check((_lib or load_library()).mx_moe_combine(MX_OUT_BF16 if y.dtype is torch.bfloat16 else MX_OUT_F32, _ptr(y), R, ldy, _ptr(rows), _ptr(weights), T, k, N,
+                                                   code, _ptr(add), lda, _ptr(out), ldo, _stream()), "mx_moe_combine")
     return out

@@ -40,6 +40,12 @@ struct Calls {  // the C entry points, by the addresses that the binding passes 
     decltype(&mx_kv_read) kv_read;
     decltype(&mx_attention_kv) attention_kv;
     decltype(&mx_attention_kv_workspace) attention_kv_workspace;
+    decltype(&mx_quantize_block128) quantize_block128;
+    decltype(&mx_gemm_block128) gemm_block128;
+    decltype(&mx_gemm_block128_grouped) gemm_block128_grouped;
+    decltype(&mx_moe_plan) moe_plan;
+    decltype(&mx_moe_plan_workspace) moe_plan_workspace;
+    decltype(&mx_moe_combine) moe_combine;
 } calls;
 
 struct Declined {};  // the arguments are not what is served here
@@ -535,6 +541,149 @@ MX_CALL(attention_kv) {  // q, row_offsets, kv_lens, block_table, the cache's si
     });
 }
 
+// ---- FP8 with an fp32 scale for each block of 128, and routing: every tensor is on the current device, or the call is declined ----
+int64_t blocks(int64_t n) { return (n + 127) / 128; }
+struct Matrix {  // rows of any distance
+    void* data;
+    int64_t rows, cols, ld;
+};
+Matrix rows_of(const Here& here, PyObject* o, at::ScalarType type) {
+    const at::Tensor& t = here.any(o, type);
+    need(t.dim() == 2);
+    const Matrix m = {address<void>(t), t.size(0), t.size(1), t.stride(0)};
+    need(t.stride(1) == 1 || m.cols <= 1);
+    return {m.data, m.rows, m.cols, m.rows > 1 ? m.ld : std::max(m.ld, m.cols)};
+}
+mx_dtype_t float_type(PyObject* o, at::ScalarType& as) {
+    as = tensor(o).scalar_type();
+    need(as == at::kFloat || as == at::kBFloat16);
+    return as == at::kFloat ? MX_OUT_F32 : MX_OUT_BF16;
+}
+
+MX_CALL(quantize_block128) {  // x, elem, block_rows, num_groups, codes, scales
+    return run(a, n, "tsiitt", [&] {
+        const Here at_;
+        const Matrix x = rows_of(at_, a[0], at::kBFloat16);
+        const mx_elem_t e = elem(a[1]);
+        const int64_t block_rows = integer(a[2]), groups_ = integer(a[3]);
+        need((block_rows == 1 || block_rows == 128) && groups_ >= 1 && x.rows % groups_ == 0);
+        const int64_t each = x.rows / groups_;
+        uint8_t* c = at_.flat<uint8_t>(a[4], at::kByte, {x.rows, x.cols});
+        float* s = at_.flat<float>(a[5], at::kFloat, {block_rows == 1 ? x.rows : groups_ * blocks(each), blocks(x.cols)});
+        void* st = at_.stream();
+        return [=] { return calls.quantize_block128(e, x.data, groups_, each, x.cols, x.ld, block_rows, c, s, st); };
+    });
+}
+struct Operand128 {
+    const uint8_t* codes;
+    const float* scales;
+    int64_t rows, K;
+};
+Operand128 operand128(const Here& here, PyObject* codes, PyObject* scales, int64_t scale_rows) {  // scale_rows < 0: as many as rows
+    const at::Tensor& c = here.any(codes, at::kByte);
+    need(c.dim() == 2 && c.is_contiguous());
+    const int64_t rows = c.size(0), K = c.size(1);
+    return {address(c), here.flat<const float>(scales, at::kFloat, {scale_rows < 0 ? rows : scale_rows, blocks(K)}), rows, K};
+}
+MX_CALL(gemm_block128) {  // a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, type, out
+    return run(a, n, "sttsttdt", [&] {
+        const Here at_;
+        const mx_elem_t ae = elem(a[0]), be = elem(a[3]);
+        const Operand128 x = operand128(at_, a[1], a[2], -1), w = operand128(at_, a[4], a[5], blocks(matrix(a[4]).size(0)));
+        need(x.K == w.K);
+        const Out o = out_matrix(a[6], a[7], x.rows, w.rows);
+        at_.any(a[7], o.type == MX_OUT_F32 ? at::kFloat : at::kBFloat16);
+        void* st = at_.stream();
+        return [=] { return calls.gemm_block128(ae, x.codes, x.scales, be, w.codes, w.scales, x.rows, w.rows, x.K, o.type, o.data, o.ld, st); };
+    });
+}
+MX_CALL(gemm_block128_grouped) {  // a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, row_offsets, N, type, a_rows, out
+    return run(a, n, "sttstttidot", [&] {
+        const Here at_;
+        const mx_elem_t ae = elem(a[0]), be = elem(a[3]);
+        const at::Tensor& off = at_.any(a[6], at::kLong);
+        need(off.dim() == 1 && off.size(0) >= 1 && off.is_contiguous());
+        const int64_t count = off.size(0) - 1, N = integer(a[7]);
+        need(N >= 0 && count <= INT32_MAX);
+        const Operand128 x = operand128(at_, a[1], a[2], -1), w = operand128(at_, a[4], a[5], count * blocks(N));
+        need(x.K == w.K && w.rows == count * N);
+        int64_t M = x.rows;
+        const int32_t* index = nullptr;
+        if (a[9] != Py_None) {
+            const at::Tensor& i = at_.any(a[9], at::kInt);
+            need(i.dim() == 1 && i.is_contiguous());
+            M = i.size(0);
+            index = address<const int32_t>(i);
+        }
+        const Out o = out_matrix(a[8], a[10], M, N);
+        at_.any(a[10], o.type == MX_OUT_F32 ? at::kFloat : at::kBFloat16);
+        const int64_t* offsets = address<const int64_t>(off);
+        void* st = at_.stream();
+        return [=] {
+            return calls.gemm_block128_grouped(ae, x.codes, x.scales, x.rows, index, be, w.codes, w.scales, (int32_t)count, offsets, M, N, x.K, o.type, o.data, o.ld, st);
+        };
+    });
+}
+MX_CALL(moe_plan) {  // logits, top_k, scoring, bias, renormalize, scale, num_tokens, experts, weights, row_offsets, rows, tokens, workspace
+    return run(a, n, "tisobfottttto", [&] {
+        static const char* const kScores[] = {"softmax", "sigmoid"};  // MX_SCORE_SOFTMAX, MX_SCORE_SIGMOID
+        const Here at_;
+        at::ScalarType as;
+        const mx_dtype_t type = float_type(a[0], as);
+        const Matrix x = rows_of(at_, a[0], as);
+        const int64_t T = x.rows, E = x.cols, k = integer(a[1]);
+        need(k >= 0);
+        const mx_score_t score = (mx_score_t)name_of(a[2], kScores);
+        const float* bias = at_.flat_or_null<const float>(a[3], at::kFloat, {E});
+        const int renormalize = flag(a[4]);
+        const float scale = (float)PyFloat_AS_DOUBLE(a[5]);
+        const int64_t* count = at_.flat_or_null<const int64_t>(a[6], at::kLong, {1});
+        int32_t *experts = at_.flat<int32_t>(a[7], at::kInt, {T, k}), *rows = at_.flat<int32_t>(a[10], at::kInt, {T, k}), *tokens = at_.flat<int32_t>(a[11], at::kInt, {T * k});
+        float* weights = at_.flat<float>(a[8], at::kFloat, {T, k});
+        int64_t* offsets = at_.flat<int64_t>(a[9], at::kLong, {E + 1});
+        // (without a workspace of the caller's one from the allocator, which gives it to later work on this stream only)
+        at::Tensor own;
+        void* work = nullptr;
+        int64_t size = calls.moe_plan_workspace(T, E, k);
+        need(size >= 0);
+        if (a[12] != Py_None) {
+            own = at_.any(a[12], at::kByte);
+            need(own.dim() == 1 && own.is_contiguous());
+            size = own.numel();
+        } else if (size) {
+            own = at::empty({size}, tensor(a[0]).options().dtype(at::kByte));
+        }
+        if (own.defined()) work = own.data_ptr();
+        void* st = at_.stream();
+        return [=] {
+            return calls.moe_plan(type, x.data, x.ld, T, count, E, k, score, bias, renormalize, scale, experts, weights, offsets, rows, tokens, work, own.defined() ? size : 0, st);
+        };
+    });
+}
+MX_CALL(moe_combine) {  // y, rows, weights, add, type, out
+    return run(a, n, "tttodt", [&] {
+        const Here at_;
+        at::ScalarType as;
+        const mx_dtype_t type = float_type(a[0], as);
+        const Matrix y = rows_of(at_, a[0], as);
+        const at::Tensor& r = at_.any(a[1], at::kInt);
+        need(r.dim() == 2 && r.is_contiguous());
+        const int64_t T = r.size(0), k = r.size(1);
+        const int32_t* rows = address<const int32_t>(r);
+        const float* weights = at_.flat<const float>(a[2], at::kFloat, {T, k});
+        const Out o = out_matrix(a[4], a[5], T, y.cols);
+        const at::ScalarType out_as = o.type == MX_OUT_F32 ? at::kFloat : at::kBFloat16;
+        at_.any(a[5], out_as);
+        Matrix add = {nullptr, T, y.cols, 0};
+        if (a[3] != Py_None) {
+            add = rows_of(at_, a[3], out_as);
+            need(add.rows == T && add.cols == y.cols);
+        }
+        void* st = at_.stream();
+        return [=] { return calls.moe_combine(type, y.data, y.rows, y.ld, rows, weights, T, k, y.cols, o.type, add.data, add.ld, o.data, o.ld, st); };
+    });
+}
+
 // entry points' addresses, in the order of `Calls`
 PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
     constexpr Py_ssize_t kCount = sizeof(Calls) / sizeof(void*);
@@ -562,7 +711,8 @@ PyObject* built_for(PyObject*, PyObject* const*, Py_ssize_t) { return PyUnicode_
 PyMethodDef methods[] = {MX_METHOD(built_for), MX_METHOD(use), MX_METHOD(quantize), MX_METHOD(quantize_mbs), MX_METHOD(quantize_mbs_pair), MX_METHOD(quantize_mbs_dynamic),
                          MX_METHOD(quantize_elem), MX_METHOD(dequantize), MX_METHOD(gemm), MX_METHOD(gemm_mbs), MX_METHOD(gemm_mbs_grouped),
                          MX_METHOD(gemm_mbs_quantize_a), MX_METHOD(gemm_mbs_elem), MX_METHOD(gemm_mbs_elem_grouped), MX_METHOD(kv_plan), MX_METHOD(qk_norm_rope), MX_METHOD(kv_write),
-                         MX_METHOD(qk_norm_rope_kv_write), MX_METHOD(kv_read), MX_METHOD(attention_kv), {nullptr, nullptr, 0, nullptr}};
+                         MX_METHOD(qk_norm_rope_kv_write), MX_METHOD(kv_read), MX_METHOD(attention_kv),
+                         MX_METHOD(quantize_block128), MX_METHOD(gemm_block128), MX_METHOD(gemm_block128_grouped), MX_METHOD(moe_plan), MX_METHOD(moe_combine), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
