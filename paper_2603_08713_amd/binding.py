@@ -122,6 +122,8 @@ def load_library() -> ctypes.CDLL:
     L.mx_gemm_block128.argtypes = [ci, vp, vp, ci, vp, vp, i64, i64, i64, ci, vp, i64, vp]
     L.mx_gemm_block128_grouped.restype = ci
     L.mx_gemm_block128_grouped.argtypes = [ci, vp, vp, i64, vp, ci, vp, vp, i32, vp, i64, i64, i64, ci, vp, i64, vp]
+    L.mx_internal_gemm_block128.restype = ci
+    L.mx_internal_gemm_block128.argtypes = [ci, ci, vp, vp, i64, vp, ci, vp, vp, ci, i32, vp, i64, i64, i64, ci, vp, i64, vp]
     L.mx_moe_plan.restype = ci
     L.mx_moe_plan.argtypes = [ci, vp, i64, i64, vp, i64, i64, ci, vp, ci, f, vp, vp, vp, vp, vp, vp, i64, vp]
     L.mx_moe_plan_workspace.restype = i64
@@ -152,8 +154,9 @@ def forced(**choices):
     """quantize_hw / quantize_elem_hw = 0 or 1 (rounding implementation), gemm_shape = a kernel form and
     tile shape code of mx_gemm.hip, gemm_elem = which kernel takes an 8-/6-bit GEMM (1 = the main kernel's general
     form, 2 = the main kernel in the form the problem allows, 3 = the few-row kernel, 16 / 17 / 18 = the main kernel on 256 x 128 /
-    128 x 128 / 64 x 128 tiles, the last two for K >= 512), attention = 1 or 2 (the kernel for few or for many rows)."""
-    allowed = {"quantize_hw", "quantize_elem_hw", "gemm_shape", "gemm_elem", "attention"}
+    128 x 128 / 64 x 128 tiles, the last two for K >= 512), attention = 1 or 2 (the kernel for few or for many rows),
+    block128 = 1 / 2 / 3 (the few-row kernel with 16 / 32 / 64 rows a tile) or 4 / 5 / 6 (64 x 128, 128 x 128, 256 x 256 tiles)."""
+    allowed = {"quantize_hw", "quantize_elem_hw", "gemm_shape", "gemm_elem", "attention", "block128"}
     if set(choices) - allowed:
         raise TypeError("unknown choice: %s" % sorted(set(choices) - allowed))
     old = getattr(_dev, "choices", {})
@@ -930,7 +933,7 @@ def mx_quantize_block128(x, elem="e4m3", block_rows=1, num_groups=1, codes=None,
 
 def mx_gemm_block128(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, out_dtype="f32", out=None):
     """C = A B^T: A [M, K] with scales for 1 x 128, B [N, K] with scales for 128 x 128, both as mx_quantize_block128 gives them."""
-    if _native is not None and out is not None and _done(
+    if _native is not None and out is not None and not getattr(_dev, "choices", None) and _done(
             _native.gemm_block128(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, out_dtype, out), "mx_gemm_block128"):
         return out
     torch = _torch_module or _torch()
@@ -941,15 +944,16 @@ def mx_gemm_block128(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, out_d
     _flat(b_scales, torch.float32, (_blocks(N), _blocks(K)), "b scales")
     code, out, ldc = _c_tensor(M, N, out_dtype, out, a_codes.device)
     _here(out, out.dtype, "out")
-    _check((_lib or load_library()).mx_gemm_block128(_elem(a_elem), _ptr(a_codes), _ptr(a_scales), _elem(b_elem), _ptr(b_codes), _ptr(b_scales), M, N, K,
-                                                     code, _ptr(out), ldc, _stream()), "mx_gemm_block128")
+    _check((_lib or load_library()).mx_internal_gemm_block128(_forced("block128") or 0, _elem(a_elem), _ptr(a_codes), _ptr(a_scales), M, None, _elem(b_elem),
+                                                              _ptr(b_codes), _ptr(b_scales), 0, 0, None, M, N, K, code, _ptr(out), ldc, _stream()),
+           "mx_gemm_block128")
     return out
 
 
 def mx_gemm_block128_grouped(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, row_offsets, N, out_dtype="f32", a_rows=None, out=None):
     """Grouped form of mx_gemm_block128: rows row_offsets[e]..row_offsets[e+1]-1 of C are rows of A times B_e^T, B stacked [G*N, K] (scales
     [G*ceil(N/128), ceil(K/128)]).  a_rows (int32, a row of A for each row of C: the tokens of mx_moe_plan): A's rows are taken where they lie."""
-    if _native is not None and out is not None and _done(
+    if _native is not None and out is not None and not getattr(_dev, "choices", None) and _done(
             _native.gemm_block128_grouped(a_elem, a_codes, a_scales, b_elem, b_codes, b_scales, row_offsets, N, out_dtype, a_rows, out), "mx_gemm_block128_grouped"):
         return out
     torch = _torch_module or _torch()
@@ -967,8 +971,8 @@ def mx_gemm_block128_grouped(a_elem, a_codes, a_scales, b_elem, b_codes, b_scale
         _flat(a_rows, torch.int32, (M,), "a_rows")
     code, out, ldc = _c_tensor(M, N, out_dtype, out, a_codes.device)
     _here(out, out.dtype, "out")
-    _check((_lib or load_library()).mx_gemm_block128_grouped(_elem(a_elem), _ptr(a_codes), _ptr(a_scales), A, _ptr(a_rows), _elem(b_elem), _ptr(b_codes),
-                                                             _ptr(b_scales), G, _ptr(row_offsets), M, N, K, code, _ptr(out), ldc, _stream()),
+    _check((_lib or load_library()).mx_internal_gemm_block128(_forced("block128") or 0, _elem(a_elem), _ptr(a_codes), _ptr(a_scales), A, _ptr(a_rows), _elem(b_elem),
+                                                              _ptr(b_codes), _ptr(b_scales), 1, G, _ptr(row_offsets), M, N, K, code, _ptr(out), ldc, _stream()),
            "mx_gemm_block128_grouped")
     return out
 

@@ -1,5 +1,6 @@
 // Entry points of the block-scaled FP8 GEMM: argument checks and the choice of the kernel.
 #include "mx_block128.h"
+#include "mx_internal.h"
 
 namespace mx {
 namespace {
@@ -19,45 +20,62 @@ int check_gemm(mx_elem_t a_elem, mx_elem_t b_elem, const Block128Args& g, mx_dty
     return MX_OK;
 }
 
-int run(mx_elem_t a_elem, mx_elem_t b_elem, Block128Args& g, mx_dtype_t c_dtype, void* stream) {
+int kernel_for(const Block128Args& g) {
+    const int64_t mean = g.num_groups ? (g.M + g.num_groups - 1) / g.num_groups : g.M;
+    return mean <= 16 ? 1 : mean <= 32 ? 2 : mean <= 64 ? 3 : mean <= 512 ? 5 : 6;
+}
+
+// force: 0 = by the rule, 1 to 3 = the few-row kernel with 16, 32, 64 rows a tile, 4 to 6 = tiles of 64 x 128, 128 x 128, 256 x 256.
+int run(mx_elem_t a_elem, mx_elem_t b_elem, Block128Args& g, mx_dtype_t c_dtype, int force, void* stream) {
+    if (force < 0 || force > 6) return MX_EINVAL;
     if (int st = check_device()) return st;
     g.c_bf16 = c_dtype == MX_OUT_BF16;
     g.vec_store = aligned(g.C, 16) && g.ldc * (g.c_bf16 ? 2 : 4) % 16 == 0;
-    const int64_t mean = g.num_groups ? (g.M + g.num_groups - 1) / g.num_groups : g.M;
-    return launch_block128_few(g, a_elem == MX_ELEM_E5M2, b_elem == MX_ELEM_E5M2, mean <= 16 ? 1 : mean <= 32 ? 2 : 4, static_cast<hipStream_t>(stream));
+    const bool a5 = a_elem == MX_ELEM_E5M2, b5 = b_elem == MX_ELEM_E5M2;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    switch (force ? force : kernel_for(g)) {
+        case 1: return launch_block128_few(g, a5, b5, 1, s);
+        case 2: return launch_block128_few(g, a5, b5, 2, s);
+        case 3: return launch_block128_few(g, a5, b5, 4, s);
+        case 4: return launch_block128_small(g, a5, b5, s);
+        case 5: return launch_block128_mid(g, a5, b5, s);
+        default: return launch_block128_large(g, a5, b5, s);
+    }
 }
 
 }  // namespace
 }  // namespace mx
 
-extern "C" int mx_gemm_block128(mx_elem_t a_elem, const uint8_t* a_codes, const float* a_scales, mx_elem_t b_elem, const uint8_t* b_codes,
-                                const float* b_scales, int64_t M, int64_t N, int64_t K, mx_dtype_t c_dtype, void* C, int64_t ldc, void* stream) {
+extern "C" int mx_internal_gemm_block128(int force, mx_elem_t a_elem, const uint8_t* a_codes, const float* a_scales, int64_t a_num_rows,
+                                         const int32_t* a_rows_or_null, mx_elem_t b_elem, const uint8_t* b_codes, const float* b_scales, int grouped, int32_t num_groups,
+                                         const int64_t* row_offsets, int64_t M, int64_t N, int64_t K, mx_dtype_t c_dtype, void* C, int64_t ldc, void* stream) {
     using namespace mx;
     Block128Args g = {};
     g.a_codes = a_codes; g.a_scales = a_scales; g.b_codes = b_codes; g.b_scales = b_scales;
     g.C = C;
-    g.a_num_rows = M; g.M = M; g.N = N; g.K = K; g.ldc = ldc;
+    g.a_num_rows = a_num_rows; g.M = M; g.N = N; g.K = K; g.ldc = ldc;
+    if (grouped) {
+        g.a_rows = a_rows_or_null; g.row_offsets = row_offsets;
+        g.num_groups = num_groups;
+        if (num_groups < 0 || M < 0 || a_num_rows < 0 || a_num_rows > (int64_t)1 << 30 || (!a_rows_or_null && a_num_rows < M)) return MX_EINVAL;
+        if (num_groups == 0) g.M = 0;  // (no group has rows)
+    }
     if (int st = check_gemm(a_elem, b_elem, g, c_dtype)) return st;
-    if (M == 0 || N == 0) return MX_OK;
-    return run(a_elem, b_elem, g, c_dtype, stream);
+    if (g.M == 0 || N == 0) return MX_OK;
+    if (grouped && !row_offsets) return MX_ENULL;
+    // rows taken through an index are addressed by 32 bits from the first one
+    if (g.a_rows && a_num_rows * K > ((int64_t)1 << 32) - 256) return MX_EUNSUPPORTED;
+    return run(a_elem, b_elem, g, c_dtype, force, stream);
+}
+
+extern "C" int mx_gemm_block128(mx_elem_t a_elem, const uint8_t* a_codes, const float* a_scales, mx_elem_t b_elem, const uint8_t* b_codes,
+                                const float* b_scales, int64_t M, int64_t N, int64_t K, mx_dtype_t c_dtype, void* C, int64_t ldc, void* stream) {
+    return mx_internal_gemm_block128(0, a_elem, a_codes, a_scales, M, nullptr, b_elem, b_codes, b_scales, 0, 0, nullptr, M, N, K, c_dtype, C, ldc, stream);
 }
 
 extern "C" int mx_gemm_block128_grouped(mx_elem_t a_elem, const uint8_t* a_codes, const float* a_scales, int64_t a_num_rows, const int32_t* a_rows_or_null,
                                         mx_elem_t b_elem, const uint8_t* b_codes, const float* b_scales, int32_t num_groups, const int64_t* row_offsets,
                                         int64_t M_total, int64_t N, int64_t K, mx_dtype_t c_dtype, void* C, int64_t ldc, void* stream) {
-    using namespace mx;
-    Block128Args g = {};
-    g.a_codes = a_codes; g.a_scales = a_scales; g.b_codes = b_codes; g.b_scales = b_scales;
-    g.a_rows = a_rows_or_null; g.row_offsets = row_offsets;
-    g.C = C;
-    g.a_num_rows = a_num_rows; g.M = M_total; g.N = N; g.K = K; g.ldc = ldc;
-    g.num_groups = num_groups;
-    if (num_groups < 0 || M_total < 0 || a_num_rows < 0 || a_num_rows > (int64_t)1 << 30 || (!a_rows_or_null && a_num_rows < M_total)) return MX_EINVAL;
-    if (num_groups == 0) g.M = 0;  // (no group has rows)
-    if (int st = check_gemm(a_elem, b_elem, g, c_dtype)) return st;
-    if (g.M == 0 || N == 0) return MX_OK;
-    if (!row_offsets) return MX_ENULL;
-    // rows taken through an index are addressed by 32 bits from the first one
-    if (a_rows_or_null && a_num_rows * K > ((int64_t)1 << 32) - 256) return MX_EUNSUPPORTED;
-    return run(a_elem, b_elem, g, c_dtype, stream);
+    return mx_internal_gemm_block128(0, a_elem, a_codes, a_scales, a_num_rows, a_rows_or_null, b_elem, b_codes, b_scales, 1, num_groups, row_offsets, M_total, N, K,
+                                     c_dtype, C, ldc, stream);
 }

@@ -229,3 +229,53 @@ def test_empty_products(mx):
     out = torch.full((4, 5), 7.0, device="cuda")
     mx.mx_gemm_block128_grouped("e4m3", z(4, 128), s(4, 1), "e4m3", z(0, 128), s(0, 1), torch.zeros(1, dtype=torch.int64, device="cuda"), 5, "f32", out=out)
     assert bool((out == 7.0).all())
+
+
+# ---- every kernel on problems that the rule gives to others ---------------------------------------------------------------------
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("M, N, K", [(1, 5, 16), (70, 300, 128), (129, 131, 2896), (300, 515, 144), (513, 257, 640), (257, 1100, 384)])
+def test_every_kernel_is_exact_on_small_numbers(mx, kernel, M, N, K):
+    g = generator(M + N + K)
+    ac, as_ = small_operand(g, M, K, M, "e5m2")
+    bc, bs = small_operand(g, N, K, ref.blocks(N), "e4m3")
+    want, _ = ref.product(ref.values(ac, as_, 1, "e5m2"), ref.values(bc, bs, 128, "e4m3"))
+    for dtype, name in ((torch.float32, "f32"), (torch.bfloat16, "bf16")):
+        wide = torch.full((M + 2, N + 3), 777.0, dtype=dtype, device="cuda")
+        with mx.forced(block128=kernel):
+            mx.mx_gemm_block128("e5m2", ac, as_, "e4m3", bc, bs, name, out=wide[1:-1, 1:N + 1])
+        assert torch.equal(wide[1:-1, 1:N + 1].double(), want.to(dtype).double())
+        wide[1:-1, 1:N + 1] = 777.0
+        assert bool((wide == 777.0).all())
+
+
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("index", [False, True])
+def test_every_kernel_by_groups(mx, kernel, index):
+    counts, N, K = [130, 0, 64, 1, 300, 0, 31] + [3] * 66, 257, 400
+    g = generator(kernel)
+    G, rows = len(counts), sum(counts)
+    A = 90 if index else rows
+    ac, as_ = small_operand(g, A, K, A, "e4m3")
+    bc, bs = small_operand(g, G * N, K, G * ref.blocks(N), "e4m3")
+    a_rows = torch.randint(0, A, (rows,), generator=g, device="cuda").int() if index else None
+    out = torch.full((rows, N), 777.0, device="cuda")
+    with mx.forced(block128=kernel):
+        mx.mx_gemm_block128_grouped("e4m3", ac, as_, "e4m3", bc, bs, offsets_of(counts), N, "f32", a_rows=a_rows, out=out)
+    a = ref.values(ac, as_, 1, "e4m3")
+    a = a if a_rows is None else a[a_rows.long()]
+    at = 0
+    for e, n in enumerate(counts):
+        b = ref.values(bc[e * N:(e + 1) * N], bs[e * ref.blocks(N):(e + 1) * ref.blocks(N)], 128, "e4m3")
+        assert torch.equal(out[at:at + n].double(), ref.product(a[at:at + n], b)[0]), e
+        at += n
+
+
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6])
+def test_every_kernel_on_quantized_tensors(mx, kernel):
+    M, N, K = 300, 400, 2896
+    g = generator(3)
+    a, b = real_operand(g, mx, M, K, 1, "e4m3"), real_operand(g, mx, N, K, 128, "e4m3")
+    want, size = ref.product(ref.values(*a, 1, "e4m3"), ref.values(*b, 128, "e4m3"))
+    with mx.forced(block128=kernel):
+        got = mx.mx_gemm_block128("e4m3", *a, "e4m3", *b, "f32").double()
+    assert bool(((got - want).abs() <= ref.product_bound(want, size, K, False)).all())
