@@ -22,6 +22,7 @@ struct Block128Args {
 
 // a_e5m2, b_e5m2: the operand's codes are E5M2 and not E4M3.
 int launch_block128_large(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);  // tiles of 256 x 256
+int launch_block128_stream(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);  // the same, a workgroup taking tile after tile: vec_store, K > 128
 int launch_block128_mid(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);    // 128 x 128
 int launch_block128_small(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);  // 64 x 128
 // Tiles of 16 row_frags x 16, K among the wavefronts (mx_gemm_block128_few.hip).
@@ -78,6 +79,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t b128_buffer(const void* p, int
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)bytes, kRawBuffer);
 }
 typedef __attribute__((address_space(4))) const float* const_f32_ptr_t;  // (scalar loads)
+// What is the same for the whole wavefront, said so: a buffer that the compiler takes for one a lane makes a loop of every load.
+__device__ __forceinline__ int64_t uniform(int64_t x) { return readlane64(x, 0); }
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t b128_uniform_buffer(const void* p, int64_t bytes) {
+    return b128_buffer(reinterpret_cast<const void*>(uniform((int64_t)reinterpret_cast<uintptr_t>(p))), uniform(bytes));
+}
 
 }  // namespace
 }  // namespace mx

@@ -22,12 +22,13 @@ int check_gemm(mx_elem_t a_elem, mx_elem_t b_elem, const Block128Args& g, mx_dty
 
 int kernel_for(const Block128Args& g) {
     const int64_t mean = g.num_groups ? (g.M + g.num_groups - 1) / g.num_groups : g.M;
-    return mean <= 16 ? 1 : mean <= 32 ? 2 : mean <= 64 ? 3 : mean <= 512 ? 5 : 6;
+    return mean <= 16 ? 1 : mean <= 32 ? 2 : mean <= 64 ? 3 : mean <= 512 ? 5 : 7;
 }
 
-// force: 0 = by the rule, 1 to 3 = the few-row kernel with 16, 32, 64 rows a tile, 4 to 6 = tiles of 64 x 128, 128 x 128, 256 x 256.
+// force: 0 = by the rule, 1 to 3 = the few-row kernel with 16, 32, 64 rows a tile, 4 to 6 = tiles of 64 x 128, 128 x 128,
+// 256 x 256, 7 = those in a stream (as 6 where they cannot).
 int run(mx_elem_t a_elem, mx_elem_t b_elem, Block128Args& g, mx_dtype_t c_dtype, int force, void* stream) {
-    if (force < 0 || force > 6) return MX_EINVAL;
+    if (force < 0 || force > 7) return MX_EINVAL;
     if (int st = check_device()) return st;
     g.c_bf16 = c_dtype == MX_OUT_BF16;
     g.vec_store = aligned(g.C, 16) && g.ldc * (g.c_bf16 ? 2 : 4) % 16 == 0;
@@ -39,7 +40,8 @@ int run(mx_elem_t a_elem, mx_elem_t b_elem, Block128Args& g, mx_dtype_t c_dtype,
         case 3: return launch_block128_few(g, a5, b5, 4, s);
         case 4: return launch_block128_small(g, a5, b5, s);
         case 5: return launch_block128_mid(g, a5, b5, s);
-        default: return launch_block128_large(g, a5, b5, s);
+        case 6: return launch_block128_large(g, a5, b5, s);
+        default: return g.vec_store && g.K > kScaled ? launch_block128_stream(g, a5, b5, s) : launch_block128_large(g, a5, b5, s);
     }
 }
 

@@ -232,7 +232,7 @@ def test_empty_products(mx):
 
 
 # ---- every kernel on problems that the rule gives to others ---------------------------------------------------------------------
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7])
 @pytest.mark.parametrize("M, N, K", [(1, 5, 16), (70, 300, 128), (129, 131, 2896), (300, 515, 144), (513, 257, 640), (257, 1100, 384)])
 def test_every_kernel_is_exact_on_small_numbers(mx, kernel, M, N, K):
     g = generator(M + N + K)
@@ -248,7 +248,7 @@ def test_every_kernel_is_exact_on_small_numbers(mx, kernel, M, N, K):
         assert bool((wide == 777.0).all())
 
 
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7])
 @pytest.mark.parametrize("index", [False, True])
 def test_every_kernel_by_groups(mx, kernel, index):
     counts, N, K = [130, 0, 64, 1, 300, 0, 31] + [3] * 66, 257, 400
@@ -270,7 +270,7 @@ def test_every_kernel_by_groups(mx, kernel, index):
         at += n
 
 
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7])
 def test_every_kernel_on_quantized_tensors(mx, kernel):
     M, N, K = 300, 400, 2896
     g = generator(3)
@@ -279,3 +279,45 @@ def test_every_kernel_on_quantized_tensors(mx, kernel):
     with mx.forced(block128=kernel):
         got = mx.mx_gemm_block128("e4m3", *a, "e4m3", *b, "f32").double()
     assert bool(((got - want).abs() <= ref.product_bound(want, size, K, False)).all())
+
+
+@pytest.mark.parametrize("M, N, K", [(4353, 4232, 144), (4353, 4232, 400), (2049, 8712, 272), (300, 520, 1040), (4353, 4232, 128)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_a_workgroup_takes_tile_after_tile(mx, M, N, K, out):
+    """More than 256 tiles of 256 x 256, the last of a row and of a column cut off, K of two blocks and more (and of one)."""
+    g = generator(M + K)
+    ac, as_ = small_operand(g, M, K, M, "e4m3")
+    bc, bs = small_operand(g, N, K, ref.blocks(N), "e4m3")
+    want, _ = ref.product(ref.values(ac, as_, 1, "e4m3"), ref.values(bc, bs, 128, "e4m3"))
+    dtype = torch.bfloat16 if out == "bf16" else torch.float32
+    wide = torch.full((M + 2, N + 16), 777.0, dtype=dtype, device="cuda")
+    with mx.forced(block128=7):
+        mx.mx_gemm_block128("e4m3", ac, as_, "e4m3", bc, bs, out, out=wide[1:-1, 8:N + 8])
+    assert torch.equal(wide[1:-1, 8:N + 8].double(), want.to(dtype).double())
+    wide[1:-1, 8:N + 8] = 777.0
+    assert bool((wide == 777.0).all())
+
+
+@pytest.mark.parametrize("index", [False, True])
+@pytest.mark.parametrize("K", [272, 528])
+def test_tile_after_tile_by_groups(mx, index, K):
+    counts, N = [3000, 0, 17, 700, 256, 0, 1] + [40] * 70 + [2100], 1096
+    g = generator(K)
+    G, rows = len(counts), sum(counts)
+    A = 900 if index else rows
+    ac, as_ = small_operand(g, A, K, A, "e4m3")
+    bc, bs = small_operand(g, G * N, K, G * ref.blocks(N), "e4m3")
+    a_rows = torch.randint(0, A, (rows,), generator=g, device="cuda").int() if index else None
+    if index:
+        a_rows[5], a_rows[3500] = -1, A
+    out = torch.full((rows + 1, N), 777.0, device="cuda")
+    with mx.forced(block128=7):
+        mx.mx_gemm_block128_grouped("e4m3", ac, as_, "e4m3", bc, bs, offsets_of(counts), N, "f32", a_rows=a_rows, out=out[:-1])
+    a = torch.cat((ref.values(ac, as_, 1, "e4m3"), torch.zeros((1, K), dtype=torch.float64, device="cuda")))
+    a = a[:-1] if a_rows is None else a[torch.where((a_rows >= 0) & (a_rows < A), a_rows, A).long()]
+    at = 0
+    for e, n in enumerate(counts):
+        b = ref.values(bc[e * N:(e + 1) * N], bs[e * ref.blocks(N):(e + 1) * ref.blocks(N)], 128, "e4m3")
+        assert torch.equal(out[at:at + n].double(), ref.product(a[at:at + n], b)[0]), e
+        at += n
+    assert bool((out[-1] == 777.0).all())
