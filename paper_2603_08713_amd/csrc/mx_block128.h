@@ -21,12 +21,13 @@ struct Block128Args {
 };
 
 // a_e5m2, b_e5m2: the operand's codes are E5M2 and not E4M3.
-int launch_block128_large(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);  // tiles of 256 x 256
+int launch_block128_large(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);   // tiles of 256 x 256
 int launch_block128_stream(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);  // the same, a workgroup taking tile after tile: vec_store, K > 128
-int launch_block128_mid(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);    // 128 x 128
-int launch_block128_small(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);  // 64 x 128
-// Tiles of 16 row_frags x 16, K among the wavefronts (mx_gemm_block128_few.hip).
-int launch_block128_few(const Block128Args& g, bool a_e5m2, bool b_e5m2, int row_frags, hipStream_t s);
+int launch_block128_mid(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);     // 128 x 128
+int launch_block128_small(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);   // 64 x 128
+int launch_block128_deep(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);    // the same with loads further ahead, for problems of few tiles
+// K among the wavefronts, tiles of 16 x 16 (shape 1), 16 x 32 (2), 32 x 32 (3) (mx_gemm_block128_few.hip).
+int launch_block128_few(const Block128Args& g, bool a_e5m2, bool b_e5m2, int shape, hipStream_t s);
 
 namespace {
 

@@ -7,9 +7,9 @@
 // rows; a wavefront's columns lie inside one block of 128, so sB is a scalar.  (With rows along the registers every result would want a factor of its own.)
 //
 // A wavefront keeps FA x FB fragments of results, the FA fragments of its rows for the whole stage and one fragment of columns at a time, each refilled
-// in place right behind the last instruction that reads it.  A stage is one block of k; codes go from memory into one of two LDS slots.  The one barrier of a stage
+// in place right behind the last instruction that reads it.  A stage is one block of k; codes go from memory into one of a few LDS slots.  The one barrier of a stage
 // stands in front of its last fragment of columns, when the stage's codes are all in registers: it publishes the next stage, whose fragments are then read
-// behind the last instructions of this one, and frees this stage's slot for the loads of the stage after the next.
+// behind the last instructions of this one, and frees this stage's slot for later loads.
 // The folding of a result stands behind both instructions of the next one: by then its matrix instruction is through, and the second wavefront of the
 // SIMD multiplies while this one folds.  The empty asm statements keep that order.
 //
@@ -25,15 +25,18 @@ namespace {
 
 constexpr int kB128TableGroups = 1024;  // groups whose rows a stream keeps in LDS
 
-// kStream: a workgroup takes tile after tile (rows of C on 16-byte boundaries, K beyond one block); else one.
-template <int FA_, int FB_, int WM_, int WN_, bool kStream_ = false>
+// kStream: a workgroup takes tile after tile (rows of C on 16-byte boundaries, K beyond one block); else one.  kSlots: LDS slots of a stage each; loads run
+// kSlots - 1 stages ahead.
+template <int FA_, int FB_, int WM_, int WN_, int kSlots_, bool kStream_ = false>
 struct B128Shape {
     static constexpr bool kStream = kStream_;
+    static constexpr int kSlots = kSlots_;
+    static_assert(kSlots == 2 || !kStream, "a tile loads the next one's first stage, not its second");
     static constexpr int FA = FA_, FB = FB_, WM = WM_, WN = WN_, NW = WM * WN, TM = WM * FA * 32, TN = WN * FB * 32;
     // a slot: A's codes, B's codes, the scales of A's rows
     static constexpr int kInB = TM * kScaled, kInS = kInB + TN * kScaled, kSlot = kInS + TM * 4;
     static constexpr int kLoadsA = TM / 8 / NW, kLoadsB = TN / 8 / NW;
-    static constexpr int kSpare = 2 * kSlot;  // (a piece for loads whose bytes nobody wants)
+    static constexpr int kSpare = kSlots * kSlot;  // (a piece for loads whose bytes nobody wants)
     static constexpr int kTable = kSpare + 256, kBytes = kTable + (kStream ? kB128TableGroups * 12 + 16 : 0);
     static_assert(kScaled % (FB * 32) == 0, "a wavefront's columns lie inside one block");
     static_assert(kLoadsA >= 1 && kLoadsA <= 4 && kLoadsB >= 1 && NW % 2 == 0 && TM / 64 <= NW, "every wavefront loads whole pieces");
@@ -140,6 +143,7 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
         return x;
     };
     const int off_row = load_row * K + piece * 16;
+    const bool owns = w < TM / 64;  // 64 rows, whose scales it loads
 
     // What is loaded next: stage ld_stage of the tile whose buffers are in ld (the one multiplied, then the one after it)
     B128Tile cur = make(first), nxt = make(first + step), ld = cur;
@@ -163,19 +167,19 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
             if constexpr (i < kLoadsA && kMode == kB128Indexed) off = past ? kOutside : at_ld.a[i];
             __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kLoadsA ? ld.a : ld.b, (lds_ptr_t)(slot + (i < kLoadsA ? 0 : S::kInB) + row0 * kScaled + w * 1024), 16, off, at, 0, 0);
         } else {
-            // (wavefronts that own no rows fetch nothing into the spare piece: the loop is free of branches)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ld.s, (lds_ptr_t)(w < TM / 64 ? slot + S::kInS + w * 256 : smem + S::kSpare), 4, at_ld.s, ld_stage * 4, 0, 0);
+            // (a load of 4 bytes a lane from as many rows costs the texture-address unit as much as four of 16: not by wavefronts that own no rows)
+            if (owns) __builtin_amdgcn_raw_ptr_buffer_load_lds(ld.s, (lds_ptr_t)(slot + S::kInS + w * 256), 4, at_ld.s, ld_stage * 4, 0, 0);
         }
     };
     auto load_next = [&]() __attribute__((always_inline)) {  // (behind the barrier that frees the slot)
         const bool wrap = ++ld_stage == nblk;
-        ld_slot = S::kSlot - ld_slot;
+        ld_slot = (ld_slot + S::kSlot) & -(int)(ld_slot != (S::kSlots - 1) * S::kSlot);  // (by bits: a choice would become a branch)
         ld_stage = wrap ? 0 : ld_stage;
         ld.a = wrap ? nxt.a : ld.a;
         ld.s = wrap ? nxt.s : ld.s;
         ld.b = wrap ? nxt.b : ld.b;
         if constexpr (kMode == kB128Indexed) {
-            const int other = -(int)wrap;  // (by bits: a choice would become a branch)
+            const int other = -(int)wrap;
 #pragma unroll
             for (int i = 0; i < kLoadsA; ++i) at_ld.a[i] = (at_ld.a[i] & ~other) | (at_nxt.a[i] & other);
             at_ld.s = (at_ld.s & ~other) | (at_nxt.s & other);
@@ -218,25 +222,30 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
     auto row_scale = [&](int m) __attribute__((always_inline)) { return *(lds_f32_ptr_t)(uintptr_t)(uint32_t)(at_s + m * 128); };
     constexpr std::integral_constant<int, 0> k0{};
     constexpr std::integral_constant<int, 1> k1{};
-    int slot_step = S::kSlot;
+    int slot_of = 0;  // the slot that at_a, at_b and at_s lie in
     auto next_slot = [&]() __attribute__((always_inline)) {
-        at_a += slot_step;
-        at_b += slot_step;
-        at_s += slot_step;
-        slot_step = -slot_step;
+        const int other = -(int)(slot_of == S::kSlots - 1), by = S::kSlot - (other & (S::kSlots * S::kSlot));
+        slot_of = (slot_of + 1) & ~other;
+        at_a += by;
+        at_b += by;
+        at_s += by;
     };
 
     v16f acc[FA][FB], P[2];
     v8i a[FA][2], b[2];
     float s[FA], s_last, sa[FA];
 
-    static_for<kLoads>([&](auto i_) { issue(i_); });
-    load_next();
+    static_for<S::kSlots - 1>([&](auto) {
+        static_for<kLoads>([&](auto i_) { issue(i_); });
+        load_next();
+    });
     static_for<FA>([&](auto r_) {
         issue_some(r_, std::integral_constant<int, 0>{});
         issue_some(r_, std::integral_constant<int, 1>{});
     });
-    __builtin_amdgcn_s_waitcnt(wait_imm(FA * kEach < kLoads ? FA * kEach : kLoads));
+    constexpr int kFirst = FA * kEach < kLoads ? FA * kEach : kLoads;  // loads of the last of those stages
+    if (owns) __builtin_amdgcn_s_waitcnt(wait_imm((S::kSlots - 2) * kLoads + kFirst));
+    else __builtin_amdgcn_s_waitcnt(wait_imm((S::kSlots - 2) * (kLoads - 1) + kFirst - (kFirst == kLoads)));
     bare_barrier();
     b[0] = frag(at_b, 0, k0);
     b[1] = frag(at_b, 0, k1);
@@ -270,7 +279,9 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
                 };
                 if constexpr (n == FB - 1) {
                     if constexpr (FB == 1) factors();  // (before the next stage's are read)
-                    __builtin_amdgcn_s_waitcnt(wait_imm(kAhead ? 1 : 0));  // (the lines asked for ahead may still be under way)
+                    // (later stages may still be under way, and the lines asked for ahead)
+                    if (S::kSlots == 2 || owns) __builtin_amdgcn_s_waitcnt(wait_imm((S::kSlots - 2) * kLoads + (kAhead ? 1 : 0)));
+                    else __builtin_amdgcn_s_waitcnt(wait_imm((S::kSlots - 2) * (kLoads - 1)));
                     bare_barrier();
                     next_slot();
                     load_next();

@@ -13,12 +13,15 @@
 namespace mx {
 namespace {
 
-constexpr int kFewWaves = 8;
+// FM, FN: fragments of 16 rows of A and of 16 columns.  kWaves: wavefronts of a workgroup.  kAhead: blocks whose loads a wavefront has in flight together.
+template <int FM_, int FN_, int kWaves_, int kAhead_>
+struct FewShape {
+    static constexpr int FM = FM_, FN = FN_, kWaves = kWaves_, kAhead = kAhead_;
+};
 
-template <int kFmtA, int kFmtB, int FM, bool kGrouped>
-__global__ __launch_bounds__(kFewWaves* kWave) void block128_few_kernel(Block128Args g) {
-    constexpr int TM = 16 * FM, TN = 16;
-    constexpr int kAhead = FM <= 2 ? 4 : 2;  // blocks whose loads are in flight together
+template <int kFmtA, int kFmtB, typename S, bool kGrouped>
+__global__ __launch_bounds__(S::kWaves* kWave) void block128_few_kernel(Block128Args g) {
+    constexpr int FM = S::FM, FN = S::FN, kFewWaves = S::kWaves, kAhead = S::kAhead, TM = 16 * FM, TN = 16 * FN;
     const int tid = threadIdx.x, l = tid & 63, r = l & 15, q = l >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -58,12 +61,14 @@ __global__ __launch_bounds__(kFewWaves* kWave) void block128_few_kernel(Block128
     }
     const int b_off = r * K + q * 32;
 
-    v4f acc[FM];
+    v4f acc[FM][FN];
 #pragma unroll
-    for (int f = 0; f < FM; ++f) acc[f] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int n = 0; n < FN; ++n) acc[f][n] = v4f{0.f, 0.f, 0.f, 0.f};
 
     struct Loads {
-        v4i b[2], a[FM][2];
+        v4i b[FN][2], a[FM][2];
         float sa[FM], sb;
     };
     auto load = [&](int g_, Loads& x) __attribute__((always_inline)) {
@@ -73,7 +78,8 @@ __global__ __launch_bounds__(kFewWaves* kWave) void block128_few_kernel(Block128
         for (int p = 0; p < 2; ++p) {
             // (K ends inside a block: pieces past it are zeros, not the next row's codes)
             const bool past = beyond || at + q * 32 + p * 16 >= K;
-            x.b[p] = __builtin_amdgcn_raw_buffer_load_b128(b_codes, past ? kOutside : b_off + p * 16, at, 0);
+#pragma unroll
+            for (int n = 0; n < FN; ++n) x.b[n][p] = __builtin_amdgcn_raw_buffer_load_b128(b_codes, past ? kOutside : b_off + n * 16 * K + p * 16, at, 0);
 #pragma unroll
             for (int f = 0; f < FM; ++f) x.a[f][p] = __builtin_amdgcn_raw_buffer_load_b128(a_codes, past || a_off[f] == kOutside ? kOutside : a_off[f] + p * 16, at, 0);
         }
@@ -82,14 +88,17 @@ __global__ __launch_bounds__(kFewWaves* kWave) void block128_few_kernel(Block128
         x.sb = sb[blk];
     };
     auto fold = [&](const Loads& x) __attribute__((always_inline)) {
-        const v8i b = __builtin_shufflevector(x.b[0], x.b[1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
         for (int f = 0; f < FM; ++f) {
             const v8i a = __builtin_shufflevector(x.a[f][0], x.a[f][1], 0, 1, 2, 3, 4, 5, 6, 7);
-            const v4f p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, v4f{0.f, 0.f, 0.f, 0.f}, kFmtB, kFmtA, 0, 0, 0, 0);
             const float s = x.sa[f] * x.sb;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[f][j] = __builtin_fmaf(p[j], s, acc[f][j]);
+            for (int n = 0; n < FN; ++n) {
+                const v8i b = __builtin_shufflevector(x.b[n][0], x.b[n][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                const v4f p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, v4f{0.f, 0.f, 0.f, 0.f}, kFmtB, kFmtA, 0, 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[f][n][j] = __builtin_fmaf(p[j], s, acc[f][n][j]);
+            }
         }
     };
     Loads x[kAhead];
@@ -103,16 +112,18 @@ __global__ __launch_bounds__(kFewWaves* kWave) void block128_few_kernel(Block128
         }
     }
 
-    __shared__ v4f part[kFewWaves][FM][kWave];
+    static_assert(FM * FN <= kFewWaves && 16 * FN <= kScaled, "a wavefront a fragment; one scale for the tile's columns");
+    __shared__ v4f part[kFewWaves][FM * FN][kWave];
 #pragma unroll
-    for (int f = 0; f < FM; ++f) part[w][f][l] = acc[f];
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int n = 0; n < FN; ++n) part[w][f * FN + n][l] = acc[f][n];
     __syncthreads();
-    if (w >= FM) return;
-    const int f = w;
-    v4f sum = part[0][f][l];
+    if (w >= FM * FN) return;
+    v4f sum = part[0][w][l];
 #pragma unroll
-    for (int i = 1; i < kFewWaves; ++i) sum += part[i][f][l];
-    const int64_t m = row0 + f * 16 + r, n = n0 + q * 4;
+    for (int i = 1; i < kFewWaves; ++i) sum += part[i][w][l];
+    const int64_t m = row0 + w / FN * 16 + r, n = n0 + w % FN * 16 + q * 4;
     if (m >= end || n >= g.N) return;
     if (g.c_bf16) {
         uint16_t* o = static_cast<uint16_t*>(g.C) + m * g.ldc + n;
@@ -136,32 +147,32 @@ __global__ __launch_bounds__(kFewWaves* kWave) void block128_few_kernel(Block128
     }
 }
 
-template <int kFmtA, int kFmtB, int FM>
+template <int kFmtA, int kFmtB, typename S>
 int launch(const Block128Args& g, hipStream_t s) {
     const int64_t blocks = ((int64_t)g.tiles_m * g.tiles_n + 7) / 8 * 8;
-    if (g.num_groups) hipLaunchKernelGGL((block128_few_kernel<kFmtA, kFmtB, FM, true>), dim3((unsigned)blocks), dim3(kFewWaves * kWave), 0, s, g);
-    else hipLaunchKernelGGL((block128_few_kernel<kFmtA, kFmtB, FM, false>), dim3((unsigned)blocks), dim3(kFewWaves * kWave), 0, s, g);
+    if (g.num_groups) hipLaunchKernelGGL((block128_few_kernel<kFmtA, kFmtB, S, true>), dim3((unsigned)blocks), dim3(S::kWaves * kWave), 0, s, g);
+    else hipLaunchKernelGGL((block128_few_kernel<kFmtA, kFmtB, S, false>), dim3((unsigned)blocks), dim3(S::kWaves * kWave), 0, s, g);
     return launch_status();
 }
-template <int FM>
-int launch_types(const Block128Args& g, bool a5, bool b5, hipStream_t s) {
-    if (a5) return b5 ? launch<1, 1, FM>(g, s) : launch<1, 0, FM>(g, s);
-    return b5 ? launch<0, 1, FM>(g, s) : launch<0, 0, FM>(g, s);
+template <typename S>
+int launch_types(const Block128Args& g0, bool a5, bool b5, hipStream_t s) {
+    Block128Args g = g0;
+    const int64_t tm = 16 * S::FM, busy = g.num_groups ? min((int64_t)g.num_groups, g.M) : 1;
+    const int64_t tiles_m = (g.M + busy * (tm - 1)) / tm, tiles_n = (g.N + 16 * S::FN - 1) / (16 * S::FN);
+    // (a launch has less than 2^32 work-items)
+    if (tiles_m * tiles_n > ((int64_t)1 << 32) / (S::kWaves * kWave) - 9) return MX_EINVAL;
+    g.tiles_m = (int)tiles_m;
+    g.tiles_n = (int)tiles_n;
+    if (a5) return b5 ? launch<1, 1, S>(g, s) : launch<1, 0, S>(g, s);
+    return b5 ? launch<0, 1, S>(g, s) : launch<0, 0, S>(g, s);
 }
 
 }  // namespace
 
-int launch_block128_few(const Block128Args& g0, bool a_e5m2, bool b_e5m2, int row_frags, hipStream_t s) {
-    Block128Args g = g0;
-    const int64_t tm = 16 * row_frags, busy = g.num_groups ? min((int64_t)g.num_groups, g.M) : 1;
-    const int64_t tiles_m = (g.M + busy * (tm - 1)) / tm, tiles_n = (g.N + 15) / 16;
-    // (a launch has less than 2^32 work-items)
-    if (tiles_m * tiles_n > ((int64_t)1 << 32) / (kFewWaves * kWave) - 9) return MX_EINVAL;
-    g.tiles_m = (int)tiles_m;
-    g.tiles_n = (int)tiles_n;
-    if (row_frags == 1) return launch_types<1>(g, a_e5m2, b_e5m2, s);
-    if (row_frags == 2) return launch_types<2>(g, a_e5m2, b_e5m2, s);
-    return launch_types<4>(g, a_e5m2, b_e5m2, s);
+int launch_block128_few(const Block128Args& g, bool a_e5m2, bool b_e5m2, int shape, hipStream_t s) {
+    if (shape == 1) return launch_types<FewShape<1, 1, 8, 2>>(g, a_e5m2, b_e5m2, s);
+    if (shape == 2) return launch_types<FewShape<1, 2, 4, 2>>(g, a_e5m2, b_e5m2, s);
+    return launch_types<FewShape<2, 2, 8, 2>>(g, a_e5m2, b_e5m2, s);
 }
 
 }  // namespace mx

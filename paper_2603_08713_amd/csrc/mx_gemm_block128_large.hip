@@ -3,6 +3,6 @@
 
 namespace mx {
 
-int launch_block128_large(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s) { return launch_b128_types<B128Shape<2, 4, 4, 2>>(g, a_e5m2, b_e5m2, s); }
+int launch_block128_large(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s) { return launch_b128_types<B128Shape<2, 4, 4, 2, 2>>(g, a_e5m2, b_e5m2, s); }
 
 }  // namespace mx

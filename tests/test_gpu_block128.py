@@ -232,7 +232,7 @@ def test_empty_products(mx):
 
 
 # ---- every kernel on problems that the rule gives to others ---------------------------------------------------------------------
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8])
 @pytest.mark.parametrize("M, N, K", [(1, 5, 16), (70, 300, 128), (129, 131, 2896), (300, 515, 144), (513, 257, 640), (257, 1100, 384)])
 def test_every_kernel_is_exact_on_small_numbers(mx, kernel, M, N, K):
     g = generator(M + N + K)
@@ -248,7 +248,7 @@ def test_every_kernel_is_exact_on_small_numbers(mx, kernel, M, N, K):
         assert bool((wide == 777.0).all())
 
 
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8])
 @pytest.mark.parametrize("index", [False, True])
 def test_every_kernel_by_groups(mx, kernel, index):
     counts, N, K = [130, 0, 64, 1, 300, 0, 31] + [3] * 66, 257, 400
@@ -270,7 +270,7 @@ def test_every_kernel_by_groups(mx, kernel, index):
         at += n
 
 
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8])
 def test_every_kernel_on_quantized_tensors(mx, kernel):
     M, N, K = 300, 400, 2896
     g = generator(3)
@@ -291,7 +291,7 @@ def test_a_workgroup_takes_tile_after_tile(mx, M, N, K, out):
     want, _ = ref.product(ref.values(ac, as_, 1, "e4m3"), ref.values(bc, bs, 128, "e4m3"))
     dtype = torch.bfloat16 if out == "bf16" else torch.float32
     wide = torch.full((M + 2, N + 16), 777.0, dtype=dtype, device="cuda")
-    with mx.forced(block128=7):
+    with mx.forced(block128=8):
         mx.mx_gemm_block128("e4m3", ac, as_, "e4m3", bc, bs, out, out=wide[1:-1, 8:N + 8])
     assert torch.equal(wide[1:-1, 8:N + 8].double(), want.to(dtype).double())
     wide[1:-1, 8:N + 8] = 777.0
@@ -311,7 +311,7 @@ def test_tile_after_tile_by_groups(mx, index, K):
     if index:
         a_rows[5], a_rows[3500] = -1, A
     out = torch.full((rows + 1, N), 777.0, device="cuda")
-    with mx.forced(block128=7):
+    with mx.forced(block128=8):
         mx.mx_gemm_block128_grouped("e4m3", ac, as_, "e4m3", bc, bs, offsets_of(counts), N, "f32", a_rows=a_rows, out=out[:-1])
     a = torch.cat((ref.values(ac, as_, 1, "e4m3"), torch.zeros((1, K), dtype=torch.float64, device="cuda")))
     a = a[:-1] if a_rows is None else a[torch.where((a_rows >= 0) & (a_rows < A), a_rows, A).long()]
