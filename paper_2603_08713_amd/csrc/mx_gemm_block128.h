@@ -47,6 +47,7 @@ typedef __attribute__((address_space(3))) const float* lds_f32_ptr_t;
 
 constexpr int kMostLoads = 4;  // (a constant of its own: with a bound of the shape's the host pass leaves the kernel out)
 constexpr int kFarOutside = (int)0x80000000;  // past every buffer of a tile's rows, and still with a few rows added
+constexpr int kB128Ahead = 1;  // stages that lines are asked for ahead of their loads
 constexpr int kB128Band = 4;   // tile-rows that an XCD's workgroups walk together
 
 enum B128Mode { kB128Plain = 0, kB128Grouped = 1, kB128Indexed = 2 };
@@ -187,8 +188,11 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
         }
     };
     auto ahead = [&]() __attribute__((always_inline)) {
-        const __amdgpu_buffer_rsrc_t from = ahead_a ? ld.a : ld.b;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr_t)(smem + S::kSpare), 4, ld_stage + 1 < nblk ? at_ld.p : kOutside, (ld_stage + 1) * kScaled, 0, 0);
+        const bool over = ld_stage + kB128Ahead >= nblk;  // (the next tile's first stages too)
+        const int st = ld_stage + kB128Ahead - (over ? nblk : 0), other = -(int)over;
+        const __amdgpu_buffer_rsrc_t here = ahead_a ? ld.a : ld.b, there = ahead_a ? nxt.a : nxt.b;
+        const int off = kMode == kB128Indexed ? (at_ld.p & ~other) | (at_nxt.p & other) : at_ld.p;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(over ? there : here, (lds_ptr_t)(smem + S::kSpare), 4, st < nblk ? off : kOutside, st * kScaled, 0, 0);
     };
     // A stage's loads go out a few at a time behind the barrier that frees their slot: all at once they would hold up every wavefront together
     // until the texture-address unit is through with them.
