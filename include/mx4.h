@@ -426,7 +426,7 @@ typedef enum {
  * num_tokens (DEVICE int64 [1]) or NULL: tokens at and beyond it are padding (a captured batch; mx_kv_plan's row_offsets[num_seqs]) and get no expert; their logits are
  * not read.  T <= 2^20, num_experts <= 1024, top_k <= 32, else MX_EUNSUPPORTED.  Outputs overlap neither each other nor what is read (MX_EINVAL).
  * workspace: DEVICE memory, 4-byte aligned, of at least mx_moe_plan_workspace(...) bytes, which the call overwrites (calls that can run at the same time need one
- * each); NULL where that is 0, up to 128 tokens. */
+ * each); NULL where that is 0 (few tokens). */
 int mx_moe_plan(mx_dtype_t logits_dtype, const void* logits, int64_t ld, int64_t T, const int64_t* num_tokens_or_null, int64_t num_experts, int64_t top_k,
                 mx_score_t score, const float* bias_or_null, int renormalize, float scale, int32_t* experts, float* weights, int64_t* row_offsets,
                 int32_t* rows, int32_t* tokens, void* workspace, int64_t workspace_bytes, void* stream);

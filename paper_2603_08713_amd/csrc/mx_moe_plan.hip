@@ -1,22 +1,29 @@
 // Which experts a step's tokens go to: the top k of every token's logits, their weights, and the places of its rows among the rows of all experts in
 // the experts' order - the row_offsets that the grouped products take - from logits that are on the GPU, so the step can be captured.
 //
-// A wavefront chooses for one token: lane l holds the values of experts l V .. l V + V - 1 as whole numbers in the values' order (NaN above all, an
-// expert at -inf as 0, which is never chosen), and k times the largest is found by DPP, its lowest lane by a ballot: of equal values the expert of
-// the lowest index.  Under a bias the values are sigma(logit) + bias in fp64, where two experts that differ do not come out equal.
+// Sixteen lanes (a row of the DPP network) choose for a token, four tokens a wavefront, or a whole wavefront does.  Lane p holds the values of experts
+// p V .. p V + V - 1 as whole numbers in the values' order (NaN above all, an expert at -inf as 0, which is never chosen).  k times the largest is found
+// by DPP, and of equal ones the lowest index.
+// Under a bias the values are sigma(logit) + bias in fp64, where two experts that differ do not come out equal.
 //
 // Places are a counting sort that keeps the tokens' order: a bit for every expert and token of a chunk of tokens, set in LDS, gives a chunk's counts and
-// the rank of a row among its expert's (bits below it).  One workgroup does everything for few tokens.  For more, the first launch chooses and leaves each
+// the rank of a row among its expert's (bits below it).  One workgroup does everything for few tokens and experts.  For more, the first launch chooses and leaves each
 // chunk's counts in the workspace, the second adds up the counts of the chunks before its own and writes the places: no atomics whose order could show.
-// Bound: latency for a decode step (one launch); for prompts the logits' bytes and two launches.
+// Bound: latency for a decode step (one launch); for prompts two launches and the instructions of the choices, all other than the 5.2 MB that 8192 tokens
+// of 128 experts read and write.  Measured through a captured graph: 64 tokens of 32 experts, 4 taken, 4.9 us (9.6 with a wavefront a token and a workgroup for
+// up to 128 tokens); 8192 of 128, 8 taken, sigmoid and bias, 17 us, of them 11 the choices and 5 the places.
 #include "mx_gemm_shared.h"
 
 namespace mx {
 namespace {
 
-constexpr int kPlanWaves = 16, kPlanThreads = kPlanWaves * kWave;
+constexpr int kPlanWaves = 16, kPlanThreads = kPlanWaves * kWave;  // (place: an expert a thread)
+constexpr int kChooseThreads = 512;
 constexpr int64_t kMostExperts = 1024, kMostChosen = 32, kMostTokens = (int64_t)1 << 20;
-constexpr int kOneChunk = 128;  // tokens up to which one workgroup does everything
+constexpr int kOneChunk = 128;  // tokens up to which one workgroup may do everything
+// It has one compute unit: 64 tokens of 32 experts, 4 of them taken, 5.1 us by one launch, 7.2 by two; 16 of 128, 8 taken, 7.3 and 7.8; 128 of 256, 8 taken, 30
+// and 12.
+constexpr int64_t kOneWork = 16384;  // tokens x experts x choices
 constexpr int kMostChunk = 1024;
 
 struct MoeArgs {
@@ -42,15 +49,29 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {  // of all lanes, in 
     x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false));  // row_bcast:31 into rows 2 and 3
     return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
-__device__ __forceinline__ float wave_sum(float x) {  // in a fixed order, in every lane
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-    return x;
+// Sums over the wavefront, in a fixed order, by DPP (through the LDS crossbar each of the six steps would wait for a round trip): what lane 63 gets, in every lane.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float dpp_of(float x) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kCtrl, kRows, 0xF, kRows == 0xF));
 }
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-    return x;
+template <int kCtrl, int kRows>
+__device__ __forceinline__ double dpp_of(double x) {
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, kCtrl, kRows, 0xF, kRows == 0xF);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), kCtrl, kRows, 0xF, kRows == 0xF);
+    return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+__device__ __forceinline__ float last_lane(float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63)); }
+__device__ __forceinline__ double last_lane(double x) { return __longlong_as_double((long long)readlane64((int64_t)__double_as_longlong(x), 63)); }
+template <typename T>
+__device__ __forceinline__ T wave_sum(T x) {
+    x += dpp_of<0x111, 0xF>(x);  // row_shr:1, 2, 4, 8
+    x += dpp_of<0x112, 0xF>(x);
+    x += dpp_of<0x114, 0xF>(x);
+    x += dpp_of<0x118, 0xF>(x);
+    x += dpp_of<0x142, 0xA>(x);  // row_bcast:15 into rows 1 and 3
+    x += dpp_of<0x143, 0xC>(x);  // row_bcast:31 into rows 2 and 3
+    return last_lane(x);
 }
 
 // Whole numbers above 0 in the order of the values, equal for equal ones; 0 for -inf; NaN the largest.
@@ -66,32 +87,56 @@ __device__ __forceinline__ uint64_t order_of(double x) {
     if (u == 0xFFF0000000000000u) return 0;
     return u >> 63 ? ~u : u | 0x8000000000000000u;
 }
+// 1 / (1 + exp(-x)) in fp64 to a few parts in 2^52, of an x that is fp32.  exp(-|x|) = 2^n exp(r), |r| <= ln 2 / 2, by its series to r^13 (the rest is below
+// 2^-56); the quotient by the reciprocal and two Newton steps.  About 30 operations, where the library's exponential and division are 100: they are made for
+// every token and expert.
 __device__ __forceinline__ double sigmoid(double x) {
-    const double e = exp(-fabs(x));
-    return (x < 0 ? e : 1.0) / (1.0 + e);
+    const double y = fmax(-fabs(x), -800.0);  // (below it: 0)
+    const double n = rint(y * 1.4426950408889634);
+    double r = fma(n, -0.69314718036912382, y);  // ln 2 in two parts, the first of few bits
+    r = fma(n, -1.9082149292705877e-10, r);
+    constexpr double kSeries[] = {1.0 / 6227020800.0, 1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0,
+                                  1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+    double e = kSeries[0];
+#pragma unroll
+    for (int i = 1; i < 14; ++i) e = fma(e, r, kSeries[i]);
+    e = ldexp(e, (int)n);
+    const double d = 1.0 + e;  // in (1, 2]
+    double q = __builtin_amdgcn_rcp(d);
+    q = fma(fma(-d, q, 1.0), q, q);
+    q = fma(fma(-d, q, 1.0), q, q);
+    const double s = x < 0 ? e * q : q;
+    return x != x ? x : s;
 }
 
-// The experts of token t: lane j < k gets the j-th (-1: there is none) and its weight.
-template <int V, bool kBias>
-__device__ __forceinline__ void choose(const MoeArgs& a, int64_t t, int lane, int& expert, float& weight) {
-    float x[V];
-    uint32_t key[V], low[V];  // low: under a bias the lower half of the order
+// The lane's logits of token t (-inf past the last expert).
+template <int V>
+__device__ __forceinline__ void load_logits(const MoeArgs& a, int64_t t, int lane, float (&x)[V]) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int e = lane * V + i;
         x[i] = -INFINITY;
-        key[i] = low[i] = 0;
         if (e < a.E) {
             const int64_t at = t * a.ld + e;
             x[i] = a.bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[at] << 16) : static_cast<const float*>(a.logits)[at];
-            if constexpr (kBias) {
-                // (an expert whose logit or whose bias is -inf is never chosen)
-                const uint64_t o = x[i] == -INFINITY ? 0 : order_of(sigmoid((double)x[i]) + (double)a.bias[e]);
-                key[i] = (uint32_t)(o >> 32);
-                low[i] = (uint32_t)o;
-            } else {
-                key[i] = order_of(x[i]);
-            }
+        }
+    }
+}
+
+// The experts of a token of these logits: lane j < k gets the j-th (-1: there is none) and its weight.  bias: the lane's.
+template <int V, bool kBias>
+__device__ __forceinline__ void choose(const MoeArgs& a, int lane, const float (&x)[V], const float (&bias)[V], int& expert, float& weight) {
+    uint32_t key[V], low[V];  // low: under a bias the lower half of the order
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        low[i] = 0;
+        if constexpr (kBias) {
+            // (an expert whose logit or whose bias is -inf is never chosen)
+            const uint64_t o = x[i] == -INFINITY ? 0 : order_of(sigmoid((double)x[i]) + (double)bias[i]);
+            key[i] = (uint32_t)(o >> 32);
+            low[i] = (uint32_t)o;
+        } else {
+            key[i] = order_of(x[i]);
         }
     }
     expert = -1;
@@ -137,16 +182,8 @@ __device__ __forceinline__ void choose(const MoeArgs& a, int64_t t, int lane, in
         const double total = a.renormalize ? wave_sum(w) : 1.0;
         weight = chosen ? (float)(w / total * (double)a.scale) : 0.f;
     } else {
-        float top = x[0];
-        bool nan = false;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            top = fmaxf(top, x[i]);
-            nan = nan || x[i] != x[i];
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-        if (__builtin_amdgcn_ballot_w64(nan) != 0) top = __uint_as_float(0x7FC00000u);
+        // the largest logit is the first choice's; NaN, where there is one, is above all and makes every weight NaN
+        const float top = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(logit)));
         const float w = chosen ? expf(logit - top) : 0.f;
         float total = w;
         if (!a.renormalize) {
@@ -159,22 +196,138 @@ __device__ __forceinline__ void choose(const MoeArgs& a, int64_t t, int lane, in
     }
 }
 
-// kOne: the only launch, of one workgroup.  Else the first of two: a chunk's choices and counts.
-template <int V, bool kBias, bool kOne>
+// ---- sixteen lanes a token ----
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {  // over the row of 16 lanes, in each of them
+    x = max(x, dpp_quad_xor1(x));
+    x = max(x, dpp_quad_xor2(x));
+    x = max(x, dpp_row_ror4(x));
+    return max(x, dpp_row_ror8(x));
+}
+__device__ __forceinline__ uint32_t row_min(uint32_t x) { return ~row_max(~x); }
+template <typename T>
+__device__ __forceinline__ T row_sum(T x) {  // what lane 0 of the row gets, in each of them (lanes add in different orders)
+    x += dpp_of<0xB1, 0xF>(x);   // quad_perm:[1,0,3,2], [2,3,0,1], row_ror:4, 8
+    x += dpp_of<0x4E, 0xF>(x);
+    x += dpp_of<0x124, 0xF>(x);
+    x += dpp_of<0x128, 0xF>(x);
+    return dpp_of<0x150, 0xF>(x);  // row_newbcast:0
+}
+__device__ __forceinline__ float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order & 0x7FFFFFFFu : ~order); }  // (NaN stays one)
+
+// The experts of the row's token: lane p gets the p-th and the (p + 16)-th (-1: there is none) and their weights.
+template <int V, bool kBias>
+__device__ __forceinline__ void choose_row(const MoeArgs& a, int p, const float (&x)[V], const float (&bias)[V], int (&expert)[2], float (&weight)[2]) {
+    uint32_t key[V], low[V];  // low: under a bias the lower half of the order
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        low[i] = 0;
+        if constexpr (kBias) {
+            // (an expert whose logit or whose bias is -inf is never chosen)
+            const uint64_t o = x[i] == -INFINITY ? 0 : order_of(sigmoid((double)x[i]) + (double)bias[i]);
+            key[i] = (uint32_t)(o >> 32);
+            low[i] = (uint32_t)o;
+        } else {
+            key[i] = order_of(x[i]);
+        }
+    }
+    expert[0] = expert[1] = -1;
+    float logit[2] = {0.f, 0.f}, first = 0.f;
+    for (int j = 0; j < a.k; ++j) {
+        uint32_t mine = key[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) mine = max(mine, key[i]);
+        const uint32_t top = row_max(mine);
+        uint32_t top_low = 0;
+        if constexpr (kBias) {
+            uint32_t mine_low = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) mine_low = key[i] == top ? max(mine_low, low[i]) : mine_low;
+            top_low = row_max(mine_low);
+        }
+        uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+        for (int i = V - 1; i >= 0; --i) at = key[i] == top && (!kBias || low[i] == top_low) ? (uint32_t)(p * V + i) : at;
+        at = row_min(at);
+        float value = value_of(top);
+        if constexpr (kBias) {
+            uint32_t bits = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) bits = at == (uint32_t)(p * V + i) ? __float_as_uint(x[i]) : bits;
+            value = __uint_as_float(row_max(bits));
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = at == (uint32_t)(p * V + i) ? 0u : key[i];
+        if (j == 0) first = value;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (j == p + 16 * h) {
+                expert[h] = top ? (int)at : -1;
+                logit[h] = value;
+            }
+    }
+    if (a.sigmoid) {
+        // (in fp64: the sum of weights that are all far below 1 is still there to divide by)
+        double w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[h] = expert[h] >= 0 ? sigmoid((double)logit[h]) : 0.0;
+        const double total = a.renormalize ? row_sum(w[0] + w[1]) : 1.0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 ? (float)(w[h] / total * (double)a.scale) : 0.f;
+    } else {
+        // the largest logit is the first choice's; NaN, where there is one, is above all and makes every weight NaN
+        float w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[h] = expert[h] >= 0 ? expf(logit[h] - first) : 0.f;
+        float total = w[0] + w[1];
+        if (!a.renormalize) {
+            total = 0.f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) total += p * V + i < a.E && x[i] != -INFINITY ? expf(x[i] - first) : 0.f;
+        }
+        total = row_sum(total);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 ? w[h] / total * a.scale : 0.f;
+    }
+}
+
+// A chunk's choices, and a bit in LDS for each.  V experts a lane, kLanes (16 or 64) lanes a token.
+template <int V, int kLanes, bool kBias, int kThreads>
 __device__ __forceinline__ void choose_chunk(const MoeArgs& a, uint32_t* mask, int64_t t0, int64_t n) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (int i = tid; i < a.E * a.masks; i += kPlanThreads) mask[i] = 0;
+    constexpr int kTokens = kThreads / kLanes, kHolds = kLanes == 16 ? 2 : 1;  // tokens at a time; choices a lane holds
+    const int tid = threadIdx.x, lane = tid % kLanes, group = tid / kLanes;
+    for (int i = tid; i < a.E * a.masks; i += kThreads) mask[i] = 0;
     __syncthreads();
-    for (int i = wave; i < a.chunk; i += kPlanWaves) {
+    float x[V], next[V], bias[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        bias[i] = kBias && lane * V + i < a.E ? a.bias[lane * V + i] : 0.f;
+        next[i] = -INFINITY;
+    }
+    const int64_t stop = min(min(t0 + a.chunk, (int64_t)a.T), n);  // (tokens behind it are padding)
+    if (t0 + group < stop) load_logits<V>(a, t0 + group, lane, next);
+    for (int base = 0; base < a.chunk && t0 + base < a.T; base += kTokens) {  // (the same for the whole workgroup)
+        const int i = base + group;
         const int64_t t = t0 + i;
-        if (t >= a.T) break;
-        int expert = -1;
-        float weight = 0.f;
-        if (t < n) choose<V, kBias>(a, t, lane, expert, weight);
-        if (lane < a.k) {
-            a.experts[t * a.k + lane] = expert;
-            a.weights[t * a.k + lane] = weight;
-            if (expert >= 0) atomicOr(&mask[expert * a.masks + (i >> 5)], 1u << (i & 31));
+        int expert[2] = {-1, -1};
+        float weight[2] = {0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            x[v] = t < stop ? next[v] : -INFINITY;
+            next[v] = -INFINITY;
+        }
+        if (t + kTokens < stop) load_logits<V>(a, t + kTokens, lane, next);  // (under way while this one is chosen for)
+        if constexpr (kLanes == 16) choose_row<V, kBias>(a, lane, x, bias, expert, weight);
+        else if (t < stop) choose<V, kBias>(a, lane, x, bias, expert[0], weight[0]);
+        if (i < a.chunk && t < a.T) {
+#pragma unroll
+            for (int h = 0; h < kHolds; ++h) {
+                const int j = lane + 16 * h;
+                if (j < a.k) {
+                    a.experts[t * a.k + j] = expert[h];
+                    a.weights[t * a.k + j] = weight[h];
+                    if (expert[h] >= 0) atomicOr(&mask[expert[h] * a.masks + (i >> 5)], 1u << (i & 31));
+                }
+            }
         }
     }
     __syncthreads();
@@ -225,13 +378,13 @@ __device__ __forceinline__ void place_chunk(const MoeArgs& a, const uint32_t* ma
     }
 }
 
-template <int V, bool kBias>
+template <int V, int kLanes, bool kBias>
 __global__ __launch_bounds__(kPlanThreads) void moe_plan_one_kernel(MoeArgs a) {
     extern __shared__ uint32_t lds[];
     __shared__ int32_t sums[kPlanWaves];
     uint32_t* mask = lds;
     int32_t *total = reinterpret_cast<int32_t*>(lds + a.E * a.masks), *at = total + a.E, *before = at + a.E;
-    choose_chunk<V, kBias, true>(a, mask, 0, tokens_of(a));
+    choose_chunk<V, kLanes, kBias, kPlanThreads>(a, mask, 0, tokens_of(a));
     if ((int)threadIdx.x < a.E) {
         int c = 0;
         for (int w = 0; w < a.masks; ++w) c += __popc(mask[threadIdx.x * a.masks + w]);
@@ -245,14 +398,14 @@ __global__ __launch_bounds__(kPlanThreads) void moe_plan_one_kernel(MoeArgs a) {
     for (int64_t i = whole + threadIdx.x; i < (int64_t)a.T * a.k; i += kPlanThreads) a.tokens[i] = -1;
 }
 
-template <int V, bool kBias>
-__global__ __launch_bounds__(kPlanThreads) void moe_choose_kernel(MoeArgs a) {
+template <int V, int kLanes, bool kBias>
+__global__ __launch_bounds__(kChooseThreads) void moe_choose_kernel(MoeArgs a) {
     extern __shared__ uint32_t lds[];
-    choose_chunk<V, kBias, false>(a, lds, (int64_t)blockIdx.x * a.chunk, tokens_of(a));
-    if ((int)threadIdx.x < a.E) {
+    choose_chunk<V, kLanes, kBias, kChooseThreads>(a, lds, (int64_t)blockIdx.x * a.chunk, tokens_of(a));
+    for (int e = threadIdx.x; e < a.E; e += kChooseThreads) {
         int c = 0;
-        for (int w = 0; w < a.masks; ++w) c += __popc(lds[threadIdx.x * a.masks + w]);
-        a.counts[(int64_t)blockIdx.x * a.E + threadIdx.x] = c;
+        for (int w = 0; w < a.masks; ++w) c += __popc(lds[e * a.masks + w]);
+        a.counts[(int64_t)blockIdx.x * a.E + e] = c;
     }
 }
 
@@ -269,7 +422,7 @@ __global__ __launch_bounds__(kPlanThreads) void moe_place_kernel(MoeArgs a) {
     const int parts = kPlanThreads / a.E, e = threadIdx.x % a.E, part = threadIdx.x / a.E;
     if (part < parts) {
         int all = 0, ahead = 0;
-#pragma unroll 8
+#pragma unroll 16
         for (int c = part; c < a.chunks; c += parts) {
             const int n = a.counts[(int64_t)c * a.E + e];
             all += n;
@@ -295,33 +448,44 @@ int chunk_of(int64_t T) {  // tokens of a chunk: as few as leave at most 256 chu
     while (c < kMostChunk && (T + c - 1) / c > 256) c *= 2;
     return c;
 }
+bool one_launch(int64_t T, int64_t E, int64_t k) { return T <= kOneChunk && T * E * k <= kOneWork; }
 
-template <int V, bool kBias>
-int launch_plan(const MoeArgs& a0, hipStream_t s) {
+template <int V, int kLanes, bool kBias>
+int launch_one(const MoeArgs& a0, hipStream_t s) {
     MoeArgs a = a0;
-    static LdsOptIn one, choose_, place;
-    if (a.T <= kOneChunk) {
-        a.chunk = kOneChunk;
-        a.masks = kOneChunk / 32;
-        const int bytes = a.E * (a.masks + 3) * 4;
-        if (int st = one.ensure(reinterpret_cast<const void*>(&moe_plan_one_kernel<V, kBias>), (int)kMostExperts * (kOneChunk / 32 + 3) * 4)) return st;
-        hipLaunchKernelGGL((moe_plan_one_kernel<V, kBias>), dim3(1), dim3(kPlanThreads), bytes, s, a);
-        return launch_status();
-    }
+    static LdsOptIn opt;
+    a.chunk = kOneChunk;
+    a.masks = kOneChunk / 32;
+    if (int st = opt.ensure(reinterpret_cast<const void*>(&moe_plan_one_kernel<V, kLanes, kBias>), (int)kMostExperts * (kOneChunk / 32 + 3) * 4)) return st;
+    hipLaunchKernelGGL((moe_plan_one_kernel<V, kLanes, kBias>), dim3(1), dim3(kPlanThreads), a.E * (a.masks + 3) * 4, s, a);
+    return launch_status();
+}
+template <int V, int kLanes, bool kBias>
+int launch_two(const MoeArgs& a0, hipStream_t s) {
+    MoeArgs a = a0;
+    static LdsOptIn choose_, place;
     a.chunk = chunk_of(a.T);
     a.chunks = (a.T + a.chunk - 1) / a.chunk;
     a.masks = a.chunk / 32;
     const int most = (int)kMostExperts * (kMostChunk / 32) * 4;
-    if (int st = choose_.ensure(reinterpret_cast<const void*>(&moe_choose_kernel<V, kBias>), most)) return st;
+    if (int st = choose_.ensure(reinterpret_cast<const void*>(&moe_choose_kernel<V, kLanes, kBias>), most)) return st;
     if (int st = place.ensure(reinterpret_cast<const void*>(&moe_place_kernel), most + (int)kMostExperts * 12)) return st;
-    hipLaunchKernelGGL((moe_choose_kernel<V, kBias>), dim3(a.chunks), dim3(kPlanThreads), a.E * a.masks * 4, s, a);
+    hipLaunchKernelGGL((moe_choose_kernel<V, kLanes, kBias>), dim3(a.chunks), dim3(kChooseThreads), a.E * a.masks * 4, s, a);
     if (int st = launch_status()) return st;
     hipLaunchKernelGGL(moe_place_kernel, dim3(a.chunks), dim3(kPlanThreads), a.E * (a.masks + 3) * 4, s, a);
     return launch_status();
 }
-template <int V>
-int launch_plan_bias(const MoeArgs& a, hipStream_t s) {
-    return a.bias ? launch_plan<V, true>(a, s) : launch_plan<V, false>(a, s);
+// Lanes a token: 16 where there are tokens for all wavefronts; for a few tokens of many experts the longer rows of 16 lanes cost more than they save (16 tokens of
+// 128 experts, 8 taken: 7.1 us by 16 lanes, 5.7 by 64; 8192 of 128, 8 taken, by two launches: 17.0 and 21.6; 16384 of 256: 41 and 47).
+template <bool kBias>
+int launch_plan(const MoeArgs& a, hipStream_t s) {
+    const bool one = one_launch(a.T, a.E, a.k);
+    if (a.E <= 32) return one ? launch_one<2, 16, kBias>(a, s) : launch_two<2, 16, kBias>(a, s);
+    if (a.E <= 64) return one ? launch_one<4, 16, kBias>(a, s) : launch_two<4, 16, kBias>(a, s);
+    if (a.E <= 128) return one ? launch_one<2, 64, kBias>(a, s) : launch_two<8, 16, kBias>(a, s);
+    if (a.E <= 256) return one ? launch_one<4, 64, kBias>(a, s) : launch_two<16, 16, kBias>(a, s);
+    if (a.E <= 512) return one ? launch_one<8, 64, kBias>(a, s) : launch_two<8, 64, kBias>(a, s);
+    return one ? launch_one<16, 64, kBias>(a, s) : launch_two<16, 64, kBias>(a, s);
 }
 
 struct Range {
@@ -344,7 +508,7 @@ int check_sizes(int64_t T, int64_t E, int64_t k) {
 extern "C" int64_t mx_moe_plan_workspace(int64_t T, int64_t num_experts, int64_t top_k) {
     using namespace mx;
     if (int st = check_sizes(T, num_experts, top_k)) return st;
-    if (T <= kOneChunk) return 0;
+    if (one_launch(T, num_experts, top_k)) return 0;
     return (T + chunk_of(T) - 1) / chunk_of(T) * num_experts * 4;
 }
 
@@ -385,9 +549,5 @@ extern "C" int mx_moe_plan(mx_dtype_t logits_dtype, const void* logits, int64_t 
     a.renormalize = renormalize != 0;
     a.scale = scale;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (num_experts <= 64) return launch_plan_bias<1>(a, s);
-    if (num_experts <= 128) return launch_plan_bias<2>(a, s);
-    if (num_experts <= 256) return launch_plan_bias<4>(a, s);
-    if (num_experts <= 512) return launch_plan_bias<8>(a, s);
-    return launch_plan_bias<16>(a, s);
+    return a.bias ? launch_plan<true>(a, s) : launch_plan<false>(a, s);
 }

@@ -72,7 +72,7 @@ def test_what_is_not_refused(lib):
         pytest.skip("the addresses are made up")
     for name, base, changes in (("mx_quantize_block128", QUANT, {}), ("mx_quantize_block128", QUANT, dict(block_rows=1)), ("mx_gemm_block128", GEMM, {}),
                                 ("mx_gemm_block128_grouped", GROUPED, {}), ("mx_gemm_block128_grouped", GROUPED, dict(index=None)), ("mx_moe_plan", PLAN, {}),
-                                ("mx_moe_plan", PLAN, dict(n=None, bias=None, score=0, T=128, work=None, bytes=0)), ("mx_moe_combine", COMBINE, {}),
+                                ("mx_moe_plan", PLAN, dict(n=None, bias=None, score=0, T=64, work=None, bytes=0)), ("mx_moe_combine", COMBINE, {}),
                                 ("mx_moe_combine", COMBINE, dict(out=A + 3 * FAR)), ("mx_moe_combine", COMBINE, dict(add=None, lda=0, k=0, y=None, rows=None, weights=None))):
         assert getattr(lib, name)(*changed(base, **changes)) == EUNSUPPORTED, (name, changes)
 
@@ -87,7 +87,7 @@ def test_empty_calls_do_nothing(lib):
 
 def test_workspace_sizes(lib):
     size = lib.mx_moe_plan_workspace
-    assert size(0, 8, 2) == 0 and size(128, 1024, 32) == 0
+    assert size(0, 8, 2) == 0 and size(64, 32, 4) == 0 and size(128, 1024, 32) == 4 * 1024 * 4
     assert size(129, 8, 2) == 5 * 8 * 4 and size(8192, 128, 8) == 256 * 128 * 4 and size(1 << 20, 1024, 32) == 1024 * 1024 * 4
     assert size(-1, 8, 2) == EINVAL and size(5, 0, 1) == EINVAL and size(5, 8, 9) == EINVAL and size(5, 1025, 1) == EUNSUPPORTED and size(5, 64, 33) == EUNSUPPORTED
     assert size((1 << 20) + 1, 8, 2) == EUNSUPPORTED
