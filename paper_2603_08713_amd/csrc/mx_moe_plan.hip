@@ -21,8 +21,8 @@ constexpr int kPlanWaves = 16, kPlanThreads = kPlanWaves * kWave;  // (place: an
 constexpr int kChooseThreads = 512;
 constexpr int64_t kMostExperts = 1024, kMostChosen = 32, kMostTokens = (int64_t)1 << 20;
 constexpr int kOneChunk = 128;  // tokens up to which one workgroup may do everything
-// It has one compute unit: 64 tokens of 32 experts, 4 of them taken, 5.1 us by one launch, 7.2 by two; 16 of 128, 8 taken, 7.3 and 7.8; 128 of 256, 8 taken, 30
-// and 12.
+// It has one compute unit.  By one launch and by two, us: 64 tokens of 32 experts, 4 of them taken, 4.9 and 6.8; 128 of 32 6.7 and 6.9; 16 of 128, 8 taken, 5.8
+// and 7.5; 32 of 128 8.5 and 7.6; 64 of 128 13.6 and 7.7.
 constexpr int64_t kOneWork = 16384;  // tokens x experts x choices
 constexpr int kMostChunk = 1024;
 
@@ -443,8 +443,11 @@ __global__ __launch_bounds__(kPlanThreads) void moe_place_kernel(MoeArgs a) {
     for (int64_t i = whole + (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < (int64_t)a.T * a.k; i += (int64_t)gridDim.x * kPlanThreads) a.tokens[i] = -1;
 }
 
-int chunk_of(int64_t T) {  // tokens of a chunk: as few as leave at most 256 chunks (each workgroup of the second launch reads all counts)
-    int c = 32;
+// Tokens of a chunk: few, so that a decode step's tokens are on many compute units at once, and as many as leave at most 256 chunks (each workgroup of the
+// second launch reads all counts).
+int chunk_of(int64_t T) {
+    int c = 8;
+    while (c < 32 && (T + c - 1) / c > 64) c *= 2;
     while (c < kMostChunk && (T + c - 1) / c > 256) c *= 2;
     return c;
 }
@@ -466,7 +469,7 @@ int launch_two(const MoeArgs& a0, hipStream_t s) {
     static LdsOptIn choose_, place;
     a.chunk = chunk_of(a.T);
     a.chunks = (a.T + a.chunk - 1) / a.chunk;
-    a.masks = a.chunk / 32;
+    a.masks = (a.chunk + 31) / 32;
     const int most = (int)kMostExperts * (kMostChunk / 32) * 4;
     if (int st = choose_.ensure(reinterpret_cast<const void*>(&moe_choose_kernel<V, kLanes, kBias>), most)) return st;
     if (int st = place.ensure(reinterpret_cast<const void*>(&moe_place_kernel), most + (int)kMostExperts * 12)) return st;
@@ -476,14 +479,15 @@ int launch_two(const MoeArgs& a0, hipStream_t s) {
     return launch_status();
 }
 // Lanes a token: 16 where there are tokens for all wavefronts; for a few tokens of many experts the longer rows of 16 lanes cost more than they save (16 tokens of
-// 128 experts, 8 taken: 7.1 us by 16 lanes, 5.7 by 64; 8192 of 128, 8 taken, by two launches: 17.0 and 21.6; 16384 of 256: 41 and 47).
+// 128 experts, 8 taken: 7.1 us by 16 lanes, 5.7 by 64; 64 of 256, sigmoid and bias, in chunks of 32 by 16 lanes 22.4, in chunks of 8 by 64 10.9; 8192 of 128,
+// 8 taken: 17.0 and 21.6; 16384 of 256: 41 and 47).
 template <bool kBias>
 int launch_plan(const MoeArgs& a, hipStream_t s) {
-    const bool one = one_launch(a.T, a.E, a.k);
+    const bool one = one_launch(a.T, a.E, a.k), few = chunk_of(a.T) == 8;
     if (a.E <= 32) return one ? launch_one<2, 16, kBias>(a, s) : launch_two<2, 16, kBias>(a, s);
     if (a.E <= 64) return one ? launch_one<4, 16, kBias>(a, s) : launch_two<4, 16, kBias>(a, s);
-    if (a.E <= 128) return one ? launch_one<2, 64, kBias>(a, s) : launch_two<8, 16, kBias>(a, s);
-    if (a.E <= 256) return one ? launch_one<4, 64, kBias>(a, s) : launch_two<16, 16, kBias>(a, s);
+    if (a.E <= 128) return one ? launch_one<2, 64, kBias>(a, s) : few ? launch_two<2, 64, kBias>(a, s) : launch_two<8, 16, kBias>(a, s);
+    if (a.E <= 256) return one ? launch_one<4, 64, kBias>(a, s) : few ? launch_two<4, 64, kBias>(a, s) : launch_two<16, 16, kBias>(a, s);
     if (a.E <= 512) return one ? launch_one<8, 64, kBias>(a, s) : launch_two<8, 64, kBias>(a, s);
     return one ? launch_one<16, 64, kBias>(a, s) : launch_two<16, 64, kBias>(a, s);
 }

@@ -87,8 +87,11 @@ def test_empty_calls_do_nothing(lib):
 
 def test_workspace_sizes(lib):
     size = lib.mx_moe_plan_workspace
-    assert size(0, 8, 2) == 0 and size(64, 32, 4) == 0 and size(128, 1024, 32) == 4 * 1024 * 4
-    assert size(129, 8, 2) == 5 * 8 * 4 and size(8192, 128, 8) == 256 * 128 * 4 and size(1 << 20, 1024, 32) == 1024 * 1024 * 4
+    assert size(0, 8, 2) == 0 and size(64, 32, 4) == 0
+    for T in (129, 500, 8192, 100000, 1 << 20):  # whole chunks' counts of 32 bits
+        for E in (1, 8, 128, 1000, 1024):
+            n = size(T, E, 1)
+            assert n > 0 and n % (4 * E) == 0 and n <= 1024 * E * 4, (T, E)
     assert size(-1, 8, 2) == EINVAL and size(5, 0, 1) == EINVAL and size(5, 8, 9) == EINVAL and size(5, 1025, 1) == EUNSUPPORTED and size(5, 64, 33) == EUNSUPPORTED
     assert size((1 << 20) + 1, 8, 2) == EUNSUPPORTED
 
