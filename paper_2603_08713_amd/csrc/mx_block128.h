@@ -53,16 +53,17 @@ __device__ __forceinline__ int b128_tile_rows(const int64_t* off, int num_groups
     for (int base = 64; base < num_groups; base += 64) total += __builtin_amdgcn_readlane(b128_group(off, num_groups, M, tile_rows, lane, base).incl, 63);
     return total;
 }
-// The group of tile-row tm and the rows of that tile (uniform over the wavefront); false past the last group.
+// The group of tile-row tm, its first tile-row, and the rows of tile-row tm (uniform over the wavefront); false past the last group.
 __device__ __forceinline__ bool b128_find(const int64_t* off, int num_groups, int64_t M, int tile_rows, int lane, int tm, B128Group g, int& group, int64_t& row0,
-                                          int64_t& end) {
+                                          int64_t& end, int& first_tm) {
     int before = 0;
     for (int base = 0;;) {
         const uint64_t hit = __builtin_amdgcn_ballot_w64(before + g.incl > tm);
         if (hit != 0) {
             const int idx = __builtin_amdgcn_readfirstlane(__builtin_ctzll(hit));
             group = base + idx;
-            row0 = readlane64(g.lo, idx) + (int64_t)(tm - before - __builtin_amdgcn_readlane(g.incl - g.rows, idx)) * tile_rows;
+            first_tm = before + __builtin_amdgcn_readlane(g.incl - g.rows, idx);
+            row0 = readlane64(g.lo, idx) + (int64_t)(tm - first_tm) * tile_rows;
             end = readlane64(g.hi, idx);
             return true;
         }

@@ -49,6 +49,9 @@ constexpr int kMostLoads = 4;  // (a constant of its own: with a bound of the sh
 constexpr int kFarOutside = (int)0x80000000;  // past every buffer of a tile's rows, and still with a few rows added
 constexpr int kB128Ahead = 1;  // stages that lines are asked for ahead of their loads
 constexpr int kB128Band = 4;   // tile-rows that an XCD's workgroups walk together
+// The same of a group, at most.  (8192 tokens of 32 experts, 4 a token, 2880 x 2880, skewed load: all groups' tile-rows in bands of 4 450 us, 412 without
+// lines asked for ahead; in bands of their own of 3, 6, 16 tile-rows 366, 366, 367; 16 experts of 2048 x 4096, 2 a token: 203, 189, 184, 184, 194.)
+constexpr int kB128GroupBand = 6;
 
 enum B128Mode { kB128Plain = 0, kB128Grouped = 1, kB128Indexed = 2 };
 
@@ -70,28 +73,41 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
 
     auto make = [&](int linear) __attribute__((always_inline)) {
         B128Tile t;
-        const int band = kB128Band * tiles_n, first_m = linear / band * kB128Band, band_rows = min(tiles_m - first_m, kB128Band);
-        t.tm = first_m + linear % band % max(band_rows, 1);
-        t.tn = linear % band / max(band_rows, 1);
+        t.row0 = t.end = 0;
+        t.tm = t.tn = 0;
         bool there = linear < last;
         int group = 0;
-        t.row0 = (int64_t)t.tm * TM;
-        t.end = g.M;
-        if constexpr (kMode != kB128Plain) {
-            if (there) {
-                if (S::kStream && g.num_groups <= kB128TableGroups) {
-                    // the last group whose first tile-row is not behind this one (empty groups share theirs with the next)
-                    const int32_t* table = reinterpret_cast<const int32_t*>(smem + S::kTable);
-                    int upto = 0;
-                    for (int base = 0; base < g.num_groups; base += kWave)
-                        upto += __builtin_popcountll(__builtin_amdgcn_ballot_w64(base + l < g.num_groups && table[3 * (base + l)] <= t.tm));
-                    group = __builtin_amdgcn_readfirstlane(upto - 1);
-                    t.row0 = __builtin_amdgcn_readfirstlane(table[3 * group + 1]) + (int64_t)(t.tm - __builtin_amdgcn_readfirstlane(table[3 * group])) * TM;
-                    t.end = __builtin_amdgcn_readfirstlane(table[3 * group + 2]);
-                } else {
-                    there = b128_find(g.row_offsets, g.num_groups, g.M, TM, l, t.tm, b128_group(g.row_offsets, g.num_groups, g.M, TM, l, 0), group, t.row0, t.end);
-                }
+        auto walk = [&](int from, int rows, int most) __attribute__((always_inline)) {  // bands of at most so many tile-rows, column by column
+            const int band = most * tiles_n, first_m = from / band * most, band_rows = max(min(rows - first_m, most), 1), at = from - first_m * tiles_n;
+            t.tm = first_m + at % band_rows;
+            t.tn = at / band_rows;
+        };
+        if constexpr (kMode == kB128Plain) {
+            walk(linear, tiles_m, kB128Band);
+            t.row0 = (int64_t)t.tm * TM;
+            t.end = g.M;
+        } else if (there) {
+            const int tm = linear / tiles_n;
+            int first_tm = 0;
+            int64_t lo = 0;
+            if (S::kStream && g.num_groups <= kB128TableGroups) {
+                // the last group whose first tile-row is not behind this one (empty groups share theirs with the next)
+                const int32_t* table = reinterpret_cast<const int32_t*>(smem + S::kTable);
+                int upto = 0;
+                for (int base = 0; base < g.num_groups; base += kWave)
+                    upto += __builtin_popcountll(__builtin_amdgcn_ballot_w64(base + l < g.num_groups && table[3 * (base + l)] <= tm));
+                group = __builtin_amdgcn_readfirstlane(upto - 1);
+                first_tm = __builtin_amdgcn_readfirstlane(table[3 * group]);
+                lo = __builtin_amdgcn_readfirstlane(table[3 * group + 1]);
+                t.end = __builtin_amdgcn_readfirstlane(table[3 * group + 2]);
+            } else {
+                there = b128_find(g.row_offsets, g.num_groups, g.M, TM, l, tm, b128_group(g.row_offsets, g.num_groups, g.M, TM, l, 0), group, lo, t.end, first_tm);
+                lo -= (int64_t)(tm - first_tm) * TM;
             }
+            // a group's tiles stand one after the other in the walk, in bands of nearly as many tile-rows each: its weights are read by neighbours, together
+            const int rows = (int)((t.end - lo + TM - 1) / TM), bands = (rows + kB128GroupBand - 1) / kB128GroupBand;
+            walk(linear - first_tm * tiles_n, rows, max((rows + bands - 1) / max(bands, 1), 1));
+            t.row0 = lo + (int64_t)t.tm * TM;
         }
         if (!there) {  // nothing: all loads give zeros
             group = 0;
@@ -119,12 +135,15 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
         return r * bytes;
     };
     struct RowsAt {
-        int a[kMostLoads], s, p;  // a: by index only
+        int a[kMostLoads], s, p;  // a: by index only; p: of the lines asked for ahead
     };
     // Lines of a stage come from beyond the L2 the first time that one of an XCD's workgroups loads them, and a stage is too short to wait for them.
     // The workgroups that share a row or column of tiles ask for a part of its lines each, a stage before they load them: a dword of every
-    // line, into the spare piece.  (Which part goes by a workgroup's place in the walk, the same for all its tiles.)  (8192 x 28672 x 8192: 1725 -> 1620 us.)
-    constexpr bool kAhead = TM == 256 && TN == 256;
+    // line, into the spare piece.  (Which part goes by a workgroup's place in the walk, the same for all its tiles.)  It pays where the codes come from HBM
+    // (8192 x 28672 x 8192: 1738 -> 1621 us; 4096 x 8192 x 14336, weights of 235 MB in turn: 428 -> 404) and costs where the last-level cache holds them
+    // (4096 x 8192 x 8192: 228 -> 233); a user's other layers come in between.  Groups share their columns among fewer workgroups and lose: 412 -> 450 for
+    // 8192 tokens of 32 experts.
+    constexpr bool kAhead = TM == 256 && TN == 256 && kMode == kB128Plain;
     const bool ahead_a = w >= 4;
     auto rows_at = [&](const B128Tile& t) __attribute__((always_inline)) {
         RowsAt x;
@@ -138,8 +157,7 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
         x.s = w < TM / 64 ? row_offset(t, w * 64 + l, nblk * 4) : kOutside;
         x.p = kOutside;
         if constexpr (kAhead) {
-            const int r = ahead_a ? (t.tn & 7) * 32 + (w & 1) * 16 + (l & 15) : (t.tm & 3) * 64 + w * 16 + (l & 15);
-            if (l < 16 && w < 6) x.p = ahead_a ? row_offset(t, r, K) : r * K;
+            if (l < 16 && w < 6) x.p = (ahead_a ? (t.tn & 7) * 32 + (w & 1) * 16 + l : (t.tm & 3) * 64 + w * 16 + l) * K;
         }
         return x;
     };
@@ -184,15 +202,13 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
 #pragma unroll
             for (int i = 0; i < kLoadsA; ++i) at_ld.a[i] = (at_ld.a[i] & ~other) | (at_nxt.a[i] & other);
             at_ld.s = (at_ld.s & ~other) | (at_nxt.s & other);
-            at_ld.p = (at_ld.p & ~other) | (at_nxt.p & other);
         }
     };
     auto ahead = [&]() __attribute__((always_inline)) {
         const bool over = ld_stage + kB128Ahead >= nblk;  // (the next tile's first stages too)
-        const int st = ld_stage + kB128Ahead - (over ? nblk : 0), other = -(int)over;
+        const int st = ld_stage + kB128Ahead - (over ? nblk : 0);
         const __amdgpu_buffer_rsrc_t here = ahead_a ? ld.a : ld.b, there = ahead_a ? nxt.a : nxt.b;
-        const int off = kMode == kB128Indexed ? (at_ld.p & ~other) | (at_nxt.p & other) : at_ld.p;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(over ? there : here, (lds_ptr_t)(smem + S::kSpare), 4, st < nblk ? off : kOutside, st * kScaled, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(over ? there : here, (lds_ptr_t)(smem + S::kSpare), 4, st < nblk ? at_ld.p : kOutside, st * kScaled, 0, 0);
     };
     // A stage's loads go out a few at a time behind the barrier that frees their slot: all at once they would hold up every wavefront together
     // until the texture-address unit is through with them.

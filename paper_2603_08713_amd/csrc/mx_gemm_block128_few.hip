@@ -33,10 +33,10 @@ __global__ __launch_bounds__(S::kWaves* kWave) void block128_few_kernel(Block128
     const int64_t linear = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((int64_t)(blockIdx.x >> 3) >= per_xcd || linear >= total) return;
     const int tm = (int)(linear % tiles_m), tn = (int)(linear / tiles_m);
-    int group = 0;
+    int group = 0, first_tm = 0;
     int64_t row0 = (int64_t)tm * TM, end = g.M;
     if constexpr (kGrouped) {
-        if (!b128_find(g.row_offsets, g.num_groups, g.M, TM, l, tm, groups, group, row0, end)) return;
+        if (!b128_find(g.row_offsets, g.num_groups, g.M, TM, l, tm, groups, group, row0, end, first_tm)) return;
     }
     const int K = (int)g.K, nblk = (K + kScaled - 1) / kScaled;
     const int64_t n0 = (int64_t)tn * TN;
