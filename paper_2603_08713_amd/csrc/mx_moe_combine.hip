@@ -106,6 +106,7 @@ extern "C" int mx_moe_combine(mx_dtype_t y_dtype, const void* y, int64_t num_row
     if ((y_dtype != MX_OUT_F32 && y_dtype != MX_OUT_BF16) || (out_dtype != MX_OUT_F32 && out_dtype != MX_OUT_BF16)) return MX_EINVAL;
     if (T < 0 || top_k < 0 || N < 0 || num_rows < 0 || T > (int64_t)1 << 30 || N > (int64_t)1 << 30 || top_k > 1024 || num_rows > (int64_t)1 << 31) return MX_EINVAL;
     if (ldy < N || ldo < N || (add_or_null && ld_add < N) || ldy > (int64_t)1 << 31 || ldo > (int64_t)1 << 31 || ld_add > (int64_t)1 << 31) return MX_EINVAL;
+    if (num_rows && ldy > ((int64_t)1 << 60) / num_rows) return MX_EINVAL;  // (its bytes would not fit 63 bits)
     if (T == 0 || N == 0) return MX_OK;
     if (!out || (top_k && (!rows || !weights || (num_rows && !y)))) return MX_ENULL;
     const int64_t ysz = y_dtype == MX_OUT_BF16 ? 2 : 4, osz = out_dtype == MX_OUT_BF16 ? 2 : 4;
