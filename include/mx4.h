@@ -403,7 +403,7 @@ int mx_gemm_block128(mx_elem_t a_elem, const uint8_t* a_codes, const float* a_sc
 /* The same by groups: rows row_offsets[e] .. row_offsets[e+1]-1 of C (DEVICE int64 [num_groups+1], as for mx_gemm_mbs_grouped; offsets outside 0 .. M_total
  * are cut) are rows of A times the e-th of the num_groups weights stacked in b_codes [num_groups * N, K] and b_scales [num_groups * ceil(N/128), ceil(K/128)].
  * a_rows (DEVICE int32 [M_total]) names the row of A (a_codes [a_num_rows, K]) that a row of C takes - the `tokens` of mx_moe_plan: tokens are
- * multiplied where they lie - and one outside 0 .. a_num_rows-1 gives a row of zeros; then a_num_rows * K is below 2^32 - 256 (else MX_EUNSUPPORTED).
+ * multiplied where they lie - and one outside 0 .. a_num_rows-1 stands for a row of zeros; then a_num_rows * K is below 2^32 - 256 (else MX_EUNSUPPORTED).
  * NULL: row r of C takes row r of A, a_num_rows >= M_total.  Rows of C at or beyond row_offsets[num_groups] are not written. */
 int mx_gemm_block128_grouped(mx_elem_t a_elem, const uint8_t* a_codes, const float* a_scales, int64_t a_num_rows, const int32_t* a_rows_or_null,
                              mx_elem_t b_elem, const uint8_t* b_codes, const float* b_scales, int32_t num_groups, const int64_t* row_offsets,

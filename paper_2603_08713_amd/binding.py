@@ -155,8 +155,8 @@ def forced(**choices):
     tile shape code of mx_gemm.hip, gemm_elem = which kernel takes an 8-/6-bit GEMM (1 = the main kernel's general
     form, 2 = the main kernel in the form the problem allows, 3 = the few-row kernel, 16 / 17 / 18 = the main kernel on 256 x 128 /
     128 x 128 / 64 x 128 tiles, the last two for K >= 512), attention = 1 or 2 (the kernel for few or for many rows),
-    block128 = 1 / 2 / 3 (the few-row kernel on tiles of 16 x 16, 16 x 32, 32 x 32) or 4 / 5 / 6 / 7 / 8 (64 x 128 tiles, the same with loads further
-    ahead, 128 x 128, 256 x 256, those in a stream)."""
+    block128 = 1 / 2 / 3 (the few-row kernel on tiles of 16 x 16, 16 x 32, 32 x 32) or 4 / 5 / 6 / 7 / 8 / 9 (64 x 128 tiles, the same with K shared
+    by two sets of wavefronts, 128 x 128, 256 x 256, those in a stream, 192 x 256)."""
     allowed = {"quantize_hw", "quantize_elem_hw", "gemm_shape", "gemm_elem", "attention", "block128"}
     if set(choices) - allowed:
         raise TypeError("unknown choice: %s" % sorted(set(choices) - allowed))

@@ -25,7 +25,8 @@ int launch_block128_large(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipSt
 int launch_block128_stream(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);  // the same, a workgroup taking tile after tile: vec_store, K > 128
 int launch_block128_mid(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);     // 128 x 128
 int launch_block128_small(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);   // 64 x 128
-int launch_block128_deep(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);    // the same with loads further ahead, for problems of few tiles
+int launch_block128_halves(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);  // the same, two sets of wavefronts sharing K, for problems of few tiles
+int launch_block128_low(const Block128Args& g, bool a_e5m2, bool b_e5m2, hipStream_t s);     // 192 x 256
 // K among the wavefronts, tiles of 16 x 16 (shape 1), 16 x 32 (2), 32 x 32 (3) (mx_gemm_block128_few.hip).
 int launch_block128_few(const Block128Args& g, bool a_e5m2, bool b_e5m2, int shape, hipStream_t s);
 

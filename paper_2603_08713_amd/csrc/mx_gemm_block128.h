@@ -26,19 +26,22 @@ namespace {
 constexpr int kB128TableGroups = 1024;  // groups whose rows a stream keeps in LDS
 
 // kStream: a workgroup takes tile after tile (rows of C on 16-byte boundaries, K beyond one block); else one.  kSlots: LDS slots of a stage each; loads run
-// kSlots - 1 stages ahead.
-template <int FA_, int FB_, int WM_, int WN_, int kSlots_, bool kStream_ = false>
+// kSlots - 1 stages ahead.  kHalves = 2: two sets of wavefronts take the blocks of K in turn, each with slots of its own, and add up at the end.
+template <int FA_, int FB_, int WM_, int WN_, int kSlots_, bool kStream_ = false, int kHalves_ = 1>
 struct B128Shape {
     static constexpr bool kStream = kStream_;
-    static constexpr int kSlots = kSlots_;
+    static constexpr int kSlots = kSlots_, kHalves = kHalves_;
     static_assert(kSlots == 2 || !kStream, "a tile loads the next one's first stage, not its second");
-    static constexpr int FA = FA_, FB = FB_, WM = WM_, WN = WN_, NW = WM * WN, TM = WM * FA * 32, TN = WN * FB * 32;
+    static_assert(kHalves == 1 || (kHalves == 2 && !kStream && FA_ == 2), "each half stores one fragment of a wavefront's rows");
+    static constexpr int FA = FA_, FB = FB_, WM = WM_, WN = WN_, NW = WM * WN, kThreads = NW * kHalves * kWave, TM = WM * FA * 32, TN = WN * FB * 32;
     // a slot: A's codes, B's codes, the scales of A's rows
     static constexpr int kInB = TM * kScaled, kInS = kInB + TN * kScaled, kSlot = kInS + TM * 4;
     static constexpr int kLoadsA = TM / 8 / NW, kLoadsB = TN / 8 / NW;
-    static constexpr int kSpare = kSlots * kSlot;  // (a piece for loads whose bytes nobody wants)
+    static constexpr int kHalf = kSlots * kSlot;      // bytes of a half's slots
+    static constexpr int kSpare = kHalves * kHalf;  // (a piece for loads whose bytes nobody wants)
     static constexpr int kTable = kSpare + 256, kBytes = kTable + (kStream ? kB128TableGroups * 12 + 16 : 0);
     static_assert(kScaled % (FB * 32) == 0, "a wavefront's columns lie inside one block");
+    static_assert(kHalves == 1 || kHalf >= NW * FB * kWave * 64, "a half's slots take a fragment of rows of every wavefront");
     static_assert(kLoadsA >= 1 && kLoadsA <= 4 && kLoadsB >= 1 && NW % 2 == 0 && TM / 64 <= NW, "every wavefront loads whole pieces");
 };
 
@@ -64,11 +67,13 @@ struct B128Tile {
 
 // The tiles first, first + step, .. (below `last`) of the walk over tiles_m x tiles_n.
 template <int kFmtA, int kFmtB, typename S, B128Mode kMode>
-__device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, int tiles_m, int tiles_n, int first, int last, int step) {
+__device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem0, int tiles_m, int tiles_n, int first, int last, int step) {
     constexpr int FA = S::FA, FB = S::FB, TM = S::TM, TN = S::TN, NW = S::NW, kLoadsA = S::kLoadsA, kLoadsB = S::kLoadsB;
     const int tid = threadIdx.x, l = tid & 63, lr = l & 31, lh = l >> 5;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w % S::WM, wn = w / S::WM;
-    const int K = (int)g.K, nblk = (K + kScaled - 1) / kScaled;
+    constexpr int kHalves = S::kHalves;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = kHalves == 1 ? 0 : wave / NW, w = kHalves == 1 ? wave : wave % NW, wm = w % S::WM, wn = w / S::WM;
+    uint8_t* smem = smem0 + half * S::kHalf;
+    const int K = (int)g.K, nblk = (K + kScaled - 1) / kScaled, stages = (nblk + kHalves - 1) / kHalves;  // (the same for both halves: a block past K is zeros)
     const int blocks_n = (int)((g.N + kScaled - 1) / kScaled);
 
     auto make = [&](int linear) __attribute__((always_inline)) {
@@ -174,7 +179,7 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
     constexpr int kLoads = kLoadsA + kLoadsB + 1;
     auto issue = [&](auto i_) __attribute__((always_inline)) {
         constexpr int i = decltype(i_)::value;
-        const int at = ld_stage * kScaled;
+        const int blk = ld_stage * kHalves + half, at = blk * kScaled;
         uint8_t* slot = smem + ld_slot;
         const bool past = at + piece * 16 >= K;  // K ends inside the block: zeros, not the next row's codes
         // (the empty asm: a register for each load's offset through the whole loop would be one too many)
@@ -187,11 +192,11 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
             __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kLoadsA ? ld.a : ld.b, (lds_ptr_t)(slot + (i < kLoadsA ? 0 : S::kInB) + row0 * kScaled + w * 1024), 16, off, at, 0, 0);
         } else {
             // (a load of 4 bytes a lane from as many rows costs the texture-address unit as much as four of 16: not by wavefronts that own no rows)
-            if (owns) __builtin_amdgcn_raw_ptr_buffer_load_lds(ld.s, (lds_ptr_t)(slot + S::kInS + w * 256), 4, at_ld.s, ld_stage * 4, 0, 0);
+            if (owns) __builtin_amdgcn_raw_ptr_buffer_load_lds(ld.s, (lds_ptr_t)(slot + S::kInS + w * 256), 4, kHalves == 1 || blk < nblk ? at_ld.s : kOutside, blk * 4, 0, 0);
         }
     };
     auto load_next = [&]() __attribute__((always_inline)) {  // (behind the barrier that frees the slot)
-        const bool wrap = ++ld_stage == nblk;
+        const bool wrap = ++ld_stage == stages;
         ld_slot = (ld_slot + S::kSlot) & -(int)(ld_slot != (S::kSlots - 1) * S::kSlot);  // (by bits: a choice would become a branch)
         ld_stage = wrap ? 0 : ld_stage;
         ld.a = wrap ? nxt.a : ld.a;
@@ -274,7 +279,7 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
         a[m][0] = frag(at_a, m * 32 * kScaled, k0);
         a[m][1] = frag(at_a, m * 32 * kScaled, k1);
     }
-    const_f32_ptr_t sb_at = cur.sb;  // of the stage whose fragments are read
+    const_f32_ptr_t sb_at = cur.sb + (kHalves == 1 ? 0 : min(half, nblk - 1));  // of the stage whose fragments are read
     float sb_next = *sb_at;
 #pragma unroll
     for (int m = 0; m < FA; ++m) sa[m] = row_scale(m);
@@ -290,7 +295,7 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
 #pragma unroll
         for (int e = 0; e < 16; ++e) P[1][e] = 0.f;
         s_last = 0.f;
-        for (int st = 0; st < nblk; ++st) {
+        for (int st = 0; st < stages; ++st) {
             static_for<FB>([&](auto n_) {
                 constexpr int n = decltype(n_)::value, next = (n + 1) % FB * 32 * kScaled;
                 auto factors = [&]() __attribute__((always_inline)) {
@@ -305,7 +310,8 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
                     bare_barrier();
                     next_slot();
                     load_next();
-                    sb_at = st + 1 < nblk ? sb_at + 1 : nxt.sb;
+                    if constexpr (kHalves == 1) sb_at = st + 1 < nblk ? sb_at + 1 : nxt.sb;
+                    else sb_at = cur.sb + min((st + 1) * kHalves + half, nblk - 1);
                     sb_next = *sb_at;
 #pragma unroll
                     for (int m = 0; m < FA; ++m) sa[m] = row_scale(m);
@@ -396,15 +402,37 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
             // a time go through the wavefront's own piece of LDS, which is free now, and leave along the rows.
             __builtin_amdgcn_s_waitcnt(wait_imm(0));
             bare_barrier();
+            if constexpr (kHalves == 2) {  // each half gives the other one the fragment of rows that that one stores
+                v4f* give = reinterpret_cast<v4f*>(smem0 + (1 - half) * S::kHalf) + w * FB * kWave * 4 + l;
+                const v4f* take = reinterpret_cast<const v4f*>(smem) + w * FB * kWave * 4 + l;
+                auto exchange = [&](auto mine_) __attribute__((always_inline)) {
+                    constexpr int mine = decltype(mine_)::value, other = FA - 1 - mine;
+                    static_for<FB * 4>([&](auto i_) {
+                        constexpr int i = decltype(i_)::value, n = i / 4, q = i % 4 * 4;
+                        give[i * kWave] = v4f{acc[other][n][q], acc[other][n][q + 1], acc[other][n][q + 2], acc[other][n][q + 3]};
+                    });
+                    __syncthreads();
+                    static_for<FB * 4>([&](auto i_) {
+                        constexpr int i = decltype(i_)::value, n = i / 4, q = i % 4 * 4;
+                        const v4f x = take[i * kWave];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[mine][n][q + e] += x[e];
+                    });
+                };
+                if (half) exchange(std::integral_constant<int, FA - 1>{});
+                else exchange(std::integral_constant<int, 0>{});
+                __syncthreads();  // (the pieces below lie there)
+            }
             auto flush = [&](auto bf16_) __attribute__((always_inline)) {
                 constexpr bool kBf16 = decltype(bf16_)::value;
                 constexpr int esz = kBf16 ? 2 : 4, per = 16 / esz, kFrags = FB * 32 * esz > 256 ? 256 / (32 * esz) : FB, kCols = kFrags * 32, pitch = kCols * esz + 16;
                 constexpr int lanes = kCols * esz / 16, rows = kWave / lanes;
-                static_assert(NW * 32 * pitch <= S::kBytes, "the pieces fit");
+                static_assert(NW * 32 * pitch <= S::kHalf, "the pieces fit");
                 uint8_t* piece_at = smem + w * 32 * pitch;
                 const int rd_row = l / lanes, rd_at = l % lanes;
                 static_for<FA * (FB / kFrags)>([&](auto i_) {
                     constexpr int m = decltype(i_)::value / (FB / kFrags), c = decltype(i_)::value % (FB / kFrags);
+                    if (kHalves == 2 && m != half) return;
                     static_for<kFrags * 4>([&](auto q_) {
                         constexpr int j = decltype(q_)::value / 4, q = decltype(q_)::value % 4, n = c * kFrags + j;
                         const v4f v = {acc[m][n][q * 4], acc[m][n][q * 4 + 1], acc[m][n][q * 4 + 2], acc[m][n][q * 4 + 3]};
@@ -449,7 +477,7 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem, i
 }
 
 template <int kFmtA, int kFmtB, typename S, B128Mode kMode>
-__global__ __launch_bounds__(S::NW* kWave, 2) void gemm_block128_kernel(Block128Args g) {
+__global__ __launch_bounds__(S::kThreads, 2) void gemm_block128_kernel(Block128Args g) {
     extern __shared__ __attribute__((aligned(128))) uint8_t smem[];  // (bits of a piece's place are exchanged in its address)
     // Tiles: workgroups are dealt round-robin to the 8 XCDs; each XCD gets a run of the walk, of which its workgroups take neighbouring tiles.
     int tiles_m = g.tiles_m;
@@ -489,7 +517,7 @@ int launch_b128_mode(const Block128Args& g, unsigned blocks, hipStream_t s) {
     static LdsOptIn opt_in;
     auto* fn = gemm_block128_kernel<kFmtA, kFmtB, S, kMode>;
     if (int st = opt_in.ensure(reinterpret_cast<const void*>(fn), S::kBytes)) return st;
-    hipLaunchKernelGGL(fn, dim3(blocks), dim3(S::NW * kWave), S::kBytes, s, g);
+    hipLaunchKernelGGL(fn, dim3(blocks), dim3(S::kThreads), S::kBytes, s, g);
     return launch_status();
 }
 template <int kFmtA, int kFmtB, typename S>

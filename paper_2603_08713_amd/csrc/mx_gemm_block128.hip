@@ -21,32 +21,36 @@ int check_gemm(mx_elem_t a_elem, mx_elem_t b_elem, const Block128Args& g, mx_dty
 }
 
 // What a kernel takes for a problem, in us: c0 and, for each round of `round` tiles, c1 + c2 for every block of K; a round that is not full costs `part` of
-// one and the rest in proportion (few rows, whose workgroups share a compute unit: 0.7 and up to a round, in proportion beyond it).  Fitted to 55 problems of 1 to 4096 rows,
-// 300 to 14336 columns and K from 256 to 8192.  What each line decides, us: 1 x 4096 x 4096 with 16 x 16 tiles 6.0, with 16 x 32 8.4; 32 x 4096 x 4096 12.7 and 10.1,
-// 32 x 32 13.7; 64 x 4096 x 4096 13.6, 64 x 128 (loads ahead) 21.0; 32 x 14336 x 4096 25.9 and 20.0; 512 x 4096 x 4096 81 and 20.0, 64 x 128 (three
-// workgroups a unit) 28.6; 1024 x 4096 x 4096 38.8 and 34.7, 128 x 128 34.2; 2048 x 4096 x 4096 64 and 48.3, 256 x 256 52.4; 4096 x 4096 x 4096 89 and 67.
+// one and the rest in proportion (few rows, whose workgroups share a compute unit: 0.7 and up to a round, in proportion beyond it).  Fitted to 108 problems, plain
+// and by group, of 1 to 32768 rows, 256 to 14336 columns and K from 256 to 8192: the choice is 2 % above the fastest in the mean, 10 % or more for 9 of them, 31 % at most
+// (3918 rows of 32 groups x 1785 x 1888, where one group has most rows).  What the lines decide at N = K = 4096, us: 1 row 16 x 16 tiles 5.5, 16 x 32 7.4; 32 rows 12.4 and 9.3,
+// 32 x 32 12.5; 64 rows 15.6 and 12.7, 64 x 128 in halves 15.2; 128 rows 22.4 and 15.2; 512 rows in halves 17.1, 64 x 128 (three workgroups a unit) 23.6; 1024 rows 32.3 and
+// 28.3, 128 x 128 30.2; 2048 rows 54.5 and 40.8, 192 x 256 42.3, 256 x 256 47.0; 4096 rows 77.8, 86.8 and 64.3; 1777 x 5001 x 2880 128 x 128 51.3, 192 x 256 37.2, 256 x 256 41.2.
 struct Price {
     int kernel, rows, cols, round;
     double part, c0, c1, c2;
 };
 constexpr Price kPrices[] = {
-    {1, 16, 16, 256, 0.0, 2.4, 0.6, 0.155}, {2, 16, 32, 256, 0.0, 2.6, 0.37, 0.19}, {3, 32, 32, 256, 0.0, 3.2, 1.6, 0.25},
-    {5, 64, 128, 256, 0.75, 1.0, 2.4, 0.52}, {4, 64, 128, 768, 0.6, 1.0, 2.5, 1.03}, {6, 128, 128, 512, 0.55, 1.0, 2.2, 1.42}, {8, 256, 256, 256, 0.72, 5.0, 5.5, 1.62},
+    {1, 16, 16, 256, 0.0, 2.4, 0.568, 0.152}, {2, 16, 32, 256, 0.0, 2.6, 0.313, 0.189}, {3, 32, 32, 256, 0.0, 3.48, 1.15, 0.195},
+    {5, 64, 128, 256, 0.78, 2.71, 2.51, 0.425}, {4, 64, 128, 768, 0.585, 1.55, 1.5, 0.91}, {6, 128, 128, 512, 0.673, 1.43, 2.43, 0.893},
+    {9, 192, 256, 256, 0.627, 0.668, 5.3, 1.48}, {8, 256, 256, 256, 0.816, 2.51, 4.79, 1.43},
 };
 int kernel_for(const Block128Args& g) {
     const double blocks = (double)((g.K + kScaled - 1) / kScaled);
     const double groups = g.num_groups ? (double)min((int64_t)g.num_groups, g.M) : 1.0;
-    // the weights (and rows) have to come from memory whatever the kernel: 3.9 TB/s by the few-row kernels, 5 by the others
+    // the weights (and rows) have to come from memory whatever the kernel
     const double megabytes = (double)(groups * g.N + g.M) * g.K * 1e-6;
-    int best = 0;
-    double least = 0.0;
+    int best = 8;
+    double least = 1e300;
     for (const Price& p : kPrices) {
+        // (more tiles than a launch takes: 2^28 rows of a few columns)
+        if (((double)g.M / p.rows + groups) * (double)((g.N + p.cols - 1) / p.cols) > 4194304.0) continue;
         // (groups: their last tile-row is half full in the mean)
         const double rows = g.num_groups ? max(groups, (double)g.M / p.rows + 0.5 * groups) : (double)((g.M + p.rows - 1) / p.rows);
         const double x = rows * (double)((g.N + p.cols - 1) / p.cols) / p.round, whole = (double)(int64_t)x;
         const double rounds = p.part == 0.0 ? (x > 1.0 ? x + 0.25 : 0.7 + 0.3 * x) : whole + (x > whole ? p.part + (1.0 - p.part) * (x - whole) : 0.0);
-        const double t = p.c0 + rounds * (p.c1 + p.c2 * blocks), price = max(t, 2.0 + megabytes / (p.part == 0.0 ? 3.9 : 5.0)) + 0.1 * t;
-        if (!best || price < least) {
+        const double t = p.c0 + rounds * (p.c1 + p.c2 * blocks), price = max(t, 2.0 + megabytes / 6.2) + 0.1 * t;
+        if (price < least) {
             best = p.kernel;
             least = price;
         }
@@ -54,10 +58,10 @@ int kernel_for(const Block128Args& g) {
     return best;
 }
 
-// force: 0 = by the rule, 1 to 3 = the few-row kernel on tiles of 16 x 16, 16 x 32, 32 x 32, 4 to 7 = tiles of 64 x 128, the same with loads further ahead,
-// 128 x 128, 256 x 256, 8 = those in a stream (as 7 where they cannot).
+// force: 0 = by the rule, 1 to 3 = the few-row kernel on tiles of 16 x 16, 16 x 32, 32 x 32, 4 to 7 = tiles of 64 x 128, the same with K shared by
+// two sets of wavefronts, 128 x 128, 256 x 256, 8 = those in a stream (as 7 where they cannot), 9 = 192 x 256.
 int run(mx_elem_t a_elem, mx_elem_t b_elem, Block128Args& g, mx_dtype_t c_dtype, int force, void* stream) {
-    if (force < 0 || force > 8) return MX_EINVAL;
+    if (force < 0 || force > 9) return MX_EINVAL;
     if (int st = check_device()) return st;
     g.c_bf16 = c_dtype == MX_OUT_BF16;
     g.vec_store = aligned(g.C, 16) && g.ldc * (g.c_bf16 ? 2 : 4) % 16 == 0;
@@ -69,9 +73,10 @@ int run(mx_elem_t a_elem, mx_elem_t b_elem, Block128Args& g, mx_dtype_t c_dtype,
         case 2:
         case 3: return launch_block128_few(g, a5, b5, kernel, s);
         case 4: return launch_block128_small(g, a5, b5, s);
-        case 5: return launch_block128_deep(g, a5, b5, s);
+        case 5: return launch_block128_halves(g, a5, b5, s);
         case 6: return launch_block128_mid(g, a5, b5, s);
         case 7: return launch_block128_large(g, a5, b5, s);
+        case 9: return launch_block128_low(g, a5, b5, s);
         default: return g.vec_store && g.K > kScaled ? launch_block128_stream(g, a5, b5, s) : launch_block128_large(g, a5, b5, s);
     }
 }

@@ -54,8 +54,8 @@ int mx_internal_attention_kv(int force, const void* q_bf16, int64_t ldq, const i
 int64_t mx_internal_attention_kv_workspace(int force, int64_t num_seqs, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
 
 // mx_gemm_block128 (grouped == 0) or mx_gemm_block128_grouped with the kernel chosen: 0 = by the dispatcher's rule, 1 / 2 / 3 = the few-row kernel on tiles of
-// 16 x 16 / 16 x 32 / 32 x 32, 4 / 5 / 6 / 7 = tiles of 64 x 128 / the same with loads further ahead / 128 x 128 / 256 x 256, 8 = those in a stream (as 7
-// where rows of C start anywhere or K is one block).
+// 16 x 16 / 16 x 32 / 32 x 32, 4 / 5 / 6 / 7 = tiles of 64 x 128 / the same with K shared by two sets of wavefronts / 128 x 128 / 256 x 256, 8 = those in a
+// stream (as 7 where rows of C start anywhere or K is one block), 9 = 192 x 256.
 int mx_internal_gemm_block128(int force, mx_elem_t a_elem, const uint8_t* a_codes, const float* a_scales, int64_t a_num_rows, const int32_t* a_rows_or_null,
                               mx_elem_t b_elem, const uint8_t* b_codes, const float* b_scales, int grouped, int32_t num_groups, const int64_t* row_offsets, int64_t M,
                               int64_t N, int64_t K, mx_dtype_t c_dtype, void* C, int64_t ldc, void* stream);

@@ -53,7 +53,7 @@ BAD_PRODUCT = [(dict(ae=5), EINVAL), (dict(be=-1), EINVAL), (dict(ae=0), EUNSUPP
                            (dict(offsets=A + 4), EALIGN), (dict(work=A + 8 * FAR + 2), EALIGN), (dict(experts=A), EINVAL), (dict(weights=A + 300 * 160 - 4), EINVAL),
                            (dict(offsets=A + FAR), EINVAL), (dict(rows=A + 2 * FAR + 156), EINVAL), (dict(tokens=A + 6 * FAR), EINVAL), (dict(work=A + 3 * FAR + 4796), EINVAL)]),
     ("mx_moe_combine", COMBINE, [(dict(ytype=2), EINVAL), (dict(otype=-1), EINVAL), (dict(T=-1), EINVAL), (dict(k=-1), EINVAL), (dict(N=-1), EINVAL), (dict(R=-1), EINVAL), (dict(ldy=39), EINVAL),
-                                 (dict(ldo=39), EINVAL), (dict(lda=39), EINVAL), (dict(k=1025), EINVAL), (dict(T=1 << 31), EINVAL), (dict(T=1 << 25), EINVAL), (dict(y=None), ENULL),
+                                 (dict(ldo=39), EINVAL), (dict(lda=39), EINVAL), (dict(k=1025), EINVAL), (dict(T=1 << 31), EINVAL), (dict(R=1 << 31, ldy=1 << 31), EINVAL), (dict(T=1 << 25), EINVAL), (dict(y=None), ENULL),
                                  (dict(rows=None), ENULL), (dict(weights=None), ENULL), (dict(out=None), ENULL), (dict(y=A + 1), EALIGN), (dict(out=A + 4 * FAR + 2), EALIGN),
                                  (dict(add=A + 3 * FAR + 2), EALIGN), (dict(rows=A + FAR + 2), EALIGN), (dict(out=A), EINVAL), (dict(out=A + FAR + 20), EINVAL),
                                  (dict(out=A + 2 * FAR), EINVAL), (dict(out=A + 3 * FAR + 4), EINVAL), (dict(out=A + 3 * FAR, ldo=44), EINVAL)]),

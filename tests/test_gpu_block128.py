@@ -221,6 +221,20 @@ def test_rows_and_scales_of_other_alignments(mx):
             assert bool((buffer == 777.0).all())
 
 
+def test_product_of_very_many_rows(mx):
+    """More tiles of 64 rows than one launch takes: a kernel of larger ones.  A row is one 1 among 16, so that it picks a weight."""
+    M, N = (1 << 28) + 70, 3
+    one = int(torch.tensor(1.0).to(torch.float8_e4m3fn).view(torch.uint8))
+    a = torch.zeros((M, 16), dtype=torch.uint8, device="cuda")
+    a.view(-1)[:M // 16 * 256].view(-1, 16, 16).diagonal(dim1=1, dim2=2).fill_(one)
+    a[M // 16 * 16:, 5] = one
+    bc, bs = small_operand(generator(1), N, 16, 1, "e4m3")
+    b = ref.values(bc, bs, 128, "e4m3").float()
+    got = mx.mx_gemm_block128("e4m3", a, torch.ones((M, 1), device="cuda"), "e4m3", bc, bs, "bf16")
+    assert bool((got[:M // 16 * 16].view(-1, 16, N) == b.T.to(torch.bfloat16)).all())
+    assert bool((got[M // 16 * 16:] == b[:, 5].to(torch.bfloat16)).all())
+
+
 def test_empty_products(mx):
     z = lambda r, c: torch.zeros((r, c), dtype=torch.uint8, device="cuda")  # noqa: E731
     s = lambda r, c: torch.zeros((r, c), device="cuda")  # noqa: E731
@@ -232,7 +246,7 @@ def test_empty_products(mx):
 
 
 # ---- every kernel on problems that the rule gives to others ---------------------------------------------------------------------
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8, 9])
 @pytest.mark.parametrize("M, N, K", [(1, 5, 16), (70, 300, 128), (129, 131, 2896), (300, 515, 144), (513, 257, 640), (257, 1100, 384)])
 def test_every_kernel_is_exact_on_small_numbers(mx, kernel, M, N, K):
     g = generator(M + N + K)
@@ -248,7 +262,7 @@ def test_every_kernel_is_exact_on_small_numbers(mx, kernel, M, N, K):
         assert bool((wide == 777.0).all())
 
 
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8, 9])
 @pytest.mark.parametrize("index", [False, True])
 def test_every_kernel_by_groups(mx, kernel, index):
     counts, N, K = [130, 0, 64, 1, 300, 0, 31] + [3] * 66, 257, 400
@@ -270,7 +284,7 @@ def test_every_kernel_by_groups(mx, kernel, index):
         at += n
 
 
-@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8])
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8, 9])
 def test_every_kernel_on_quantized_tensors(mx, kernel):
     M, N, K = 300, 400, 2896
     g = generator(3)
