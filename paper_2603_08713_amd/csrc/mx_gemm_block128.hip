@@ -22,7 +22,7 @@ int check_gemm(mx_elem_t a_elem, mx_elem_t b_elem, const Block128Args& g, mx_dty
 
 // What a kernel takes for a problem, in us: c0 and, for each round of `round` tiles, c1 + c2 for every block of K; a round that is not full costs `part` of
 // one and the rest in proportion (few rows, whose workgroups share a compute unit: 0.7 and up to a round, in proportion beyond it).  Fitted to 108 problems, plain
-// and by group, of 1 to 32768 rows, 256 to 14336 columns and K from 256 to 8192: the choice is 2 % above the fastest in the mean, 10 % or more for 9 of them, 31 % at most
+// and by group, of 1 to 32768 rows, 256 to 14336 columns and K from 256 to 8192: the choice is 1.6 % above the fastest in the mean, 10 % or more for 6 of them, 31 % at most
 // (3918 rows of 32 groups x 1785 x 1888, where one group has most rows).  What the lines decide at N = K = 4096, us: 1 row 16 x 16 tiles 5.5, 16 x 32 7.4; 32 rows 12.4 and 9.3,
 // 32 x 32 12.5; 64 rows 15.6 and 12.7, 64 x 128 in halves 15.2; 128 rows 22.4 and 15.2; 512 rows in halves 17.1, 64 x 128 (three workgroups a unit) 23.6; 1024 rows 32.3 and
 // 28.3, 128 x 128 30.2; 2048 rows 54.5 and 40.8, 192 x 256 42.3, 256 x 256 47.0; 4096 rows 77.8, 86.8 and 64.3; 1777 x 5001 x 2880 128 x 128 51.3, 192 x 256 37.2, 256 x 256 41.2.
@@ -37,14 +37,15 @@ constexpr Price kPrices[] = {
 };
 int kernel_for(const Block128Args& g) {
     const double blocks = (double)((g.K + kScaled - 1) / kScaled);
-    const double groups = g.num_groups ? (double)min((int64_t)g.num_groups, g.M) : 1.0;
+    // groups that have rows: fewer than rows and groups would allow, as a router's choices fall (0.7: of a skewed load)
+    const double groups = g.num_groups ? max(1.0, g.num_groups * (1.0 - exp(-0.7 * (double)g.M / g.num_groups))) : 1.0;
     // the weights (and rows) have to come from memory whatever the kernel
     const double megabytes = (double)(groups * g.N + g.M) * g.K * 1e-6;
     int best = 8;
     double least = 1e300;
     for (const Price& p : kPrices) {
         // (more tiles than a launch takes: 2^28 rows of a few columns)
-        if (((double)g.M / p.rows + groups) * (double)((g.N + p.cols - 1) / p.cols) > 4194304.0) continue;
+        if (((double)g.M / p.rows + g.num_groups + 1) * (double)((g.N + p.cols - 1) / p.cols) > 4194304.0) continue;
         // (groups: their last tile-row is half full in the mean)
         const double rows = g.num_groups ? max(groups, (double)g.M / p.rows + 0.5 * groups) : (double)((g.M + p.rows - 1) / p.rows);
         const double x = rows * (double)((g.N + p.cols - 1) / p.cols) / p.round, whole = (double)(int64_t)x;

@@ -37,4 +37,4 @@ extern "C" const char* mx_status_string(int status) {
     }
 }
 
-extern "C" int mx_version(void) { return 300; }
+extern "C" int mx_version(void) { return 400; }
