@@ -335,3 +335,23 @@ def test_tile_after_tile_by_groups(mx, index, K):
         assert torch.equal(out[at:at + n].double(), ref.product(a[at:at + n], b)[0]), e
         at += n
     assert bool((out[-1] == 777.0).all())
+
+
+@pytest.mark.parametrize("kernel", [0, 2, 4, 5, 8, 9])
+def test_more_groups_than_a_table_holds(mx, kernel):
+    """1100 groups, most of one row or none, a few of more than a tile."""
+    N, K = 40, 144
+    counts = [(3 * i) % 4 % 3 for i in range(1100)]
+    counts[7], counts[1030], counts[1099] = 300, 270, 530
+    g = generator(9)
+    rows = sum(counts)
+    ac, as_ = small_operand(g, rows, K, rows, "e4m3")
+    bc, bs = small_operand(g, len(counts) * N, K, len(counts), "e4m3")
+    out = torch.full((rows + 2, N), 777.0, device="cuda")
+    with mx.forced(**({"block128": kernel} if kernel else {})):
+        mx.mx_gemm_block128_grouped("e4m3", ac, as_, "e4m3", bc, bs, offsets_of(counts), N, "f32", out=out[:-2])
+    a, b = ref.values(ac, as_, 1, "e4m3"), torch.cat([ref.values(bc[i * N:(i + 1) * N], bs[i:i + 1], 128, "e4m3") for i in range(len(counts))])
+    of_row = torch.repeat_interleave(torch.arange(len(counts), device="cuda"), torch.tensor(counts, device="cuda"))
+    want = (a[:, None, :] * b.view(len(counts), N, K)[of_row]).sum(2)
+    assert torch.equal(out[:-2].double(), want)
+    assert bool((out[-2:] == 777.0).all())

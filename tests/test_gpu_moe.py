@@ -112,6 +112,20 @@ def test_plan_of_many_tokens(mx):
     assert torch.equal(offsets[1:], torch.bincount(chosen.flatten(), minlength=E).cumsum(0))
 
 
+def test_plan_of_many_tokens_among_the_most_experts(mx):
+    """2^19 and some tokens, 1024 experts: the largest tables in LDS."""
+    T, E = (1 << 19) + 77, 1024
+    chosen = torch.randint(0, E, (T, 1), generator=generator(4), device="cuda")
+    chosen[5000:9000] = 1023
+    logits = torch.zeros((T, E), dtype=torch.bfloat16, device="cuda").scatter_(1, chosen, 8.0)
+    experts, weights, offsets, rows, tokens = mx.mx_moe_plan(logits, 1, "sigmoid", torch.zeros(E, device="cuda"))
+    assert torch.equal(experts.long(), chosen) and bool((weights == 1.0).all())
+    order = torch.sort(chosen.flatten(), stable=True).indices
+    assert torch.equal(tokens.long(), order)
+    assert torch.equal(rows.flatten().long()[order], torch.arange(T, device="cuda"))
+    assert torch.equal(offsets[1:], torch.bincount(chosen.flatten(), minlength=E).cumsum(0))
+
+
 @pytest.mark.parametrize("T", [100, 1000])
 def test_plan_writes_its_outputs_only(mx, T):
     E, k = 33, 4
