@@ -420,6 +420,7 @@ typedef enum {
  * get fewer.  Written:
  *   experts int32, weights fp32 [T, top_k]  the choices, largest first, and their scores (without the bias), divided by their sum if renormalize != 0, times
  *                                           `scale`; -1 and 0 where there is none.  (Renormalized softmax is the softmax over the chosen logits.)
+ *                                           A quotient by the sum is right for every finite logit, also where the scores themselves are below fp64's smallest number.
  *   row_offsets int64 [num_experts+1]       rows of expert e: row_offsets[e] .. row_offsets[e+1]-1, the tokens in order
  *   rows int32 [T, top_k]                   the row of each choice; -1
  *   tokens int32 [T * top_k]                the token of each row; -1 at and beyond row_offsets[num_experts]

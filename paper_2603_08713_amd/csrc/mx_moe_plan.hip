@@ -87,6 +87,7 @@ __device__ __forceinline__ uint64_t order_of(double x) {
     if (u == 0xFFF0000000000000u) return 0;
     return u >> 63 ? ~u : u | 0x8000000000000000u;
 }
+__device__ __forceinline__ float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order & 0x7FFFFFFFu : ~order); }  // (NaN stays one)
 // 1 / (1 + exp(-x)) in fp64 to a few parts in 2^52, of an x that is fp32.  exp(-|x|) = 2^n exp(r), |r| <= ln 2 / 2, by its series to r^13 (the rest is below
 // 2^-56); the quotient by the reciprocal and two Newton steps.  About 30 operations, where the library's exponential and division are 100: they are made for
 // every token and expert.
@@ -108,6 +109,12 @@ __device__ __forceinline__ double sigmoid(double x) {
     const double s = x < 0 ? e * q : q;
     return x != x ? x : s;
 }
+
+// Scores are divided by their sum, which fp64 holds only down to about exp(-700).  Below this sum (all chosen logits are below -485) they are taken relative to the
+// largest one instead: far below 0 the score is exp(x), up to exp(x) of itself, so sigmoid(x - largest - 500) is the same multiple of it for every choice.  At or
+// above it a score that is subnormal, or 0, is less than exp(-200) of the sum: nothing in fp32, whatever `scale`.
+constexpr double kLeastSum = 0x1p-700;
+__device__ __forceinline__ double far_score(float x, float largest) { return sigmoid((double)x - (double)largest - 500.0); }
 
 // The lane's logits of token t (-inf past the last expert).
 template <int V>
@@ -177,9 +184,13 @@ __device__ __forceinline__ void choose(const MoeArgs& a, int lane, const float (
     }
     const bool chosen = expert >= 0;
     if (a.sigmoid) {
-        // (in fp64: the sum of weights that are all far below 1 is still there to divide by)
-        const double w = chosen ? sigmoid((double)logit) : 0.0;
-        const double total = a.renormalize ? wave_sum(w) : 1.0;
+        double w = chosen ? sigmoid((double)logit) : 0.0;
+        double total = a.renormalize ? wave_sum(w) : 1.0;
+        if (total < kLeastSum) {  // (the same for the whole wavefront)
+            const float largest = value_of(wave_max(chosen ? order_of(logit) : 0u));
+            w = chosen ? far_score(logit, largest) : 0.0;
+            total = wave_sum(w);
+        }
         weight = chosen ? (float)(w / total * (double)a.scale) : 0.f;
     } else {
         // the largest logit is the first choice's; NaN, where there is one, is above all and makes every weight NaN
@@ -212,7 +223,6 @@ __device__ __forceinline__ T row_sum(T x) {  // what lane 0 of the row gets, in 
     x += dpp_of<0x128, 0xF>(x);
     return dpp_of<0x150, 0xF>(x);  // row_newbcast:0
 }
-__device__ __forceinline__ float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order & 0x7FFFFFFFu : ~order); }  // (NaN stays one)
 
 // The experts of the row's token: lane p gets the p-th and the (p + 16)-th (-1: there is none) and their weights.
 template <int V, bool kBias>
@@ -266,11 +276,16 @@ __device__ __forceinline__ void choose_row(const MoeArgs& a, int p, const float 
             }
     }
     if (a.sigmoid) {
-        // (in fp64: the sum of weights that are all far below 1 is still there to divide by)
         double w[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) w[h] = expert[h] >= 0 ? sigmoid((double)logit[h]) : 0.0;
-        const double total = a.renormalize ? row_sum(w[0] + w[1]) : 1.0;
+        double total = a.renormalize ? row_sum(w[0] + w[1]) : 1.0;
+        if (total < kLeastSum) {  // (the same for the row of lanes)
+            const float largest = value_of(row_max(max(expert[0] >= 0 ? order_of(logit[0]) : 0u, expert[1] >= 0 ? order_of(logit[1]) : 0u)));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w[h] = expert[h] >= 0 ? far_score(logit[h], largest) : 0.0;
+            total = row_sum(w[0] + w[1]);
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 ? (float)(w[h] / total * (double)a.scale) : 0.f;
     } else {

@@ -355,3 +355,87 @@ def test_more_groups_than_a_table_holds(mx, kernel):
     want = (a[:, None, :] * b.view(len(counts), N, K)[of_row]).sum(2)
     assert torch.equal(out[:-2].double(), want)
     assert bool((out[-2:] == 777.0).all())
+
+
+# ---- scales near the smallest normal number, fp32 results, E5M2 tensors, many tiles a workgroup -----------------------------------
+@pytest.mark.parametrize("kernel", [1, 2, 3, 4, 5, 6, 7, 8, 9])
+@pytest.mark.parametrize("a, b", [("e4m3", "e4m3"), ("e5m2", "e5m2")])
+def test_products_of_scales_below_the_normal_numbers(mx, kernel, a, b):
+    """Scales down to the quantizer's floor, 2^-126: their product rounds to a multiple of 2^-149, which the blocks' sums multiply."""
+    M, N, K = 70, 300, 656
+    g = generator(kernel)
+    codes = lambda rows, elem: (torch.randn((rows, K), generator=g, device="cuda") * ref.TOP[elem] / 8).clamp(-ref.TOP[elem], ref.TOP[elem]).to(ref.F8[elem])  # noqa: E731
+    ac, bc = codes(M, a).view(torch.uint8), codes(N, b).view(torch.uint8)
+    fraction = lambda *shape: 1 + torch.rand(shape, generator=g, device="cuda")  # noqa: E731
+    as_ = fraction(M, ref.blocks(K)) * torch.exp2(torch.randint(-126, -100, (M, 1), generator=g, device="cuda").float())
+    bs = fraction(ref.blocks(N), ref.blocks(K)) * torch.exp2(torch.randint(-30, 0, (ref.blocks(N), 1), generator=g, device="cuda").float())
+    as_[0], as_[1], as_[2] = 2.0 ** -126, 2.0 ** -126, 1.3 * 2.0 ** -73
+    bs[1] = 1.7 * 2.0 ** -73
+    with mx.forced(block128=kernel):
+        got = mx.mx_gemm_block128(a, ac, as_, b, bc, bs, "f32").double()
+    want, size = ref.product(ref.values(ac, as_, 1, a), ref.values(bc, bs, 128, b))
+    # a product of scales is off by half of 2^-149 at most, and so is each of the blocks' multiply-adds
+    ones = lambda rows: torch.ones((rows, ref.blocks(K)), device="cuda")  # noqa: E731
+    _, codes_size = ref.product(ref.values(ac, ones(M), 1, a), ref.values(bc, ones(ref.blocks(N)), 128, b))
+    assert bool(((got - want).abs() <= ref.product_bound(want, size, K, False) + 2.0 ** -149 * (codes_size + ref.blocks(K))).all())
+
+
+@pytest.mark.parametrize("M, N, K", [(1, 512, 4096), (64, 512, 4096), (300, 515, 1168), (1000, 1031, 2896), (2100, 2060, 1024)])
+@pytest.mark.parametrize("a, b", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
+def test_fp32_products_of_quantized_tensors_are_near(mx, M, N, K, a, b):
+    """Each product is cut off below 2^-14 of the largest of its 16.  For quantized N(0, 1) that one is below four times a product's RMS in the mean square, and with
+    errors that do not depend on each other the outputs are off by less than 4 x 2^-14 of theirs in the RMS."""
+    g = generator(M + N + K)
+    x = mx.mx_quantize_block128(torch.randn((M, K), generator=g, device="cuda").to(torch.bfloat16), a)
+    w = mx.mx_quantize_block128((0.02 * torch.randn((N, K), generator=g, device="cuda")).to(torch.bfloat16), b, 128)
+    want, size = ref.product(ref.values(*x, 1, a), ref.values(*w, 128, b))
+    got = mx.mx_gemm_block128(a, *x, b, *w, "f32").double()
+    assert bool(((got - want).abs() <= ref.product_bound(want, size, K, False)).all())
+    off = float((got - want).square().mean().sqrt() / want.square().mean().sqrt())
+    print("rms error / rms: %.3g" % off)
+    assert off <= 2.0 ** -12
+    assert torch.equal(mx.mx_gemm_block128(a, *x, b, *w, "f32").double(), got)  # (the same sums every time)
+
+
+@pytest.mark.parametrize("M, N, K", [(8449, 8456, 144), (8449, 8456, 400)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_a_workgroup_takes_many_tiles(mx, M, N, K, out):
+    """34 x 34 tiles of 256 x 256 among 256 workgroups: four and five each, the last of a row and of a column cut off."""
+    g = generator(M + K)
+    ac, as_ = small_operand(g, M, K, M, "e4m3")
+    bc, bs = small_operand(g, N, K, ref.blocks(N), "e5m2")
+    want, _ = ref.product(ref.values(ac, as_, 1, "e4m3"), ref.values(bc, bs, 128, "e5m2"))
+    dtype = torch.bfloat16 if out == "bf16" else torch.float32
+    wide = torch.full((M + 2, N + 16), 777.0, dtype=dtype, device="cuda")
+    with mx.forced(block128=8):
+        mx.mx_gemm_block128("e4m3", ac, as_, "e5m2", bc, bs, out, out=wide[1:-1, 8:N + 8])
+    assert torch.equal(wide[1:-1, 8:N + 8].double(), want.to(dtype).double())
+    wide[1:-1, 8:N + 8] = 777.0
+    assert bool((wide == 777.0).all())
+
+
+@pytest.mark.parametrize("index", [False, True])
+@pytest.mark.parametrize("K, out", [(144, "bf16"), (400, "f32")])
+def test_many_tiles_by_groups(mx, index, K, out):
+    """97 tile-rows by 12 columns among 256 workgroups; rows behind the last group stay."""
+    counts, N = [3000, 0, 17, 700, 256, 0, 1] + [40] * 70 + [2100], 2904
+    g = generator(K)
+    G, rows = len(counts), sum(counts)
+    A = 900 if index else rows + 1
+    ac, as_ = small_operand(g, A, K, A, "e4m3")
+    bc, bs = small_operand(g, G * N, K, G * ref.blocks(N), "e4m3")
+    a_rows = torch.randint(0, A, (rows + 1,), generator=g, device="cuda").int() if index else None
+    if index:
+        a_rows[5], a_rows[3500], a_rows[7000] = -1, A, 1 << 30
+    dtype = torch.bfloat16 if out == "bf16" else torch.float32
+    c = torch.full((rows + 1, N), 777.0, dtype=dtype, device="cuda")
+    with mx.forced(block128=8):
+        mx.mx_gemm_block128_grouped("e4m3", ac, as_, "e4m3", bc, bs, offsets_of(counts), N, out, a_rows=a_rows, out=c)
+    a = torch.cat((ref.values(ac, as_, 1, "e4m3"), torch.zeros((1, K), dtype=torch.float64, device="cuda")))
+    a = a[:-1] if a_rows is None else a[torch.where((a_rows >= 0) & (a_rows < A), a_rows, A).long()]
+    at = 0
+    for e, n in enumerate(counts):
+        b = ref.values(bc[e * N:(e + 1) * N], bs[e * ref.blocks(N):(e + 1) * ref.blocks(N)], 128, "e4m3")
+        assert torch.equal(c[at:at + n].double(), ref.product(a[at:at + n], b)[0].to(dtype).double()), e
+        at += n
+    assert bool((c[-1] == 777.0).all())

@@ -310,3 +310,56 @@ def test_two_streams_at_once(mx):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(o, want[i]) for o in got[i])
+
+
+# ---- scores that fp64 holds no longer ---------------------------------------------------------------------------------------
+def renormalized_sigmoid(logits, experts, scale=1.0):
+    """score / sum of the chosen scores, by the scores' logarithms: log(1 / (1 + exp(-x))) = -log(1 + exp(-x)), which far below 0 is x itself."""
+    x = logits.cpu().double().numpy()
+    e = experts.cpu().numpy()
+    log = -np.logaddexp(0.0, -np.take_along_axis(x, np.maximum(e, 0).astype(np.int64), 1))
+    log = np.where(e >= 0, log, -np.inf)
+    w = np.exp(log - log.max(1, keepdims=True))
+    return np.where(e >= 0, w / w.sum(1, keepdims=True) * scale, 0.0)
+
+
+@pytest.mark.parametrize("T, E, k", [(16, 20, 5), (16, 70, 5), (100, 500, 20), (200, 33, 18), (700, 128, 8), (300, 1000, 32)])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_plan_shares_scores_of_logits_far_below_zero(mx, T, E, k, with_bias, dtype):
+    """Finite logits whose scores are 0 in 64 bits (or have lost bits there): divided by their sum they are exp(logit - largest), still."""
+    g = generator(T + E + k)
+    low = torch.finfo(dtype).min
+    logits = torch.empty((T, E), device="cuda").uniform_(-820.0, -380.0, generator=g)
+    few = torch.rand((T, E), generator=g, device="cuda") * 3
+    logits[0] = -1e4
+    logits[1] = low
+    logits[2] = -1e9
+    logits[2, 3:5] = -1e9 + 4096
+    logits[3] = low
+    logits[3, 11] = -2000.0  # the only one that counts
+    logits[4] = -1e4 + 0 * few[4]
+    logits[4, :3] = float("-inf")
+    logits[5] = -745.0 - few[5]
+    logits[6] = -708.0 - few[6]
+    logits[7] = -500.0 - 60 * few[7]
+    logits[8] = -485.0 - few[8]
+    logits[9] = low
+    logits[9, 2] = 3.0
+    logits[10] = -1e17
+    logits[11, 1:] = float("-inf")  # one expert, of no score
+    logits[11, 0] = -5000.0
+    logits[12] = -90.0 - 30 * few[12]
+    logits = logits.to(dtype)
+    bias = torch.randn(E, generator=g, device="cuda") if with_bias else None
+    scale = 2.5
+    experts, weights, offsets, rows, tokens = mx.mx_moe_plan(logits, k, "sigmoid", bias, True, scale)
+    want = renormalized_sigmoid(logits, experts, scale)
+    w = weights.cpu().double().numpy()
+    assert not np.isnan(want).any()
+    # fp64 up to here, whose exponentials of differences up to 2^10 are off by 2^-42; rounded to 32 bits once (half of 2^-149 below the normal numbers)
+    assert np.all(np.abs(w - want) <= 2.0 ** -23 * want + 2.0 ** -149)
+    # the choices, places and counts go by the logits as before
+    same = ref.plan(logits, k, "sigmoid", bias, False)
+    for a, b in ((experts, same[0]), (offsets, same[2]), (rows, same[3]), (tokens, same[4])):
+        assert np.array_equal(a.cpu().numpy(), b)
