@@ -416,8 +416,8 @@ typedef enum {
 
 /* Which experts the tokens of a step go to, for the grouped products of this library (all of them take row_offsets).  logits [T, ld] of logits_dtype, one a token
  * and expert.  A token gets the top_k experts of the largest logits - with a bias (fp32 [num_experts]; sigmoid only, else MX_EUNSUPPORTED): of the
- * largest score + bias, taken in fp64 - of equal ones the lowest index.  NaN is above every number.  An expert of logit (or bias) -inf is never taken, so a token may
- * get fewer.  Written:
+ * largest score + bias, taken in fp64 - of equal ones the lowest index.  NaN is above every number.  An expert of logit (or bias) -inf is never taken
+ * (whatever its bias, or logit), so a token may get fewer.  Written:
  *   experts int32, weights fp32 [T, top_k]  the choices, largest first, and their scores (without the bias), divided by their sum if renormalize != 0, times
  *                                           `scale`; -1 and 0 where there is none.  (Renormalized softmax is the softmax over the chosen logits.)
  *                                           A quotient by the sum is right for every finite logit, also where the scores themselves are below fp64's smallest number.

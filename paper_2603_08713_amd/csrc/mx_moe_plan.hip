@@ -138,8 +138,8 @@ __device__ __forceinline__ void choose(const MoeArgs& a, int lane, const float (
     for (int i = 0; i < V; ++i) {
         low[i] = 0;
         if constexpr (kBias) {
-            // (an expert whose logit or whose bias is -inf is never chosen)
-            const uint64_t o = x[i] == -INFINITY ? 0 : order_of(sigmoid((double)x[i]) + (double)bias[i]);
+            // (an expert whose logit or whose bias is -inf is never chosen, also where the other one is NaN)
+            const uint64_t o = x[i] == -INFINITY || bias[i] == -INFINITY ? 0 : order_of(sigmoid((double)x[i]) + (double)bias[i]);
             key[i] = (uint32_t)(o >> 32);
             low[i] = (uint32_t)o;
         } else {
@@ -232,8 +232,8 @@ __device__ __forceinline__ void choose_row(const MoeArgs& a, int p, const float 
     for (int i = 0; i < V; ++i) {
         low[i] = 0;
         if constexpr (kBias) {
-            // (an expert whose logit or whose bias is -inf is never chosen)
-            const uint64_t o = x[i] == -INFINITY ? 0 : order_of(sigmoid((double)x[i]) + (double)bias[i]);
+            // (an expert whose logit or whose bias is -inf is never chosen, also where the other one is NaN)
+            const uint64_t o = x[i] == -INFINITY || bias[i] == -INFINITY ? 0 : order_of(sigmoid((double)x[i]) + (double)bias[i]);
             key[i] = (uint32_t)(o >> 32);
             low[i] = (uint32_t)o;
         } else {

@@ -363,3 +363,22 @@ def test_plan_shares_scores_of_logits_far_below_zero(mx, T, E, k, with_bias, dty
     same = ref.plan(logits, k, "sigmoid", bias, False)
     for a, b in ((experts, same[0]), (offsets, same[2]), (rows, same[3]), (tokens, same[4])):
         assert np.array_equal(a.cpu().numpy(), b)
+
+
+@pytest.mark.parametrize("T, E", [(3, 20), (3, 70), (100, 70), (700, 70), (200, 300)])
+def test_plan_never_takes_an_expert_of_bias_minus_infinity(mx, T, E):
+    """Not even where its logit is NaN or +inf: the plan is that of logits which are -inf there."""
+    k = 6
+    logits = torch.randn((T, E), generator=generator(T + E), device="cuda")
+    bias = torch.randn(E, generator=generator(E), device="cuda")
+    out = torch.arange(E, device="cuda") % 4 == 1
+    bias[out] = float("-inf")
+    logits[0, out] = float("nan")
+    logits[1, 5], logits[2, 1] = float("nan"), float("inf")
+    masked = logits.masked_fill(out, float("-inf"))
+    for renormalize in (True, False):
+        got = mx.mx_moe_plan(logits, k, "sigmoid", bias, renormalize)
+        assert not bool(torch.isnan(got[1]).any())
+        for a, b in zip(got, mx.mx_moe_plan(masked, k, "sigmoid", bias, renormalize)):
+            assert torch.equal(a, b)
+        same_plan(masked, k, "sigmoid", bias, renormalize, got)
