@@ -382,18 +382,19 @@ def test_products_of_scales_below_the_normal_numbers(mx, kernel, a, b):
 
 @pytest.mark.parametrize("M, N, K", [(1, 512, 4096), (64, 512, 4096), (300, 515, 1168), (1000, 1031, 2896), (2100, 2060, 1024)])
 @pytest.mark.parametrize("a, b", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
-def test_fp32_products_of_quantized_tensors_are_near(mx, M, N, K, a, b):
-    """Each product is cut off below 2^-14 of the largest of its 16.  For quantized N(0, 1) that one is below four times a product's RMS in the mean square, and with
-    errors that do not depend on each other the outputs are off by less than 4 x 2^-14 of theirs in the RMS."""
+@pytest.mark.parametrize("larger", [1.0, 100.0])
+def test_fp32_products_of_quantized_tensors_are_near(mx, M, N, K, a, b, larger):
+    """N(0, 1), and one channel in a hundred larger.  Products are cut off 13 bits below the largest of 16 at the most, which alone would allow 2^-12 of the output's RMS for
+    N(0, 1) (the largest of 16 is below four times their RMS); most have fewer bits than that, and 1e-4 is what is promised."""
     g = generator(M + N + K)
-    x = mx.mx_quantize_block128(torch.randn((M, K), generator=g, device="cuda").to(torch.bfloat16), a)
+    x = torch.randn((M, K), generator=g, device="cuda")
+    x[:, ::100] *= larger
+    x = mx.mx_quantize_block128(x.to(torch.bfloat16), a)
     w = mx.mx_quantize_block128((0.02 * torch.randn((N, K), generator=g, device="cuda")).to(torch.bfloat16), b, 128)
     want, size = ref.product(ref.values(*x, 1, a), ref.values(*w, 128, b))
     got = mx.mx_gemm_block128(a, *x, b, *w, "f32").double()
     assert bool(((got - want).abs() <= ref.product_bound(want, size, K, False)).all())
-    off = float((got - want).square().mean().sqrt() / want.square().mean().sqrt())
-    print("rms error / rms: %.3g" % off)
-    assert off <= 2.0 ** -12
+    assert float((got - want).square().mean().sqrt()) <= 1e-4 * float(want.square().mean().sqrt())
     assert torch.equal(mx.mx_gemm_block128(a, *x, b, *w, "f32").double(), got)  # (the same sums every time)
 
 
