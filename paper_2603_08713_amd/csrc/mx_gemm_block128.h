@@ -407,13 +407,15 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem0, 
             if constexpr (kHalves == 2) {  // each half gives the other one the fragment of rows that that one stores
                 v4f* give = reinterpret_cast<v4f*>(smem0 + (1 - half) * S::kHalf) + w * FB * kWave * 4 + l;
                 const v4f* take = reinterpret_cast<const v4f*>(smem) + w * FB * kWave * 4 + l;
-                auto exchange = [&](auto mine_) __attribute__((always_inline)) {
-                    constexpr int mine = decltype(mine_)::value, other = FA - 1 - mine;
+                auto put = [&](auto other_) __attribute__((always_inline)) {
+                    constexpr int other = decltype(other_)::value;
                     static_for<FB * 4>([&](auto i_) {
                         constexpr int i = decltype(i_)::value, n = i / 4, q = i % 4 * 4;
                         give[i * kWave] = v4f{acc[other][n][q], acc[other][n][q + 1], acc[other][n][q + 2], acc[other][n][q + 3]};
                     });
-                    __syncthreads();
+                };
+                auto add = [&](auto mine_) __attribute__((always_inline)) {
+                    constexpr int mine = decltype(mine_)::value;
                     static_for<FB * 4>([&](auto i_) {
                         constexpr int i = decltype(i_)::value, n = i / 4, q = i % 4 * 4;
                         const v4f x = take[i * kWave];
@@ -421,8 +423,13 @@ __device__ __forceinline__ void b128_run(const Block128Args& g, uint8_t* smem0, 
                         for (int e = 0; e < 4; ++e) acc[mine][n][q + e] += x[e];
                     });
                 };
-                if (half) exchange(std::integral_constant<int, FA - 1>{});
-                else exchange(std::integral_constant<int, 0>{});
+                constexpr std::integral_constant<int, 0> first_{};
+                constexpr std::integral_constant<int, FA - 1> last_{};
+                if (half) put(first_);
+                else put(last_);
+                __syncthreads();  // (outside the branch: every wavefront comes to the same barrier)
+                if (half) add(last_);
+                else add(first_);
                 __syncthreads();  // (the pieces below lie there)
             }
             auto flush = [&](auto bf16_) __attribute__((always_inline)) {
