@@ -15,8 +15,11 @@
 //
 // A workgroup of the largest shape takes tile after tile, and the stages of its tiles form one stream: the last stages of a tile load the first ones of
 // the next, and results leave straight from the registers while those are under way.
-// Bound: at 4096 x 14336 x 4096 (238 us, 2.0 PFLOP/s at 1.85 GHz) 3.5 rounds of 256 tiles, in whose clocks matrix instructions take 59 % and vector instructions 46 %;
-// small tiles by what the L2 delivers, 11 to 13 TB/s.  Shapes in turn, us: 64 x 128 346, 128 x 128 296, 192 x 256 242, 256 x 256 as single tiles 237 and in a stream 231.
+// Bound: at 4096 x 14336 x 4096 (238 us, 2.0 PFLOP/s at 1.85 GHz) 3.5 rounds of 256 tiles, in which a SIMD has a matrix instruction of 64 clocks every 112.
+// Its issue port is as loaded: 12 clocks for the instruction, 4.6 for each of the 11.3 vector instructions beside it (8 of them folds), 5 for each of 1.6 LDS
+// reads, 72 in all.  Neither is full; two wavefronts do not keep both busy at once.  Small tiles, where they are as many as the compute units or more: what the
+// L2 delivers, 11 to 13 TB/s.  Shapes in turn, us: 64 x 128 346, 128 x 128 296, 192 x 256 242, 256 x 256 as single tiles 237 and in a stream 231.
+// Registers: the stream takes all 256 vector ones and spills one of them by groups, and 20 to 22 scalar ones always (into lanes of a vector register).
 // LDS image of a stage: [row][128 B], the 16-byte piece c of row r at c ^ ((r >> 1) & 7); a row's scale in a table of its own.
 #pragma once
 

@@ -22,8 +22,9 @@ int check_gemm(mx_elem_t a_elem, mx_elem_t b_elem, const Block128Args& g, mx_dty
 
 // What a kernel takes for a problem, in us: c0 and, for each round of `round` tiles, c1 + c2 for every block of K; a round that is not full costs `part` of
 // one and the rest in proportion (few rows, whose workgroups share a compute unit: 0.7 and up to a round, in proportion beyond it).  Fitted to 108 problems, plain
-// and by group, of 1 to 32768 rows, 256 to 14336 columns and K from 256 to 8192: the choice is 1.6 % above the fastest in the mean, 10 % or more for 6 of them, 31 % at most
-// (3918 rows of 32 groups x 1785 x 1888, where one group has most rows).  What the lines decide at N = K = 4096, us: 1 row 16 x 16 tiles 5.5, 16 x 32 7.4; 32 rows 12.4 and 9.3,
+// and by group, of 1 to 32768 rows, 256 to 14336 columns and K from 256 to 8192: the choice is 1.7 % above the fastest in the mean, 10 % or more for 7 of them, 31 % at most
+// (3918 rows of 32 groups x 1785 x 1888, where one group has most rows; of the plain ones 24 % at 440 x 11713 x 2272).  On 86 others it is 3.1 %, 10 or more for 10,
+// 43 % at most (3340 rows of 32 groups x 1679 x 3328; plain ones 12.5 % at most, 40 x 5839 x 1728).  What the lines decide at N = K = 4096, us: 1 row 16 x 16 tiles 5.5, 16 x 32 7.4; 32 rows 12.4 and 9.3,
 // 32 x 32 12.5; 64 rows 15.6 and 12.7, 64 x 128 in halves 15.2; 128 rows 22.4 and 15.2; 512 rows in halves 17.1, 64 x 128 (three workgroups a unit) 23.6; 1024 rows 32.3 and
 // 28.3, 128 x 128 30.2; 2048 rows 54.5 and 40.8, 192 x 256 42.3, 256 x 256 47.0; 4096 rows 77.8, 86.8 and 64.3; 1777 x 5001 x 2880 128 x 128 51.3, 192 x 256 37.2, 256 x 256 41.2.
 struct Price {

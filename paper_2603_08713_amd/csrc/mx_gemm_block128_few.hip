@@ -5,8 +5,8 @@
 // One v_mfma_f32_16x16x128_f8f6f4 is one P_g of 16 columns by 16 rows.  Weights go in as srcA and activations as srcB, so a lane holds four
 // neighbouring columns of ONE row: the scale of a block is one number a lane, sB one a wavefront, and four multiply-adds fold P_g in.
 // Codes go from memory straight into the operand registers: lane 16 q + r loads bytes 32 q .. 32 q + 31 of row r's block (which k a byte
-// stands for does not matter as long as both operands agree), whole 128-byte lines.  The eight wavefronts of a workgroup take the blocks of K in turn
-// and add up through LDS, in a fixed order.
+// stands for does not matter as long as both operands agree), whole 128-byte lines.  The wavefronts of a workgroup (eight; four on tiles of 16 x 32)
+// take the blocks of K in turn and add up through LDS, in a fixed order.
 // Bound: the weights' bytes, read once for every 16 FM rows (1 x 4096 x 4096 5.4 us, 3.1 TB/s with the launch; 32 x 14336 x 4096 20 us).
 #include "mx_block128.h"
 

@@ -4,14 +4,18 @@
 // Sixteen lanes (a row of the DPP network) choose for a token, four tokens a wavefront, or a whole wavefront does.  Lane p holds the values of experts
 // p V .. p V + V - 1 as whole numbers in the values' order (NaN above all, an expert at -inf as 0, which is never chosen).  k times the largest is found
 // by DPP, and of equal ones the lowest index.
-// Under a bias the values are sigma(logit) + bias in fp64, where two experts that differ do not come out equal.
+// Under a bias the values are sigma(logit) + bias in fp64, which keeps differences down to its spacing near the sum; scores that have run into 1, or that the bias
+// drowns, tie, and the lowest index is taken.
 //
 // Places are a counting sort that keeps the tokens' order: a bit for every expert and token of a chunk of tokens, set in LDS, gives a chunk's counts and
 // the rank of a row among its expert's (bits below it).  One workgroup does everything for few tokens and experts.  For more, the first launch chooses and leaves each
 // chunk's counts in the workspace, the second adds up the counts of the chunks before its own and writes the places: no atomics whose order could show.
-// Bound: latency for a decode step (one launch); for prompts two launches and the instructions of the choices, all other than the 5.2 MB that 8192 tokens
-// of 128 experts read and write.  Measured through a captured graph: 64 tokens of 32 experts, 4 taken, 4.9 us (9.6 with a wavefront a token and a workgroup for
-// up to 128 tokens); 8192 of 128, 8 taken, sigmoid and bias, 17 us, of them 11 the choices and 5 the places.
+// Bound: latency for a decode step (one launch); for prompts two launches, and in the choices their instructions (half of the clocks) and, with two wavefronts a SIMD,
+// the waits between them, all other than the 5.2 MB that 8192 tokens of 128 experts read and write.  Measured through a captured graph: 64 tokens of 32 experts, 4 taken,
+// 4.6 us (9.6 with a wavefront a token and a workgroup for up to 128 tokens); 8192 of 128, 8 taken, sigmoid and bias, 17 us, of them 12 the choices and 5 the places;
+// softmax 12.
+// Registers: without a bias only the kernels for more than 512 experts spill, scalar ones; with one the choices spill 13 (8 experts a lane) to 73 scalar ones (16 a lane)
+// into lanes of a vector register, and the one launch for more than 512 experts 20 vector ones, which its 1024 threads leave it 128 of.
 #include "mx_gemm_shared.h"
 
 namespace mx {
@@ -21,8 +25,8 @@ constexpr int kPlanWaves = 16, kPlanThreads = kPlanWaves * kWave;  // (place: an
 constexpr int kChooseThreads = 512;
 constexpr int64_t kMostExperts = 1024, kMostChosen = 32, kMostTokens = (int64_t)1 << 20;
 constexpr int kOneChunk = 128;  // tokens up to which one workgroup may do everything
-// It has one compute unit.  By one launch and by two, us: 64 tokens of 32 experts, 4 of them taken, 4.9 and 6.8; 128 of 32 6.7 and 6.9; 16 of 128, 8 taken, 5.8
-// and 7.5; 32 of 128 8.5 and 7.6; 64 of 128 13.6 and 7.7.
+// It has one compute unit.  By one launch and by two, us: 64 tokens of 32 experts, 4 of them taken, 4.6 and 6.3; 128 of 32 6.4 and 6.4; 16 of 128, 8 taken, 5.3
+// and 6.7; 32 of 128 7.8 and 7.2; 64 of 128 12.9 and 7.5.
 constexpr int64_t kOneWork = 16384;  // tokens x experts x choices
 constexpr int kMostChunk = 1024;
 
@@ -458,8 +462,9 @@ __global__ __launch_bounds__(kPlanThreads) void moe_place_kernel(MoeArgs a) {
     for (int64_t i = whole + (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < (int64_t)a.T * a.k; i += (int64_t)gridDim.x * kPlanThreads) a.tokens[i] = -1;
 }
 
-// Tokens of a chunk: few, so that a decode step's tokens are on many compute units at once, and as many as leave at most 256 chunks (each workgroup of the
-// second launch reads all counts).
+// Tokens of a chunk: few, so that a decode step's tokens are on many compute units at once, and as many as leave at most 256 chunks, since each workgroup of the
+// second launch reads all counts.  LDS holds the bits of 1024 tokens, so beyond 2^18 tokens there are more chunks, 1024 of them at the most, and those reads grow with
+// the square of the tokens (1 GB out of the caches at 2^20 tokens of 256 experts).
 int chunk_of(int64_t T) {
     int c = 8;
     while (c < 32 && (T + c - 1) / c > 64) c *= 2;
