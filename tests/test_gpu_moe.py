@@ -382,3 +382,16 @@ def test_plan_never_takes_an_expert_of_bias_minus_infinity(mx, T, E):
         for a, b in zip(got, mx.mx_moe_plan(masked, k, "sigmoid", bias, renormalize)):
             assert torch.equal(a, b)
         same_plan(masked, k, "sigmoid", bias, renormalize, got)
+
+
+@pytest.mark.parametrize("T, E", [(8, 24), (8, 100), (500, 100), (500, 300)])
+def test_plan_scores_that_have_run_into_one_tie(mx, T, E):
+    """Scores of 1 in 64 bits, and scores that the bias drowns, are equal whatever their logits: the lowest index is taken."""
+    g = generator(E)
+    far = torch.tensor([45.0, 40.0, 60.0, 3e4, float("inf")], device="cuda")
+    logits = far[torch.randint(0, 5, (T, E), generator=g, device="cuda")]
+    logits[T // 2:] = -far[torch.randint(0, 4, (T - T // 2, E), generator=g, device="cuda")]
+    bias = torch.where(torch.arange(E, device="cuda") % 3 == 0, 0.25, 0.5)
+    got = mx.mx_moe_plan(logits, 5, "sigmoid", bias, False)
+    assert torch.equal(got[0], torch.tensor([1, 2, 4, 5, 7], dtype=torch.int32, device="cuda").expand(T, 5))
+    same_plan(logits, 5, "sigmoid", bias, False, got)
